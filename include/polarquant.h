@@ -301,6 +301,105 @@ int pq_append_keys(const pq_layout* layout, const void* new_keys, pq_dtype key_d
                    int64_t n_pool_pages, void* hip_stream);
 
 /*
+ * ---- chunks of new tokens ----------------------------------------------------------------------
+ * A step of a serving loop that takes in more than one token of a sequence at a time (a prompt, part of
+ * one, drafted tokens) is three calls, ordered on one stream:
+ *   pq_plan_pages       where the new tokens go: pages for them, their slots, the chunks' starts
+ *   pq_append_chunk     their keys and values into the cache
+ *   pq_chunk_attention  their queries over the cache, each over the tokens up to its own
+ * Nothing is read back by the host between them, and all three may be captured in a graph.  The tokens of a batch are
+ * rows [0, n_tokens) of its tensors, sequence s's chunk is rows [starts[s], starts[s + 1]); a
+ * sequence may have none.  Rows from starts[n_seqs] on (padding) belong to nobody.
+ */
+
+/*
+ * pq_plan_pages -- block tables and slots from the request lengths.  Sequence s holds seq_lens[s] tokens
+ * in its block-table row and gets new_lens[s] more; a page that these begin is the next one of free_pages, in the
+ * order of the sequences and, within one, of its tokens.
+ *
+ *   seq_lens, new_lens   device int32 [n_seqs]; negative counts as 0; a sequence's sum, and that of all
+ *                        new_lens, is below 2^31.  Not changed in place: no output may be one of the inputs
+ *   free_pages           device int32 [n_free]: page ids to take from the front of (NULL if n_free is 0)
+ *   block_table          device int32 [n_seqs][max_pages_per_seq]; entries of the pages that new tokens begin are written,
+ *                        -1 where free_pages has run out; others are left as they are.  A page
+ *                        past the row's width has no entry (its place in free_pages is skipped)
+ *   starts               device int32 [n_seqs + 1], written: sums of new_lens before each sequence, and all
+ *   slots                device int64 [max_new_tokens], written: page * g + place in the page of each new token, -1 if its
+ *                        page is missing and for places past the last new token.  Tokens past max_new_tokens get neither
+ *                        slots nor pages
+ *   lens_after           device int32 [n_seqs], written: seq_lens + new_lens
+ *   counts               device int32 [2], written: pages that the new tokens begin (the call has used the first
+ *                        min(counts[0], n_free) of free_pages; more than n_free means that some are missing), new tokens
+ *
+ * n_seqs <= 2^20, max_new_tokens < 2^31.  No workspace; calls that overlap share nothing but their outputs.
+ */
+int pq_plan_pages(const pq_layout* layout, const int32_t* seq_lens, const int32_t* new_lens, int32_t n_seqs,
+                  const int32_t* free_pages, int32_t n_free, int32_t* block_table, int32_t max_pages_per_seq,
+                  int32_t* starts, int64_t* slots, int64_t max_new_tokens, int32_t* lens_after, int32_t* counts,
+                  void* hip_stream);
+
+/*
+ * pq_append_chunk -- pq_append_keys for any number of new tokens per sequence, and their values.  The caches' keys are
+ * byte for byte what pq_append_keys makes of the same keys token by token: complete groups in the packed pages, the
+ * rest as fp16 rows in the residual buffer, whose rows behind the last token are left as they were.
+ *
+ *   keys          device, PQ_F16 or PQ_F32, element i of KV head h of row n at keys[n * key_token_stride + h *
+ *                 key_head_stride + i] (strides in elements, multiples of 16 bytes; 16-byte aligned)
+ *   values        device fp16 with strides of its own (multiples of 16 bytes; 16-byte aligned); NULL: keys only
+ *   n_tokens      rows of keys and values
+ *   starts        device int32 [n_seqs + 1] (pq_plan_pages); non-decreasing, within [0, n_tokens]
+ *   seq_lens      device int32 [n_seqs]: lengths BEFORE the append; a negative one skips the sequence's keys
+ *   slots         device int64 [n_tokens]: where a value row goes (pq_plan_pages); a slot outside the pool, -1 among
+ *                 them, skips the row.  The same slot twice: one of the two rows (with quantized values a mixture).
+ *                 Ignored without values
+ *   residual      device fp16 [n_seqs][n_kv_heads][g][d] (16-byte aligned)
+ *   v_pool, v_bits, v_params_pool   as in pq_decode_attention; quantized values as pq_encode_values makes them, and only the
+ *                 named slots are written
+ *   A group whose page index is >= max_pages_per_seq or whose page id is outside the pool is not encoded.
+ *
+ * n_tokens == 0 or n_seqs == 0 is a no-op.
+ */
+int pq_append_chunk(const pq_layout* layout, const void* keys, pq_dtype key_dtype, int64_t key_token_stride,
+                    int64_t key_head_stride, const void* values, int64_t value_token_stride, int64_t value_head_stride,
+                    int64_t n_tokens, int32_t n_seqs, const int32_t* starts, const int32_t* seq_lens,
+                    const int64_t* slots, void* residual, const int32_t* block_table, int32_t max_pages_per_seq,
+                    void* codes_pool, void* params_pool, void* v_pool, int32_t v_bits, void* v_params_pool,
+                    int64_t n_pool_pages, void* hip_stream);
+
+/* Bytes of scratch pq_chunk_attention needs (256-byte aligned device memory), whatever its window; 0 on invalid arguments. */
+size_t pq_chunk_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_t n_q_heads, int64_t n_tokens,
+                                int32_t max_seq_len);
+
+/*
+ * pq_chunk_attention -- attention of the chunks' queries over the paged cache, the chunks' own tokens in it
+ * (pq_append_chunk comes before).  The query of row starts[s] + i stands at position seq_lens[s] - n + i, n being the length
+ * of sequence s's chunk, and sees the tokens up to its own; with a window, of these, the last `window` and the
+ * first n_sinks.
+ *
+ *   q             device fp16 [n_tokens][n_q_heads][d], post-RoPE (16-byte aligned; PQ_F32: PQ_ERR_UNSUPPORTED).  Query head h reads
+ *                 KV head h / (n_q_heads / n_kv_heads); the ratio may be 1 .. 16
+ *   starts        device int32 [n_seqs + 1] (pq_plan_pages); non-decreasing, within [0, n_tokens]
+ *   seq_lens      device int32 [n_seqs]: lengths WITH the chunks (pq_plan_pages' lens_after); above max_seq_len they are
+ *                 treated as max_seq_len.  A query that would stand before the sequence's first token gets a row of zeros
+ *   window        0: none; n_sinks >= 0 counts with a window only
+ *   out           device fp16 [n_tokens][n_q_heads][d] (16-byte aligned); rows of no chunk are left as they were
+ *   the others    as in pq_decode_attention.  Block-table entries of pages that no query sees are not read and may be anything: pages
+ *                 that a window has left behind can be given back
+ *   workspace     >= pq_chunk_workspace_bytes(layout, n_seqs, n_q_heads, n_tokens, max_seq_len), 256-byte aligned; contents are
+ *                 scratch.  Calls that overlap need one each, captured ones too
+ *
+ * Softmax statistics and sums are fp32.  Reconstructed keys, probabilities and de-quantized values enter the matrix products as
+ * fp16, each rounded once (keys of the uniform grid from two products).  Keys, and values of all tokens of a page that is seen, must be finite.
+ * n_tokens == 0 is a no-op.
+ */
+int pq_chunk_attention(const pq_layout* layout, const void* q, pq_dtype q_dtype, int64_t n_tokens, int32_t n_seqs,
+                       int32_t n_q_heads, const int32_t* starts, const void* codes_pool, const void* params_pool,
+                       const void* v_pool, int32_t v_bits, const void* v_params_pool, int64_t n_pool_pages,
+                       const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* seq_lens,
+                       int32_t max_seq_len, int32_t window, int32_t n_sinks, float sm_scale, void* out,
+                       const void* residual_keys, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
  * pq_score_keys -- the query-key product alone: raw scores q . k~ of every cached token
  * through the lookup table (Section 3.3, Appendix A).  This is the operation whose latency
  * the paper reports in Section 5.2 (query-key multiplication kernel).  Arguments as in

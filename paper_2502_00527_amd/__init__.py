@@ -30,6 +30,7 @@ __all__ = [
     "pq_vq_bytes_per_page", "pq_vq_params_bytes_per_page", "pq_encode_values",
     "pq_probe_read_stream", "pq_decode_kernel_name", "pq_decode_merges_in_kernel",
     "pq_decode_attention_static", "PQ_STATIC_SCRATCH_BYTES",
+    "pq_plan_pages", "pq_append_chunk", "pq_chunk_attention", "pq_chunk_workspace_bytes",
 ]
 
 PQ_F16, PQ_F32 = 0, 1
@@ -88,6 +89,15 @@ _SIGNATURES = {
                               c_int32, c_void_p, c_int32, c_void_p, c_int64, c_void_p, c_void_p]),
     "pq_decode_kernel_name": (ctypes.c_char_p, [_LP, c_int32, c_int32, c_int32, c_int32]),
     "pq_decode_merges_in_kernel": (c_int32, [_LP, c_int32, c_int32, c_int32, c_int32]),
+    "pq_plan_pages": (c_int, [_LP, c_void_p, c_void_p, c_int32, c_void_p, c_int32, c_void_p, c_int32, c_void_p, c_void_p,
+                              c_int64, c_void_p, c_void_p, c_void_p]),
+    "pq_append_chunk": (c_int, [_LP, c_void_p, c_int, c_int64, c_int64, c_void_p, c_int64, c_int64, c_int64, c_int32, c_void_p,
+                                c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_void_p,
+                                c_int64, c_void_p]),
+    "pq_chunk_workspace_bytes": (c_size_t, [_LP, c_int32, c_int32, c_int64, c_int32]),
+    "pq_chunk_attention": (c_int, [_LP, c_void_p, c_int, c_int64, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p,
+                                   c_int32, c_void_p, c_int64, c_void_p, c_int32, c_void_p, c_int32, c_int32, c_int32, c_float,
+                                   c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
     "pq_probe_read_stream": (c_int, [c_void_p, c_size_t, c_void_p, c_void_p]),
 }
 
@@ -117,6 +127,7 @@ class _ByCtypes:
         return None
 
     decode_attention = score_keys = encode_keys = encode_values = append_keys = _decline
+    plan_pages = append_chunk = chunk_attention = _decline
 
 
 def _marshaller():
@@ -239,17 +250,22 @@ def pq_encode_keys(layout: Layout, keys, page_ids, codes_pool, params_pool) -> N
     _check(st, "pq_encode_keys")
 
 
+def _value_pool(layout, v_pool, v_bits, v_params):
+    """Pointers of the value pool and its parameters, and the pages it holds."""
+    import torch
+    if v_bits == 16:
+        return (_dev_ptr(v_pool, "v_pool", (torch.float16,)), None,
+                v_pool.numel() * v_pool.element_size() // max(1, pq_values_bytes_per_page(layout)))
+    return (_dev_ptr(v_pool, "v_pool", (torch.uint8,)), _dev_ptr(v_params, "v_params", (torch.float16,)),
+            v_pool.numel() // max(1, pq_vq_bytes_per_page(layout, v_bits)))
+
+
 def _decode_common(layout, q, codes_pool, params_pool, v_pool, block_table, seq_lens, v_bits=16, v_params=None):
     import torch
     if q.dim() != 3 or q.shape[2] != layout.head_dim:
         raise PolarQuantError("q must be [n_seqs, n_q_heads, head_dim]")
     n_pool_pages = _key_pool_pages(layout, codes_pool, params_pool)
-    if v_bits == 16:
-        v_ptr, vp_ptr = _dev_ptr(v_pool, "v_pool", (torch.float16,)), None
-        n_v_pages = v_pool.numel() * v_pool.element_size() // max(1, pq_values_bytes_per_page(layout))
-    else:
-        v_ptr, vp_ptr = _dev_ptr(v_pool, "v_pool", (torch.uint8,)), _dev_ptr(v_params, "v_params", (torch.float16,))
-        n_v_pages = v_pool.numel() // max(1, pq_vq_bytes_per_page(layout, v_bits))
+    v_ptr, vp_ptr, n_v_pages = _value_pool(layout, v_pool, v_bits, v_params)
     if n_v_pages < n_pool_pages:
         raise PolarQuantError("value pool holds fewer pages than the codes pool")
     return dict(
@@ -388,6 +404,109 @@ def pq_score_keys(layout: Layout, q, codes_pool, params_pool, block_table, seq_l
         _dev_ptr(scores, "scores", (torch.float32,)), scores.shape[-1],
         None if residual is None else _dev_ptr(residual, "residual", (torch.float16,)), _stream())
     _check(st, "pq_score_keys")
+
+
+def pq_plan_pages(layout: Layout, seq_lens, new_lens, free_pages, block_table, starts, slots, lens_after, counts) -> None:
+    """Pages and slots of a batch's new tokens; see include/polarquant.h.  seq_lens, new_lens, lens_after int32 [n_seqs], starts
+    int32 [n_seqs + 1], counts int32 [2], free_pages int32 [n_free], block_table int32 [n_seqs, width], slots int64 [bound of the
+    new tokens]; the last five but free_pages are written."""
+    if _done((_calls or _marshaller()).plan_pages(
+            layout, seq_lens, new_lens, free_pages, block_table, starts, slots, lens_after, counts), "pq_plan_pages"):
+        return
+    import torch
+    i32 = (torch.int32,)
+    n = seq_lens.numel()
+    if new_lens.numel() != n or lens_after.numel() != n or starts.numel() != n + 1 or counts.numel() < 2:
+        raise PolarQuantError("new_lens and lens_after must be [n_seqs], starts [n_seqs + 1], counts [2]")
+    if block_table.dim() != 2 or block_table.shape[0] != n:
+        raise PolarQuantError("block_table must be [n_seqs, pages]")
+    st = load_library().pq_plan_pages(
+        ctypes.byref(layout), _dev_ptr(seq_lens, "seq_lens", i32), _dev_ptr(new_lens, "new_lens", i32), n,
+        _dev_ptr(free_pages, "free_pages", i32), free_pages.numel(), _dev_ptr(block_table, "block_table", i32), block_table.shape[1],
+        _dev_ptr(starts, "starts", i32), _dev_ptr(slots, "slots", (torch.int64,)), slots.numel(),
+        _dev_ptr(lens_after, "lens_after", i32), _dev_ptr(counts, "counts", i32), _stream())
+    _check(st, "pq_plan_pages")
+
+
+def _rows(t, layout: Layout, name: str, dtypes) -> None:
+    if t.dim() != 3 or t.shape[1] != layout.n_kv_heads or t.shape[2] != layout.head_dim:
+        raise PolarQuantError(f"{name} must be [n_tokens, n_kv_heads, head_dim]")
+    if t.dtype not in dtypes or t.stride(2) != 1 or not t.is_cuda:
+        raise PolarQuantError(f"{name} must be a device tensor of one of {dtypes} with a contiguous last dimension")
+
+
+def _per_sequence(starts, seq_lens, block_table) -> int:
+    """Number of sequences of a batch of chunks."""
+    n = seq_lens.numel()
+    if starts.numel() != n + 1 or block_table.dim() != 2 or block_table.shape[0] != n:
+        raise PolarQuantError("starts must be [n_seqs + 1], seq_lens [n_seqs], block_table [n_seqs, pages]")
+    return n
+
+
+def pq_append_chunk(layout: Layout, keys, values, starts, seq_lens, slots, residual, block_table, codes_pool, params_pool,
+                    v_pool=None, v_bits: int = 16, v_params=None) -> None:
+    """keys [n_tokens, n_kv_heads, d] fp16/fp32 and values fp16 (or None) of a batch's chunks into the cache; starts int32
+    [n_seqs + 1], slots int64 [n_tokens] (None without values); seq_lens int32 [n_seqs] = lengths before the append."""
+    if _done((_calls or _marshaller()).append_chunk(
+            layout, keys, values, starts, seq_lens, slots, residual, block_table, codes_pool, params_pool, v_pool, v_bits, v_params),
+            "pq_append_chunk"):
+        return
+    import torch
+    _rows(keys, layout, "keys", (torch.float16, torch.float32))
+    n = _per_sequence(starts, seq_lens, block_table)
+    n_pool_pages = _key_pool_pages(layout, codes_pool, params_pool)
+    _check_residual(layout, residual, n)
+    v_args = (None, 0, 0)
+    v_ptr = vp_ptr = slot_ptr = None
+    if values is not None:
+        _rows(values, layout, "values", (torch.float16,))
+        if values.shape[0] != keys.shape[0] or slots.numel() != keys.shape[0]:
+            raise PolarQuantError("values and slots must have as many rows as keys")
+        v_args = (values.data_ptr(), values.stride(0), values.stride(1))
+        slot_ptr = _dev_ptr(slots, "slots", (torch.int64,))
+        v_ptr, vp_ptr, n_v_pages = _value_pool(layout, v_pool, v_bits, v_params)
+        if n_v_pages < n_pool_pages:
+            raise PolarQuantError("value pool holds fewer pages than the codes pool")
+    st = load_library().pq_append_chunk(
+        ctypes.byref(layout), keys.data_ptr(), _float_kind(keys, "keys"), keys.stride(0), keys.stride(1), *v_args, keys.shape[0], n,
+        _dev_ptr(starts, "starts", (torch.int32,)), _dev_ptr(seq_lens, "seq_lens", (torch.int32,)), slot_ptr,
+        _dev_ptr(residual, "residual", (torch.float16,)), _dev_ptr(block_table, "block_table", (torch.int32,)), block_table.shape[1],
+        _dev_ptr(codes_pool, "codes_pool"), _dev_ptr(params_pool, "params_pool"), v_ptr, v_bits, vp_ptr, n_pool_pages, _stream())
+    _check(st, "pq_append_chunk")
+
+
+def _check_residual(layout: Layout, residual, n_seqs: int) -> None:
+    if residual is not None and residual.numel() < n_seqs * layout.n_kv_heads * layout.group_tokens * layout.head_dim:
+        raise PolarQuantError("residual must be [n_seqs, n_kv_heads, group_tokens, head_dim]")
+
+
+def pq_chunk_workspace_bytes(layout: Layout, n_seqs: int, n_q_heads: int, n_tokens: int, max_seq_len: int) -> int:
+    return load_library().pq_chunk_workspace_bytes(ctypes.byref(layout), n_seqs, n_q_heads, n_tokens, max_seq_len)
+
+
+def pq_chunk_attention(layout: Layout, q, starts, codes_pool, params_pool, v_pool, block_table, seq_lens, max_seq_len: int,
+                       sm_scale: float, out, workspace, residual=None, v_bits: int = 16, v_params=None, window: int = 0,
+                       n_sinks: int = 0) -> None:
+    """Attention of chunks of new tokens, which pq_append_chunk has put into the cache; see include/polarquant.h.  q and `out`
+    fp16 [n_tokens, n_q_heads, d]; starts int32 [n_seqs + 1]; seq_lens int32 [n_seqs] with the chunks; `workspace` a uint8
+    device tensor of at least pq_chunk_workspace_bytes(...) bytes."""
+    if _done((_calls or _marshaller()).chunk_attention(
+            layout, q, starts, codes_pool, params_pool, v_pool, block_table, seq_lens, max_seq_len, sm_scale, out, workspace, residual,
+            v_bits, v_params, window, n_sinks), "pq_chunk_attention"):
+        return
+    import torch
+    n = _per_sequence(starts, seq_lens, block_table)
+    c = _decode_common(layout, q, codes_pool, params_pool, v_pool, block_table, seq_lens, v_bits, v_params)
+    if out.shape != q.shape:
+        raise PolarQuantError("out must have q's shape")
+    _check_residual(layout, residual, n)
+    st = load_library().pq_chunk_attention(
+        ctypes.byref(layout), c["q"], c["qk"], q.shape[0], n, c["n_q"], _dev_ptr(starts, "starts", (torch.int32,)), c["codes"],
+        c["params"], c["v"], c["vbits"], c["vpar"], c["n_pool"], c["bt"], c["width"], c["lens"], max_seq_len, window, n_sinks,
+        sm_scale, _dev_ptr(out, "out", (torch.float16,)),
+        None if residual is None else _dev_ptr(residual, "residual", (torch.float16,)),
+        _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream())
+    _check(st, "pq_chunk_attention")
 
 
 def pq_probe_read_stream(src, sink) -> None:

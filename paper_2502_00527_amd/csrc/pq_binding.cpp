@@ -245,6 +245,115 @@ PyObject* append_keys(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// Sequences of a batch of chunks: starts [n + 1], seq_lens [n], block_table [n, width].
+int32_t sequences(const at::Tensor& starts, const at::Tensor& lens, const at::Tensor& table) {
+  if (starts.numel() != lens.numel() + 1 || table.dim() != 2 || table.size(0) != lens.numel()) throw Decline{};
+  return integer32(lens.numel());
+}
+void* residual_of(PyObject* o, const pq_layout* l, int32_t n_seqs) {
+  const at::Tensor& t = contiguous_tensor(o, at::kHalf);
+  if (t.numel() < static_cast<int64_t>(n_seqs) * l->n_kv_heads * l->group_tokens * l->head_dim) throw Decline{};
+  return t.data_ptr();
+}
+// The value pool and its parameters, which hold at least n_pages pages.
+struct ValuePool {
+  void *pool, *params = nullptr;
+  ValuePool(const pq_layout* l, PyObject* v_pool, PyObject* v_params, int32_t v_bits, int64_t n_pages) {
+    const at::Tensor& v = contiguous_tensor(v_pool, v_bits == 16 ? at::kHalf : at::kByte);
+    if (v_bits != 16) params = contiguous_tensor(v_params, at::kHalf).data_ptr();
+    if (pages(bytes_of(v), v_bits == 16 ? pq_values_bytes_per_page(l) : pq_vq_bytes_per_page(l, v_bits)) < n_pages) throw Decline{};
+    pool = v.data_ptr();
+  }
+};
+int32_t* ints(const at::Tensor& t) { return static_cast<int32_t*>(t.data_ptr()); }
+
+// (layout, seq_lens, new_lens, free_pages, block_table, starts, slots, lens_after, counts)
+PyObject* plan_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 9, [&] {
+    const pq_layout layout = layout_of(a[0]), *const l = &layout;
+    const at::Tensor &lens = contiguous_tensor(a[1], at::kInt), &fresh = contiguous_tensor(a[2], at::kInt), &free_pages = contiguous_tensor(a[3], at::kInt),
+                     &table = contiguous_tensor(a[4], at::kInt), &starts = contiguous_tensor(a[5], at::kInt), &slots = contiguous_tensor(a[6], at::kLong),
+                     &after = contiguous_tensor(a[7], at::kInt), &counts = contiguous_tensor(a[8], at::kInt);
+    const int32_t n_seqs = sequences(starts, lens, table);
+    if (fresh.numel() != n_seqs || after.numel() != n_seqs || counts.numel() < 2) throw Decline{};
+    const int32_t n_free = integer32(free_pages.numel()), width = integer32(table.size(1));
+    const int64_t most = slots.numel();
+    int32_t *const lp = ints(lens), *const np = ints(fresh), *const fp = ints(free_pages), *const tp = ints(table), *const sp = ints(starts),
+            *const ap = ints(after), *const cp = ints(counts);
+    int64_t* const slot = static_cast<int64_t*>(slots.data_ptr());
+    void* const stream = current_stream();
+    return without_lock([&] { return pq_plan_pages(l, lp, np, n_seqs, fp, n_free, tp, width, sp, slot, most, ap, cp, stream); });
+  });
+}
+
+// (layout, keys, values, starts, seq_lens, slots, residual, block_table, codes, params, v_pool, v_bits, v_params)
+PyObject* append_chunk(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 13, [&] {
+    const pq_layout layout = layout_of(a[0]), *const l = &layout;
+    const at::Tensor& keys = device_tensor(a[1]);
+    check_rows(keys, l, true);
+    if (keys.stride(2) != 1) throw Decline{};
+    const pq_dtype kind = float_kind(keys);
+    const at::Tensor &starts = contiguous_tensor(a[3], at::kInt), &lens = contiguous_tensor(a[4], at::kInt), &table = contiguous_tensor(a[7], at::kInt);
+    const int32_t n_seqs = sequences(starts, lens, table), width = integer32(table.size(1)), v_bits = integer32(integer(a[11]));
+    void* const residual = residual_of(a[6], l, n_seqs);
+    const at::Tensor &codes = contiguous_tensor(a[8]), &params = contiguous_tensor(a[9]);
+    const int64_t n_pages = key_pool_pages(l, codes, params), tokens = keys.size(0), key_token = keys.stride(0), key_head = keys.stride(1);
+    void *vp = nullptr, *pool = nullptr, *pool_params = nullptr;
+    int64_t *slot = nullptr, v_token = 0, v_head = 0;
+    if (a[2] != Py_None) {
+      const at::Tensor& values = device_tensor(a[2]);
+      check_rows(values, l, true);
+      const at::Tensor& slots = contiguous_tensor(a[5], at::kLong);
+      if (values.scalar_type() != at::kHalf || values.stride(2) != 1 || values.size(0) != tokens || slots.numel() != tokens) throw Decline{};
+      const ValuePool v(l, a[10], a[12], v_bits, n_pages);
+      vp = values.data_ptr();
+      v_token = values.stride(0);
+      v_head = values.stride(1);
+      slot = static_cast<int64_t*>(slots.data_ptr());
+      pool = v.pool;
+      pool_params = v.params;
+    }
+    void *const kp = keys.data_ptr(), *const cp = codes.data_ptr(), *const pp = params.data_ptr(), *const stream = current_stream();
+    const int32_t *const sp = ints(starts), *const lp = ints(lens), *const tp = ints(table);
+    return without_lock([&] {
+      return pq_append_chunk(l, kp, kind, key_token, key_head, vp, v_token, v_head, tokens, n_seqs, sp, lp, slot, residual, tp, width, cp, pp, pool,
+                             v_bits, pool_params, n_pages, stream);
+    });
+  });
+}
+
+// (layout, q, starts, codes, params, v_pool, block_table, seq_lens, max_seq_len, sm_scale, out, workspace, residual, v_bits, v_params,
+//  window, n_sinks)
+PyObject* chunk_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 17, [&] {
+    const pq_layout layout = layout_of(a[0]), *const l = &layout;
+    const at::Tensor& q = contiguous_tensor(a[1]);
+    check_rows(q, l, false);
+    const pq_dtype kind = float_kind(q);
+    const at::Tensor &codes = contiguous_tensor(a[3]), &params = contiguous_tensor(a[4]);
+    const int64_t n_pages = key_pool_pages(l, codes, params), tokens = q.size(0);
+    const int32_t v_bits = integer32(integer(a[13]));
+    const ValuePool v(l, a[5], a[14], v_bits, n_pages);
+    const at::Tensor &starts = contiguous_tensor(a[2], at::kInt), &table = contiguous_tensor(a[6], at::kInt), &lens = contiguous_tensor(a[7], at::kInt);
+    const int32_t n_seqs = sequences(starts, lens, table), n_heads = integer32(q.size(1)), width = integer32(table.size(1)),
+                  max_seq_len = integer32(integer(a[8])), window = integer32(integer(a[15])), n_sinks = integer32(integer(a[16]));
+    if (!PyFloat_CheckExact(a[9])) throw Decline{};
+    const float sm_scale = static_cast<float>(PyFloat_AS_DOUBLE(a[9]));
+    const at::Tensor &out = contiguous_tensor(a[10], at::kHalf), &workspace = contiguous_tensor(a[11]);
+    if (out.sizes() != q.sizes()) throw Decline{};
+    void* const residual = a[12] == Py_None ? nullptr : residual_of(a[12], l, n_seqs);
+    void *const qp = q.data_ptr(), *const cp = codes.data_ptr(), *const pp = params.data_ptr(), *const op = out.data_ptr(), *const ws = workspace.data_ptr(),
+         *const stream = current_stream();
+    const int32_t *const sp = ints(starts), *const tp = ints(table), *const lp = ints(lens);
+    const size_t ws_bytes = bytes_of(workspace);
+    return without_lock([&] {
+      return pq_chunk_attention(l, qp, kind, tokens, n_seqs, n_heads, sp, cp, pp, v.pool, v_bits, v.params, n_pages, tp, width, lp, max_seq_len, window,
+                                n_sinks, sm_scale, op, residual, ws, ws_bytes, stream);
+    });
+  });
+}
+
 PyObject* set_layout_type(PyObject*, PyObject* type) {
   Py_INCREF(type);
   Py_XSETREF(layout_type, type);
@@ -253,7 +362,8 @@ PyObject* set_layout_type(PyObject*, PyObject* type) {
 
 #define PQ_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {PQ_METHOD(decode_attention), PQ_METHOD(score_keys), PQ_METHOD(encode_keys), PQ_METHOD(encode_values),
-                         PQ_METHOD(append_keys), {"set_layout_type", set_layout_type, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         PQ_METHOD(append_keys), PQ_METHOD(plan_pages), PQ_METHOD(append_chunk), PQ_METHOD(chunk_attention),
+                         {"set_layout_type", set_layout_type, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Argument marshalling for libpolarquant.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

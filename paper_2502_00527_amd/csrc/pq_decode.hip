@@ -141,14 +141,6 @@ bool launch_grouped(int rt, int v_bits, const DecodeArgs& a, dim3 grid, hipStrea
   }
 }
 
-// Index of a bit allocation in the key-side tables of its symbol width (pq_decode_matrix.hpp).
-int key_table_index(const pq_layout* l) {
-  const int w = l->r_bits + l->t_bits;
-  for (int i = 0; i < 3; ++i)
-    if (kTableRadiusBits[w == 8][i] == l->r_bits) return i;
-  return 0;                                  // not reached: layout_supported() admits what is built
-}
-
 // The caller's workspace: the chunks' partials and the units' arrival words.  Its size is that of
 // the chunk plan of plan_chunks() or of one partial for each of four_page_groups() + units, whichever
 // is larger; plan_uniform() and device_cut() keep within it.  (Of the words only `units` are used.

@@ -108,6 +108,13 @@ struct KeyTables {
 };
 // the bit allocations of a width, in table order
 constexpr int kTableRadiusBits[2][3] = {{3, 4, 2}, {4, 5, 3}};       // W = 6: (3,3) (4,2) (2,4); W = 8: (4,4) (5,3) (3,5)
+// Index of a bit allocation in the key-side tables of its symbol width.
+[[maybe_unused]] int key_table_index(const pq_layout* l) {
+  const int w = l->r_bits + l->t_bits;
+  for (int i = 0; i < 3; ++i)
+    if (kTableRadiusBits[w == 8][i] == l->r_bits) return i;
+  return 0;                                  // not reached: layout_supported() admits what is built
+}
 template <int W>
 constexpr KeyTables<W> make_key_tables() {
   constexpr double kPi = 3.14159265358979323846;
