@@ -399,6 +399,25 @@ int pq_chunk_attention(const pq_layout* layout, const void* q, pq_dtype q_dtype,
                        int32_t max_seq_len, int32_t window, int32_t n_sinks, float sm_scale, void* out,
                        const void* residual_keys, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* Bytes of scratch pq_window_attention needs (256-byte aligned device memory); 0 on invalid arguments. */
+size_t pq_window_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_t n_q_heads, int32_t max_seq_len,
+                                 int32_t window, int32_t n_sinks);
+
+/*
+ * pq_window_attention -- pq_decode_attention of a model with a sliding window: a query sees the last `window` tokens of its
+ * sequence (its own with them) and the first n_sinks.  Arguments as in pq_decode_attention, and
+ *   window, n_sinks   window >= 1, n_sinks >= 0; where they meet the sequence is seen as a whole
+ *   workspace         >= pq_window_workspace_bytes(...) of the same arguments
+ * Pages between the sinks and the window are not read: their block-table entries may be anything, so that the pages can be
+ * given back.  Results are pq_decode_attention's over the tokens that are seen, in precision too.
+ */
+int pq_window_attention(const pq_layout* layout, const void* q, pq_dtype q_dtype, int32_t n_seqs, int32_t n_q_heads,
+                        const void* codes_pool, const void* params_pool, const void* v_pool, int32_t v_bits,
+                        const void* v_params_pool, int64_t n_pool_pages, const int32_t* block_table,
+                        int32_t max_pages_per_seq, const int32_t* seq_lens, int32_t max_seq_len, int32_t window,
+                        int32_t n_sinks, float sm_scale, float* out, const void* residual_keys, void* workspace,
+                        size_t workspace_bytes, void* hip_stream);
+
 /*
  * pq_score_keys -- the query-key product alone: raw scores q . k~ of every cached token
  * through the lookup table (Section 3.3, Appendix A).  This is the operation whose latency

@@ -31,6 +31,7 @@ __all__ = [
     "pq_probe_read_stream", "pq_decode_kernel_name", "pq_decode_merges_in_kernel",
     "pq_decode_attention_static", "PQ_STATIC_SCRATCH_BYTES",
     "pq_plan_pages", "pq_append_chunk", "pq_chunk_attention", "pq_chunk_workspace_bytes",
+    "pq_window_attention", "pq_window_workspace_bytes",
 ]
 
 PQ_F16, PQ_F32 = 0, 1
@@ -98,6 +99,10 @@ _SIGNATURES = {
     "pq_chunk_attention": (c_int, [_LP, c_void_p, c_int, c_int64, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p,
                                    c_int32, c_void_p, c_int64, c_void_p, c_int32, c_void_p, c_int32, c_int32, c_int32, c_float,
                                    c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "pq_window_workspace_bytes": (c_size_t, [_LP, c_int32, c_int32, c_int32, c_int32, c_int32]),
+    "pq_window_attention": (c_int, [_LP, c_void_p, c_int, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_void_p, c_int64,
+                                    c_void_p, c_int32, c_void_p, c_int32, c_int32, c_int32, c_float, c_void_p, c_void_p, c_void_p,
+                                    c_size_t, c_void_p]),
     "pq_probe_read_stream": (c_int, [c_void_p, c_size_t, c_void_p, c_void_p]),
 }
 
@@ -127,7 +132,7 @@ class _ByCtypes:
         return None
 
     decode_attention = score_keys = encode_keys = encode_values = append_keys = _decline
-    plan_pages = append_chunk = chunk_attention = _decline
+    plan_pages = append_chunk = chunk_attention = window_attention = _decline
 
 
 def _marshaller():
@@ -507,6 +512,31 @@ def pq_chunk_attention(layout: Layout, q, starts, codes_pool, params_pool, v_poo
         None if residual is None else _dev_ptr(residual, "residual", (torch.float16,)),
         _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream())
     _check(st, "pq_chunk_attention")
+
+
+def pq_window_workspace_bytes(layout: Layout, n_seqs: int, n_q_heads: int, max_seq_len: int, window: int, n_sinks: int) -> int:
+    return load_library().pq_window_workspace_bytes(ctypes.byref(layout), n_seqs, n_q_heads, max_seq_len, window, n_sinks)
+
+
+def pq_window_attention(layout: Layout, q, codes_pool, params_pool, v_pool, block_table, seq_lens, max_seq_len: int, window: int,
+                        n_sinks: int, sm_scale: float, out, workspace, residual=None, v_bits: int = 16, v_params=None) -> None:
+    """One decode step per sequence through a sliding window with sinks; see include/polarquant.h.  Arguments as in
+    pq_decode_attention; `workspace` of at least pq_window_workspace_bytes(...) bytes."""
+    if _done((_calls or _marshaller()).window_attention(
+            layout, q, codes_pool, params_pool, v_pool, block_table, seq_lens, max_seq_len, window, n_sinks, sm_scale, out, workspace,
+            residual, v_bits, v_params), "pq_window_attention"):
+        return
+    import torch
+    c = _decode_common(layout, q, codes_pool, params_pool, v_pool, block_table, seq_lens, v_bits, v_params)
+    if block_table.dim() != 2 or block_table.shape[0] != c["n_seqs"] or seq_lens.numel() != c["n_seqs"] or out.shape != q.shape:
+        raise PolarQuantError("block_table must be [n_seqs, pages], seq_lens [n_seqs], out of q's shape")
+    _check_residual(layout, residual, c["n_seqs"])
+    st = load_library().pq_window_attention(
+        ctypes.byref(layout), c["q"], c["qk"], c["n_seqs"], c["n_q"], c["codes"], c["params"], c["v"], c["vbits"], c["vpar"],
+        c["n_pool"], c["bt"], c["width"], c["lens"], max_seq_len, window, n_sinks, sm_scale, _dev_ptr(out, "out", (torch.float32,)),
+        None if residual is None else _dev_ptr(residual, "residual", (torch.float16,)),
+        _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream())
+    _check(st, "pq_window_attention")
 
 
 def pq_probe_read_stream(src, sink) -> None:

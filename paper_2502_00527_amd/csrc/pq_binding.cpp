@@ -354,6 +354,37 @@ PyObject* chunk_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// (layout, q, codes, params, v_pool, block_table, seq_lens, max_seq_len, window, n_sinks, sm_scale, out, workspace, residual, v_bits,
+//  v_params)
+PyObject* window_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 16, [&] {
+    const pq_layout layout = layout_of(a[0]), *const l = &layout;
+    const at::Tensor& q = contiguous_tensor(a[1]);
+    check_rows(q, l, false);
+    const pq_dtype kind = float_kind(q);
+    const at::Tensor &codes = contiguous_tensor(a[2]), &params = contiguous_tensor(a[3]);
+    const int64_t n_pages = key_pool_pages(l, codes, params);
+    const int32_t v_bits = integer32(integer(a[14])), n_seqs = integer32(q.size(0)), n_heads = integer32(q.size(1));
+    const ValuePool v(l, a[4], a[15], v_bits, n_pages);
+    const at::Tensor &table = contiguous_tensor(a[5], at::kInt), &lens = contiguous_tensor(a[6], at::kInt);
+    if (table.dim() != 2 || table.size(0) != n_seqs || lens.numel() != n_seqs) throw Decline{};
+    const int32_t width = integer32(table.size(1)), max_seq_len = integer32(integer(a[7])), window = integer32(integer(a[8])), n_sinks = integer32(integer(a[9]));
+    if (!PyFloat_CheckExact(a[10])) throw Decline{};
+    const float sm_scale = static_cast<float>(PyFloat_AS_DOUBLE(a[10]));
+    const at::Tensor &out = contiguous_tensor(a[11], at::kFloat), &workspace = contiguous_tensor(a[12]);
+    if (out.sizes() != q.sizes()) throw Decline{};
+    void* const residual = a[13] == Py_None ? nullptr : residual_of(a[13], l, n_seqs);
+    void *const qp = q.data_ptr(), *const cp = codes.data_ptr(), *const pp = params.data_ptr(), *const ws = workspace.data_ptr(), *const stream = current_stream();
+    float* const op = static_cast<float*>(out.data_ptr());
+    const int32_t *const tp = ints(table), *const lp = ints(lens);
+    const size_t ws_bytes = bytes_of(workspace);
+    return without_lock([&] {
+      return pq_window_attention(l, qp, kind, n_seqs, n_heads, cp, pp, v.pool, v_bits, v.params, n_pages, tp, width, lp, max_seq_len, window, n_sinks,
+                                 sm_scale, op, residual, ws, ws_bytes, stream);
+    });
+  });
+}
+
 PyObject* set_layout_type(PyObject*, PyObject* type) {
   Py_INCREF(type);
   Py_XSETREF(layout_type, type);
@@ -362,7 +393,7 @@ PyObject* set_layout_type(PyObject*, PyObject* type) {
 
 #define PQ_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {PQ_METHOD(decode_attention), PQ_METHOD(score_keys), PQ_METHOD(encode_keys), PQ_METHOD(encode_values),
-                         PQ_METHOD(append_keys), PQ_METHOD(plan_pages), PQ_METHOD(append_chunk), PQ_METHOD(chunk_attention),
+                         PQ_METHOD(append_keys), PQ_METHOD(plan_pages), PQ_METHOD(append_chunk), PQ_METHOD(chunk_attention), PQ_METHOD(window_attention),
                          {"set_layout_type", set_layout_type, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Argument marshalling for libpolarquant.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -22,16 +22,19 @@ namespace {
 constexpr int kMergeThreads = 256;
 constexpr int kMergeSlices = kMergeThreads / 32;
 
+// kWindow: the lengths are what a sliding window leaves of them.
+template <bool kWindow>
 __global__ __launch_bounds__(kMergeThreads) void pq_decode_merge_kernel(
     const float* __restrict__ ws_acc, const float* __restrict__ ws_ml,
     const int32_t* __restrict__ seq_lens, float* __restrict__ out, int32_t n_q_heads,
-    int32_t max_seq_len, int32_t pages_per_chunk, int32_t n_chunks, int32_t n_big, int32_t pages_small) {
+    int32_t max_seq_len, int32_t pages_per_chunk, int32_t n_chunks, int32_t n_big, int32_t pages_small, int32_t window, int32_t n_sinks) {
   __shared__ float4 part_o[kMergeSlices][32];
   __shared__ float part_l[kMergeSlices];
   __shared__ float wave_max[kMergeThreads / 64];
   const int head = blockIdx.x, seq = blockIdx.y, tid = threadIdx.x;
   const int slice = tid >> 5, quad = tid & 31;
-  const int L = min(seq_lens[seq], max_seq_len);
+  int L = min(seq_lens[seq], max_seq_len);
+  if constexpr (kWindow) L = WindowView(L, window, n_sinks).len;
   const int64_t oh = static_cast<int64_t>(seq) * n_q_heads + head;
   if (L <= 0) {
     if (tid < kHeadDim) out[oh * kHeadDim + tid] = 0.f;
@@ -287,14 +290,12 @@ int launch_scores(const pq_layout* layout, DecodeArgs a, hipStream_t stream) {
   return e == hipSuccess ? PQ_OK : record_hip_error(e);
 }
 
-// Everything the decode entry points have in common: argument checks, kernel arguments, and the
-// launches.  `out` null = only the first stage of the two-stage (grid) path, the chunk partials.
-int decode_launch(const pq_layout* layout, const void* q, pq_dtype q_dtype, int32_t n_seqs, int32_t n_q_heads,
-                  const void* codes_pool, const void* params_pool, const void* v_pool, int32_t v_bits,
-                  const void* v_params_pool, int64_t n_pool_pages, const int32_t* block_table,
-                  int32_t max_pages_per_seq, const int32_t* seq_lens, int32_t max_seq_len, float sm_scale,
-                  float* out, float* scores, int64_t scores_stride, const void* residual_keys,
-                  void* workspace, size_t workspace_bytes, void* hip_stream) {
+// Checks of the arguments that attention over the whole cache and through a window have in common.
+int check_attention(const pq_layout* layout, const void* q, pq_dtype q_dtype, int32_t n_seqs, int32_t n_q_heads,
+                    const void* codes_pool, const void* params_pool, const void* v_pool, int32_t v_bits,
+                    const void* v_params_pool, int64_t n_pool_pages, const int32_t* block_table,
+                    int32_t max_pages_per_seq, const int32_t* seq_lens, int32_t max_seq_len, float sm_scale,
+                    const void* residual_keys) {
   const int st = check_decode_shape(layout, n_seqs, n_q_heads, max_seq_len);
   if (st != PQ_OK) return st;
   if (!q || !codes_pool || !params_pool || !v_pool || !block_table || !seq_lens) return PQ_ERR_INVALID_ARG;
@@ -302,7 +303,6 @@ int decode_launch(const pq_layout* layout, const void* q, pq_dtype q_dtype, int3
   if (n_pool_pages <= 0 || max_pages_per_seq <= 0) return PQ_ERR_INVALID_ARG;
   const int64_t need_pages = (static_cast<int64_t>(max_seq_len) + kGroup - 1) / kGroup;
   if (need_pages > max_pages_per_seq) return PQ_ERR_INVALID_ARG;
-  if (scores && scores_stride < max_seq_len) return PQ_ERR_INVALID_ARG;
   if (!isfinite(sm_scale)) return PQ_ERR_INVALID_ARG;
   if (v_bits != 16 && v_bits != 4 && v_bits != 2) return PQ_ERR_UNSUPPORTED;
   if (v_bits != 16 && !v_params_pool) return PQ_ERR_INVALID_ARG;
@@ -313,14 +313,14 @@ int decode_launch(const pq_layout* layout, const void* q, pq_dtype q_dtype, int3
   if ((reinterpret_cast<uintptr_t>(v_params_pool) | reinterpret_cast<uintptr_t>(block_table) |
        reinterpret_cast<uintptr_t>(seq_lens)) & 3u)
     return PQ_ERR_INVALID_ARG;
-  const int rt = layout->r_bits * 10 + layout->t_bits;
-  const bool grouped = layout->angle_quantizer == PQ_ANGLE_GROUPED;
+  return PQ_OK;
+}
 
-  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return PQ_ERR_WORKSPACE;
-  const Workspace ws = carve_workspace(workspace, layout, n_seqs, n_q_heads, max_seq_len);
-  if (workspace_bytes < ws.bytes) return PQ_ERR_WORKSPACE;
-  const ChunkPlan plan = plan_attention(layout, out != nullptr ? v_bits : 16, n_seqs, n_q_heads, max_seq_len);
-
+// What their kernels are given alike.
+DecodeArgs attention_args(const pq_layout* layout, const void* q, pq_dtype q_dtype, int32_t n_seqs, int32_t n_q_heads,
+                          const void* codes_pool, const void* params_pool, const void* v_pool, const void* v_params_pool,
+                          int64_t n_pool_pages, const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* seq_lens,
+                          int32_t max_seq_len, float sm_scale, float* out, const void* residual_keys, const Workspace& ws, const ChunkPlan& plan) {
   DecodeArgs a = {};
   a.q = q;
   a.codes = static_cast<const uint8_t*>(codes_pool);
@@ -331,12 +331,10 @@ int decode_launch(const pq_layout* layout, const void* q, pq_dtype q_dtype, int3
   a.block_table = block_table;
   a.seq_lens = seq_lens;
   a.n_seqs = n_seqs;
-  a.scores = scores;
   a.ws_acc = ws.acc;
   a.ws_ml = ws.ml;
   a.out = out;
   a.arrivals = ws.arrivals;
-  a.scores_stride = scores_stride;
   a.n_pool_pages = n_pool_pages;
   a.n_kv_heads = layout->n_kv_heads;
   a.n_q_heads = n_q_heads;
@@ -349,10 +347,38 @@ int decode_launch(const pq_layout* layout, const void* q, pq_dtype q_dtype, int3
   a.q_is_f32 = q_dtype == PQ_F32 ? 1 : 0;
   a.scale_log2 = static_cast<float>(static_cast<double>(sm_scale) * 1.4426950408889634074);
   fill_angle_tables(a, layout->t_bits);
+  a.group_total = n_q_heads / layout->n_kv_heads;
+  a.table_index = key_table_index(layout);
+  return a;
+}
+
+// The decode entry points but for the window's: argument checks, kernel arguments, and the
+// launches.  `out` null = only the first stage of the two-stage (grid) path, the chunk partials.
+int decode_launch(const pq_layout* layout, const void* q, pq_dtype q_dtype, int32_t n_seqs, int32_t n_q_heads,
+                  const void* codes_pool, const void* params_pool, const void* v_pool, int32_t v_bits,
+                  const void* v_params_pool, int64_t n_pool_pages, const int32_t* block_table,
+                  int32_t max_pages_per_seq, const int32_t* seq_lens, int32_t max_seq_len, float sm_scale,
+                  float* out, float* scores, int64_t scores_stride, const void* residual_keys,
+                  void* workspace, size_t workspace_bytes, void* hip_stream) {
+  const int st = check_attention(layout, q, q_dtype, n_seqs, n_q_heads, codes_pool, params_pool, v_pool, v_bits, v_params_pool, n_pool_pages, block_table,
+                                 max_pages_per_seq, seq_lens, max_seq_len, sm_scale, residual_keys);
+  if (st != PQ_OK) return st;
+  if (scores && scores_stride < max_seq_len) return PQ_ERR_INVALID_ARG;
+  const int rt = layout->r_bits * 10 + layout->t_bits;
+  const bool grouped = layout->angle_quantizer == PQ_ANGLE_GROUPED;
+
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return PQ_ERR_WORKSPACE;
+  const Workspace ws = carve_workspace(workspace, layout, n_seqs, n_q_heads, max_seq_len);
+  if (workspace_bytes < ws.bytes) return PQ_ERR_WORKSPACE;
+  const ChunkPlan plan = plan_attention(layout, out != nullptr ? v_bits : 16, n_seqs, n_q_heads, max_seq_len);
+
+  DecodeArgs a = attention_args(layout, q, q_dtype, n_seqs, n_q_heads, codes_pool, params_pool, v_pool, v_params_pool, n_pool_pages, block_table,
+                                max_pages_per_seq, seq_lens, max_seq_len, sm_scale, out, residual_keys, ws, plan);
+  a.scores = scores;
+  a.scores_stride = scores_stride;
 
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  const int group_total = n_q_heads / layout->n_kv_heads;
-  a.group_total = group_total;
+  const int group_total = a.group_total;
   const bool roles = choose_attention_kernel(layout, v_bits, n_seqs, n_q_heads, max_seq_len) == AttentionKernel::kRoles;
   const DeviceCut cut = out != nullptr ? device_cut(layout, plan, v_bits, n_seqs, n_q_heads, max_seq_len) : DeviceCut{0, 0, 0};
   const bool merged = out != nullptr && merges_in_kernel(layout, plan, cut, n_seqs, n_q_heads, max_seq_len);
@@ -362,7 +388,6 @@ int decode_launch(const pq_layout* layout, const void* q, pq_dtype q_dtype, int3
   a.fit_chunks = cut.fit_chunks;
   const dim3 grid = a.cut_places > 0 ? dim3(layout->n_kv_heads, a.cut_places) : dim3(layout->n_kv_heads, n_seqs, plan.n_chunks);
   a.wide_groups = out != nullptr && wide_groups(layout, plan, n_seqs, max_seq_len) ? 1 : 0;
-  a.table_index = key_table_index(layout);
   // A pass over the cache serves up to 8 query heads of a KV head (with the grouped quantizer on the vector unit, whose kernel
   // stores its scores itself, all one or two).
   const bool vector = grouped && !grouped_on_matrix(layout, group_total);
@@ -385,9 +410,9 @@ int decode_launch(const pq_layout* layout, const void* q, pq_dtype q_dtype, int3
   }
   if (e != hipSuccess) return record_hip_error(e);
   if (out != nullptr && !merged) {
-    hipLaunchKernelGGL(pq_decode_merge_kernel, dim3(n_q_heads, n_seqs), dim3(kMergeThreads), 0, stream, ws.acc,
+    hipLaunchKernelGGL(pq_decode_merge_kernel<false>, dim3(n_q_heads, n_seqs), dim3(kMergeThreads), 0, stream, ws.acc,
                        ws.ml, seq_lens, out, n_q_heads, max_seq_len, plan.pages_per_chunk, plan.n_chunks, plan.n_big,
-                       plan.pages_small);
+                       plan.pages_small, 0, 0);
     e = hipGetLastError();
     if (e != hipSuccess) return record_hip_error(e);
   }
@@ -435,10 +460,10 @@ extern "C" int pq_decode_merge(const pq_layout* layout, int32_t n_seqs, int32_t 
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return PQ_ERR_WORKSPACE;
   const Workspace ws = carve_workspace(const_cast<void*>(workspace), layout, n_seqs, n_q_heads, max_seq_len);
   if (workspace_bytes < ws.bytes) return PQ_ERR_WORKSPACE;
-  hipLaunchKernelGGL(pq_decode_merge_kernel, dim3(n_q_heads, n_seqs), dim3(kMergeThreads), 0,
+  hipLaunchKernelGGL(pq_decode_merge_kernel<false>, dim3(n_q_heads, n_seqs), dim3(kMergeThreads), 0,
                      static_cast<hipStream_t>(hip_stream), ws.acc, ws.ml, seq_lens, out, n_q_heads,
                      max_seq_len, plan.pages_per_chunk, plan.n_chunks, plan.n_big,
-                       plan.pages_small);
+                       plan.pages_small, 0, 0);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return record_hip_error(e);
   return PQ_OK;
@@ -475,6 +500,78 @@ extern "C" int pq_decode_attention_static(const pq_layout* layout, const void* q
   return pq_decode_attention(layout, q, q_dtype, n_seqs, n_q_heads, codes_pool, params_pool, v_pool, v_bits,
                              v_params_pool, n_pool_pages, block_table, max_pages_per_seq, seq_lens, max_seq_len,
                              sm_scale, out, scores, scores_stride, residual_keys, ws, need, hip_stream);
+}
+
+namespace pq {
+namespace {
+
+// The window's workspace: one partial a chunk and query head, and the units' arrival words.
+Workspace carve_window_workspace(void* base, const pq_layout* l, int32_t n_seqs, int32_t n_q_heads, const ChunkPlan& plan) {
+  const size_t slots = static_cast<size_t>(n_seqs) * n_q_heads * plan.n_chunks;
+  const size_t acc_bytes = round256(slots * kHeadDim * sizeof(float)), ml_bytes = round256(slots * 2 * sizeof(float));
+  Workspace w;
+  w.acc = static_cast<float*>(base);
+  w.ml = reinterpret_cast<float*>(static_cast<uint8_t*>(base) + acc_bytes);
+  w.arrivals = reinterpret_cast<uint64_t*>(static_cast<uint8_t*>(base) + acc_bytes + ml_bytes);
+  w.bytes = acc_bytes + ml_bytes + round256(static_cast<size_t>(n_seqs) * l->n_kv_heads * sizeof(uint64_t));
+  return w;
+}
+
+int check_window(const pq_layout* l, int32_t n_seqs, int32_t n_q_heads, int32_t max_seq_len, int32_t window, int32_t n_sinks) {
+  const int st = check_decode_shape(l, n_seqs, n_q_heads, max_seq_len);
+  if (st != PQ_OK) return st;
+  if (window <= 0 || n_sinks < 0) return PQ_ERR_INVALID_ARG;
+  return plan_window(l, n_seqs, window_bound(max_seq_len, window, n_sinks)).n_chunks > 65535 ? PQ_ERR_UNSUPPORTED : PQ_OK;   // grid.z
+}
+
+}  // namespace
+}  // namespace pq
+
+extern "C" size_t pq_window_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_t n_q_heads, int32_t max_seq_len,
+                                            int32_t window, int32_t n_sinks) {
+  if (check_window(layout, n_seqs, n_q_heads, max_seq_len, window, n_sinks) != PQ_OK) return 0;
+  return carve_window_workspace(nullptr, layout, n_seqs, n_q_heads, plan_window(layout, n_seqs, window_bound(max_seq_len, window, n_sinks))).bytes;
+}
+
+extern "C" int pq_window_attention(const pq_layout* layout, const void* q, pq_dtype q_dtype, int32_t n_seqs, int32_t n_q_heads,
+                                   const void* codes_pool, const void* params_pool, const void* v_pool, int32_t v_bits,
+                                   const void* v_params_pool, int64_t n_pool_pages, const int32_t* block_table,
+                                   int32_t max_pages_per_seq, const int32_t* seq_lens, int32_t max_seq_len, int32_t window,
+                                   int32_t n_sinks, float sm_scale, float* out, const void* residual_keys, void* workspace,
+                                   size_t workspace_bytes, void* hip_stream) {
+  if (!out || (reinterpret_cast<uintptr_t>(out) & 15u)) return PQ_ERR_INVALID_ARG;
+  int st = check_attention(layout, q, q_dtype, n_seqs, n_q_heads, codes_pool, params_pool, v_pool, v_bits, v_params_pool, n_pool_pages, block_table,
+                           max_pages_per_seq, seq_lens, max_seq_len, sm_scale, residual_keys);
+  if (st == PQ_OK) st = check_window(layout, n_seqs, n_q_heads, max_seq_len, window, n_sinks);
+  if (st != PQ_OK) return st;
+  const int32_t bound = window_bound(max_seq_len, window, n_sinks);
+  const ChunkPlan plan = plan_window(layout, n_seqs, bound);
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return PQ_ERR_WORKSPACE;
+  const Workspace ws = carve_window_workspace(workspace, layout, n_seqs, n_q_heads, plan);
+  if (workspace_bytes < ws.bytes) return PQ_ERR_WORKSPACE;
+  DecodeArgs a = attention_args(layout, q, q_dtype, n_seqs, n_q_heads, codes_pool, params_pool, v_pool, v_params_pool, n_pool_pages, block_table,
+                                max_pages_per_seq, seq_lens, max_seq_len, sm_scale, out, residual_keys, ws, plan);
+  a.window = std::min(window, max_seq_len);
+  a.n_sinks = std::min(n_sinks, max_seq_len);
+  const bool merged = window_merges_in_kernel(layout, plan, n_seqs);
+  a.merge_in_kernel = merged ? 1 : 0;
+  a.wide_groups = wide_groups(layout, plan, n_seqs, bound) ? 1 : 0;
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  const dim3 grid(layout->n_kv_heads, n_seqs, plan.n_chunks);
+  hipError_t e = hipSuccess;
+  for (a.head0 = 0; a.head0 < a.group_total && e == hipSuccess; a.head0 += a.n_heads) {
+    a.n_heads = std::min(a.group_total - a.head0, kMaxHeads);
+    if (v_bits == 16) launch_window_v16(layout, a, grid, stream);
+    else if (v_bits == 4) launch_window_v4(layout, a, grid, stream);
+    else launch_window_v2(layout, a, grid, stream);
+    e = hipGetLastError();
+  }
+  if (e == hipSuccess && !merged) {
+    hipLaunchKernelGGL(pq_decode_merge_kernel<true>, dim3(n_q_heads, n_seqs), dim3(kMergeThreads), 0, stream, ws.acc, ws.ml, seq_lens, out, n_q_heads,
+                       max_seq_len, plan.pages_per_chunk, plan.n_chunks, plan.n_big, plan.pages_small, a.window, a.n_sinks);
+    e = hipGetLastError();
+  }
+  return e == hipSuccess ? PQ_OK : record_hip_error(e);
 }
 
 extern "C" int pq_score_keys(const pq_layout* layout, const void* q, pq_dtype q_dtype, int32_t n_seqs,

@@ -91,6 +91,8 @@ struct DecodeArgs {
   float scale_log2;         // sm_scale * log2(e)
   float cos_tab[kMaxAngleBins];
   float sin_tab[kMaxAngleBins];
+  int32_t window;           // pq_window_attention: tokens of the window, and the sinks
+  int32_t n_sinks;
 };
 
 // Launcher of the grouped quantizer's vector-unit attention kernels (rt = 10 r + t; pq_decode_partials_ga.hip).
@@ -99,6 +101,23 @@ struct DecodeArgs {
 bool launch_attention_partials_ga(int rt, int G, int v_bits, const DecodeArgs& a, dim3 grid, hipStream_t st);
 
 namespace {
+
+// What a sliding window leaves of a sequence of L tokens: the first n_sinks and the last `window`.  Whole pages between them do not exist for a
+// launch: it sees a sequence of `len` tokens whose pages from `sink_pages` on are `skip` further on in the block table.  On the
+// pages at the edges the tokens [from, to) of the sequence are masked.
+struct WindowView {
+  int len, sink_pages, skip, from, to;
+  WindowView() = default;
+  __device__ __forceinline__ WindowView(int L, int window, int n_sinks) {
+    L = max(L, 0);
+    from = n_sinks;
+    to = max(n_sinks, L - window);
+    sink_pages = (n_sinks + kGroup - 1) / kGroup;
+    skip = max(0, to / kGroup - sink_pages);
+    len = L - skip * kGroup;
+  }
+  __device__ __forceinline__ int page(int v) const { return v + (v >= sink_pages ? skip : 0); }
+};
 
 // Chunks a sequence of n_pages pages has, when the first n_big are `big` pages long and the others `small`.
 __device__ __forceinline__ int chunks_of_pages(int n_pages, int big, int n_big, int small) {

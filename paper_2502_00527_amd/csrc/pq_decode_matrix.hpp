@@ -59,6 +59,10 @@ bool launch_attention_grouped_v16(int rt, const DecodeArgs& a, dim3 grid, hipStr
 bool launch_attention_grouped_v4(int rt, const DecodeArgs& a, dim3 grid, hipStream_t st);
 bool launch_attention_grouped_v2(int rt, const DecodeArgs& a, dim3 grid, hipStream_t st);
 bool launch_scores_grouped(int rt, const DecodeArgs& a, dim3 grid, hipStream_t st);
+// Through a sliding window, of either quantizer (pq_decode_window.hip, one per value width).
+bool launch_window_v16(const pq_layout* l, const DecodeArgs& a, dim3 grid, hipStream_t st);
+bool launch_window_v4(const pq_layout* l, const DecodeArgs& a, dim3 grid, hipStream_t st);
+bool launch_window_v2(const pq_layout* l, const DecodeArgs& a, dim3 grid, hipStream_t st);
 
 namespace {
 
@@ -866,14 +870,32 @@ struct GroupedWalk {
 // one through the scalar cache, a page ahead of their use.  Entries of the table row are read
 // without knowing the sequence's length; `get` masks the pages past the wavefront's last one, and
 // block-table entries outside the pool.
-template <int NW>
+template <int NW, bool kWindow = false>
 struct PageIds {
   const PQ_CONST int32_t* table;   // block-table row of the sequence, at the wavefront's first page
+  // (kWindow: at its first page; the wavefront's first page, and where pages are left out)
+  int first, skip_from, skip;
   int64_t n_pool_pages;
   int n_row;                       // entries of the row that belong to the wavefront from there on
   int n_p;                         // pages of the wavefront in this chunk
   int ahead;                       // entry of the page that get() is asked for next
-  __device__ __forceinline__ void fetch(int k) { ahead = k < n_row ? table[NW * k] : -1; }
+  __device__ __forceinline__ void fetch(int k) {
+    if constexpr (kWindow) {
+      const int v = first + NW * k, page = v + (v >= skip_from ? skip : 0);
+      ahead = page < n_row ? table[page] : -1;
+    } else {
+      ahead = k < n_row ? table[NW * k] : -1;
+    }
+  }
+  __device__ __forceinline__ void start(const DecodeArgs& a, int seq, int first_page, const WindowView& view) {
+    table = reinterpret_cast<const PQ_CONST int32_t*>(reinterpret_cast<uintptr_t>(a.block_table + static_cast<int64_t>(seq) * a.max_pages_per_seq));
+    n_pool_pages = a.n_pool_pages;
+    n_row = a.max_pages_per_seq;
+    first = first_page;
+    skip_from = uni(view.sink_pages);
+    skip = uni(view.skip);
+    fetch(0);
+  }
   __device__ __forceinline__ void start(const DecodeArgs& a, int seq, int first_page) {
     table = reinterpret_cast<const PQ_CONST int32_t*>(
         reinterpret_cast<uintptr_t>(a.block_table + static_cast<int64_t>(seq) * a.max_pages_per_seq + first_page));
@@ -1019,14 +1041,15 @@ __device__ __forceinline__ void grouped_scores_body(const DecodeArgs& a) {
 // ---- attention ----------------------------------------------------------------------------------
 // kCut: the chunks are cut on the device (a.cut_places > 0).  kMatWaves: wavefronts of the work-group, 4 or 8.
 // kGroupedRadius: 0 on the uniform grid; with the grouped angle quantizer the radius bits (queries of either type are
-// taken as fp32 there, so that Q32 is true).
-template <int W, int VB, int NH, bool Q32, bool kCut, int kMatWaves, int kGroupedRadius = 0>
+// taken as fp32 there, so that Q32 is true).  kWindow: through a sliding window with sinks (WindowView; the launch is cut on the host).
+template <int W, int VB, int NH, bool Q32, bool kCut, int kMatWaves, int kGroupedRadius = 0, bool kWindow = false>
 __device__ __forceinline__ void attention_body(const DecodeArgs& a) {
   constexpr int UB = 2 * W;
   constexpr int kMatThreads = kMatWaves * 64;
   constexpr bool kQuantV = VB != 16;
   constexpr bool kGrouped = kGroupedRadius != 0;
   static_assert(!kGrouped || (Q32 && kMatWaves == 4), "what the grouped quantizer's kernels are");
+  static_assert(!kWindow || !kCut, "the cut on the device goes by the whole lengths");
   constexpr TokenOrder kOrder = token_order(VB);
   constexpr int kChain = kQuantV ? 16 : 4;
   constexpr uint32_t kCodesBytes = kBlocks * kGroup * UB;
@@ -1110,9 +1133,16 @@ __device__ __forceinline__ void attention_body(const DecodeArgs& a) {
   QueryFetch qf;
   if constexpr (kGrouped) qf = a.q_is_f32 ? fetch_query_heads<true>(a, q_at, tid) : fetch_query_heads<false>(a, q_at, tid).widened();
   else qf = fetch_query_heads<Q32>(a, q_at, tid);
-  PageIds<kMatWaves> pids;
-  pids.start(a, seq, page0 + wave);
-  L = uni(clamped_len(a, seq));
+  PageIds<kMatWaves, kWindow> pids;
+  WindowView view;
+  if constexpr (kWindow) {
+    view = WindowView(clamped_len(a, seq), a.window, a.n_sinks);
+    pids.start(a, seq, page0 + wave, view);
+    L = uni(view.len);
+  } else {
+    pids.start(a, seq, page0 + wave);
+    L = uni(clamped_len(a, seq));
+  }
   n_pages = pages_of_len(L);
   if (cut_later) {
     npg = min(kMatWaves, n_pages);                                     // at least
@@ -1280,6 +1310,21 @@ __device__ __forceinline__ void attention_body(const DecodeArgs& a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           if (((batch_token<kOrder>(t, rot_cur) + row_token<kOrder>(4 * row + i)) ^ other) >= nv) w.s[t][i] = kNegInf;
+    }
+    if constexpr (kWindow) {
+      const int page = uni(view.page(pi)), from = view.from - page * kGroup, to = view.to - page * kGroup;
+      if (to > 0 && from < kGroup) {
+        const int row = lane_now() >> 4, other = NH == 4 && (lane_now() & 4) ? 64 : 0;
+        int first = uni(from), last = uni(to);
+        asm volatile("" : "+s"(first), "+s"(last));
+#pragma unroll
+        for (int t = 0; t < kOwn; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int token = (batch_token<kOrder>(t, rot_cur) + row_token<kOrder>(4 * row + i)) ^ other;
+            if (token >= first && token < last) w.s[t][i] = kNegInf;
+          }
+      }
     }
     float pm = max2(w.s[0][0], w.s[0][1]);
     pm = max3(pm, w.s[0][2], w.s[0][3]);

@@ -213,6 +213,27 @@ inline bool merges_in_kernel(const pq_layout* l, const ChunkPlan& host, const De
   return cut.places > 0 || host.n_chunks == 1 || (host.n_chunks <= kMergeFan && large_launch(l, n_seqs, max_seq_len));
 }
 
+// Attention through a sliding window.  The longest sequence that a launch can see: the sinks' pages, and the window's, which may
+// begin inside a page.
+inline int32_t window_bound(int32_t max_seq_len, int32_t window, int32_t n_sinks) {
+  const int64_t pages = (static_cast<int64_t>(n_sinks) + kGroup - 1) / kGroup + (static_cast<int64_t>(window) + kGroup - 1) / kGroup + 1;
+  return static_cast<int32_t>(std::min<int64_t>(max_seq_len, pages * kGroup));
+}
+// Its chunks: most sequences are as long as the window lets them be, so that they are alike, and as many as start at once.
+inline ChunkPlan plan_window(const pq_layout* l, int32_t n_seqs, int32_t bound) {
+  const int64_t pages = (static_cast<int64_t>(bound) + kGroup - 1) / kGroup, units = static_cast<int64_t>(n_seqs) * l->n_kv_heads;
+  const int64_t most = std::max<int64_t>(1, kResidentGroups / units);
+  int64_t length = std::max<int64_t>((pages + most - 1) / most, std::min<int64_t>(pages, kWaveRound));
+  if (pages < 2 * kWaveRound) length = pages;                                  // less than two pages a wavefront: nothing to merge
+  ChunkPlan p;
+  p.pages_per_chunk = p.pages_small = static_cast<int32_t>(length);
+  p.n_chunks = p.n_big = static_cast<int32_t>((pages + length - 1) / length);
+  return p;
+}
+inline bool window_merges_in_kernel(const pq_layout* l, const ChunkPlan& plan, int32_t n_seqs) {
+  return plan.n_chunks == 1 || (plan.n_chunks <= kMergeFan && static_cast<int64_t>(n_seqs) * l->n_kv_heads * plan.n_chunks >= kComputeUnits);
+}
+
 // Work-groups of 8 wavefronts: sequences of one chunk with more pages than 4 wavefronts take at once, and no more
 // units than compute units (two work-groups of 4 share one otherwise).  One sequence of 777 tokens 13.3 -> 12.2 us
 // (11.5 now, with a shorter end of the chunk), 16 of them 15.0 -> 14.7; up to 4 pages the wider work-group costs 1 us (300 tokens: 9.7 -> 10.7).  From 8 pages on
