@@ -55,7 +55,7 @@ size_t round256(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
 ChunkLaunch plan_launch(const pq_layout* l, int32_t n_seqs, int32_t n_q_heads, int64_t n_tokens, int64_t max_pages) {
   ChunkLaunch p;
   const int64_t group = n_q_heads / l->n_kv_heads;
-  p.rows_of_16 = n_tokens * group <= 24 * static_cast<int64_t>(n_seqs) ? 1 : 4;
+  p.rows_of_16 = n_tokens * group <= 24 * static_cast<int64_t>(n_seqs) ? 1 : chunk::kTileRows / 16;
   p.tile_tokens = static_cast<int>(16 * p.rows_of_16 / group);
   p.n_items = std::min<int64_t>(n_tokens, n_tokens / p.tile_tokens + n_seqs);
   const int64_t units = std::max<int64_t>(1, p.n_items * l->n_kv_heads), resident = p.rows_of_16 == 1 ? 2 * kComputeUnits : kComputeUnits;

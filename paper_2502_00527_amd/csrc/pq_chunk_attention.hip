@@ -14,6 +14,31 @@ namespace {
 namespace chunk {
 
 #define PQ_CHUNK_ATTR(rt) __launch_bounds__(kChunkWaves * 64) __attribute__((amdgpu_waves_per_eu(rt == 1 ? 2 : 1, rt == 1 ? 2 : 1)))
+#define PQ_SHARED_ATTR __launch_bounds__(kSharedWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
+
+template <int RB, int TB, int VB, bool kGrouped>
+__global__ PQ_SHARED_ATTR void pq_chunk_shared_kernel(const ChunkAttentionArgs a) {
+  shared_body<std::conditional_t<kGrouped, SharedGroupedKeys<RB, TB>, SharedUniformKeys<RB, TB>>, RB, VB>(a);
+}
+template <int RB, int TB, int VB>
+bool launch_shared(bool grouped, const ChunkAttentionArgs& a, dim3 grid, hipStream_t st) {
+  if (grouped) hipLaunchKernelGGL((pq_chunk_shared_kernel<RB, TB, VB, true>), grid, dim3(kSharedWaves * 64), 0, st, a);
+  else hipLaunchKernelGGL((pq_chunk_shared_kernel<RB, TB, VB, false>), grid, dim3(kSharedWaves * 64), 0, st, a);
+  return true;
+}
+template <int VB>
+bool launch_shared(const pq_layout* l, const ChunkAttentionArgs& a, dim3 grid, hipStream_t st) {
+  const bool grouped = l->angle_quantizer == PQ_ANGLE_GROUPED;
+  switch (l->r_bits * 10 + l->t_bits) {
+    case 44: return launch_shared<4, 4, VB>(grouped, a, grid, st);
+    case 33: return launch_shared<3, 3, VB>(grouped, a, grid, st);
+    case 53: return launch_shared<5, 3, VB>(grouped, a, grid, st);
+    case 35: return launch_shared<3, 5, VB>(grouped, a, grid, st);
+    case 42: return launch_shared<4, 2, VB>(grouped, a, grid, st);
+    case 24: return launch_shared<2, 4, VB>(grouped, a, grid, st);
+    default: return false;
+  }
+}
 
 template <int W, int VB, int RT>
 __global__ PQ_CHUNK_ATTR(RT) void pq_chunk_attention_kernel(const ChunkAttentionArgs a) { attention_body<UniformKeys<W>, W, false, VB, RT>(a); }
@@ -40,7 +65,7 @@ bool launch(const pq_layout* l, const ChunkAttentionArgs& a, dim3 grid, hipStrea
 }  // namespace
 
 bool PQ_CHUNK_LAUNCH(const pq_layout* l, int rows_of_16, const ChunkAttentionArgs& a, dim3 grid, hipStream_t st) {
-  return rows_of_16 == 1 ? chunk::launch<PQ_CHUNK_VB, 1>(l, a, grid, st) : chunk::launch<PQ_CHUNK_VB, 4>(l, a, grid, st);
+  return rows_of_16 == 1 ? chunk::launch<PQ_CHUNK_VB, 1>(l, a, grid, st) : chunk::launch_shared<PQ_CHUNK_VB>(l, a, grid, st);
 }
 
 }  // namespace pq

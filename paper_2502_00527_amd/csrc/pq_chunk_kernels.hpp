@@ -542,6 +542,421 @@ __device__ __forceinline__ void attention_body(const ChunkAttentionArgs& a) {
   }
 }
 
+// ---- many rows: operands shared through LDS -------------------------------------------------------------------
+// A work-group of 8 wavefronts serves up to 256 rows of one KV head.  Each page is unpacked once: wavefront w makes the key operands of
+// tile w (16 tokens) and half of the value operands of step w / 2 (32 tokens) and stores them as the matrix instructions
+// read them, 16 bytes a lane, while everybody computes with the page before; one barrier a page.  A wavefront has 32 rows,
+// or, where the work-group has fewer, shares them with others that take other tokens of the page.
+constexpr int kSharedWaves = 8;
+constexpr int kSharedRows = 32;                    // of a wavefront
+constexpr int kSharedRT = kSharedRows / 16;
+constexpr int kTileRows = kSharedWaves * kSharedRows;
+constexpr int kImage = kGroup * kHeadDim * 2;      // bytes of a page's key or value operands
+
+// Key coordinates in fp32, rounded once.  trig: (cos, sin) of the angle levels.
+template <int RB, int TB>
+struct SharedUniformKeys {
+  static constexpr int W = RB + TB, NA = 1 << TB;
+  static constexpr int kLdsBytes = NA * 256;       // 32 copies of an entry: no bank conflicts
+  static constexpr bool kGrouped = false;
+  uint32_t table, lane_at;
+  __device__ __forceinline__ void init(const uint8_t* lds, const ChunkAttentionArgs&, int tid) {
+    table = lds_addr(lds);
+    lane_at = (tid & 31) * 8;
+    for (int i = tid; i < NA * 32; i += kSharedWaves * 64) {
+      const float turns = (static_cast<float>(i >> 5) + 0.5f) * (1.f / NA) - 0.5f;
+      *(PQ_LDS f32x2*)static_cast<uintptr_t>(table + i * 8) = f32x2{cosf(turns * 6.283185307179586f), sinf(turns * 6.283185307179586f)};
+    }
+  }
+  __device__ __forceinline__ void build(uint32_t, int, int) {}
+  template <int K>
+  __device__ __forceinline__ f32x2 trig(uint32_t angle, int) const {
+    return *(const PQ_LDS f32x2*)static_cast<uintptr_t>(table + lane_at + angle * 256);
+  }
+};
+// Grouped quantizer: the page's levels, as fp16, made by the work-group for the page after the next (two tables).
+template <int RB, int TB>
+struct SharedGroupedKeys {
+  static constexpr int W = RB + TB, NA = 1 << TB;
+  static constexpr int kPageBytes = kPairs * NA * 4;
+  static constexpr int kLdsBytes = 2 * kPageBytes;
+  static constexpr bool kGrouped = true;
+  uint32_t table, row;
+  __device__ __forceinline__ void init(const uint8_t* lds, const ChunkAttentionArgs&, int tid) {
+    table = lds_addr(lds);
+    row = table + ((tid & 63) >> 4) * (16 * NA * 4);
+  }
+  // angle: {fp16 s, fp16 z} of pair `lane`
+  __device__ __forceinline__ void build(uint32_t angle, int parity, int tid) {
+    const int lane = tid & 63, wave = tid >> 6;
+    const float level = static_cast<float>(lane & (NA - 1)) + 0.5f;
+    constexpr int kPairsAtOnce = 64 >> TB;
+    for (int it = wave; it < NA; it += kSharedWaves) {
+      const f16x2 sz = u2h(static_cast<uint32_t>(__shfl(static_cast<int>(angle), it * kPairsAtOnce + (lane >> TB))));
+      const float turns = fmaf(level, static_cast<float>(sz.x), static_cast<float>(sz.y)) * 0.15915494309189535f;
+      *(PQ_LDS uint32_t*)static_cast<uintptr_t>(table + parity * kPageBytes + it * 256 + lane * 4) = h2u(to_half2(__builtin_amdgcn_cosf(turns), __builtin_amdgcn_sinf(turns)));
+    }
+  }
+  template <int K>
+  __device__ __forceinline__ f32x2 trig(uint32_t angle, int parity) const {
+    const f16x2 t = u2h(*(const PQ_LDS uint32_t*)static_cast<uintptr_t>(row + parity * kPageBytes + K * (NA * 4) + angle * 4));
+    return f32x2{static_cast<float>(t.x), static_cast<float>(t.y)};
+  }
+};
+
+// One page on its way from memory to the operands in LDS: a wavefront's part of it.
+template <typename Keys, int RB, int VB>
+struct PageProducer {
+  static constexpr int W = Keys::W;
+  static constexpr uint32_t kCodesBytes = kBlocks * kGroup * 2 * W;
+  static constexpr uint32_t kParamWords = kPairs * (Keys::kGrouped ? 2 : 1);
+  Unit<W / 2> unit;
+  uint32_t params[16], angle;
+  u32x2 rows[VB == 16 ? 8 : 1];
+  Values<VB == 16 ? 4 : VB> quantized;
+  u32x2 tail[8];                                    // un-quantized keys, x and y of four pairs, four times
+  bool is_tail;
+
+  // id < 0: masked, zeros everywhere
+  __device__ __forceinline__ void load(const ChunkAttentionArgs& a, int kvh, int id, int page, int tail_page, __amdgpu_buffer_rsrc_t tail_rows, int nv, int wave, int lane) {
+    const int quarter = lane >> 4, col = lane & 15;
+    const int64_t ph = static_cast<int64_t>(max(id, 0)) * a.n_kv_heads + kvh;
+    is_tail = page == tail_page;
+    const bool packed = id >= 0 && !is_tail;
+    const __amdgpu_buffer_rsrc_t rc = make_rsrc(a.codes + ph * kCodesBytes, packed ? kCodesBytes : 0u);
+    const __amdgpu_buffer_rsrc_t rp = make_rsrc(a.params + ph * kParamWords, packed ? kParamWords * 4u : 0u);
+    unit = load_unit<W>(rc, (quarter * kGroup + col) * (2 * W), static_cast<uint32_t>(16 * wave) * (2 * W));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint4 p = buf_load16<kAuxCached>(rp, quarter * 64, i * 16);
+      params[4 * i] = p.x; params[4 * i + 1] = p.y; params[4 * i + 2] = p.z; params[4 * i + 3] = p.w;
+    }
+    if (is_tail) {
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
+        const uint32_t at = (16 * wave + col) * (kHeadDim * 2) + quarter * 32 + ks * 8;
+        tail[2 * ks] = __builtin_amdgcn_raw_buffer_load_b64(tail_rows, at, 0, kAuxCached);
+        tail[2 * ks + 1] = __builtin_amdgcn_raw_buffer_load_b64(tail_rows, at, kPairs * 2, kAuxCached);
+      }
+    }
+    const __amdgpu_buffer_rsrc_t rv = make_rsrc(static_cast<const uint8_t*>(a.values) + ph * Values<VB>::kPageBytes,
+                                                id < 0 ? 0u : (VB == 16 ? static_cast<uint32_t>(nv) * (kHeadDim * 2) : Values<VB>::kPageBytes));
+    if constexpr (VB == 16) {
+      const uint32_t voff = quarter * 1024 + col * 16 + (wave & 1) * 8;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) rows[j] = __builtin_amdgcn_raw_buffer_load_b64(rv, voff, (32 * (wave >> 1) + 16 * (j >> 2) + (j & 3)) * 256, kAuxCached);
+    } else {
+      const __amdgpu_buffer_rsrc_t rvp = make_rsrc(a.v_params + ph * kGroup, id < 0 ? 0u : static_cast<uint32_t>(nv) * 4u);
+      quantized.load(rv, rvp, wave >> 1, lane);
+    }
+  }
+  // angle parameters, asked for a page earlier than the rest
+  static __device__ __forceinline__ uint32_t load_angle(const ChunkAttentionArgs& a, int kvh, int id, int lane) {
+    const int64_t ph = static_cast<int64_t>(max(id, 0)) * a.n_kv_heads + kvh;
+    return buf_load4<kAuxCached>(make_rsrc(a.params + ph * kParamWords, id < 0 ? 0u : kParamWords * 4u), lane * 4, kPairs * 4);
+  }
+
+  __device__ __forceinline__ void store(const Keys& keys, int parity, uint8_t* key_image, uint8_t* value_image, int wave, int lane) const {
+    f16x8* const k_to = reinterpret_cast<f16x8*>(key_image) + wave * 4 * 64 + lane;
+    if (is_tail) {
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
+        const u32x2 x = tail[2 * ks], y = tail[2 * ks + 1];
+        k_to[ks * 64] = as_operand(__builtin_amdgcn_perm(y.x, x.x, 0x05040100u), __builtin_amdgcn_perm(y.x, x.x, 0x07060302u),
+                                   __builtin_amdgcn_perm(y.y, x.y, 0x05040100u), __builtin_amdgcn_perm(y.y, x.y, 0x07060302u));
+      }
+    } else {
+      unrolled<4>([&](auto ks_) {
+        constexpr int ks = decltype(ks_)::value;
+        uint32_t w[4];
+        unrolled<4>([&](auto e_) {
+          constexpr int e = decltype(e_)::value, K = 4 * ks + e;
+          const uint32_t sym = symbol<W, K>(unit);
+          const f32x2 t = keys.template trig<K>(sym >> RB, parity);
+          const f16x2 sz = u2h(params[K]);
+          const float s = static_cast<float>(sz.x), rho = fmaf(static_cast<float>(sym & ((1u << RB) - 1u)), s, fmaf(0.5f, s, static_cast<float>(sz.y)));
+          w[e] = h2u(to_half2(rho * t.x, rho * t.y));
+        });
+        k_to[ks * 64] = as_operand(w[0], w[1], w[2], w[3]);
+      });
+    }
+    f16x8* const v_to = reinterpret_cast<f16x8*>(value_image) + ((wave >> 1) * 8 + (wave & 1) * 4) * 64 + lane;
+    if constexpr (VB == 16) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        auto word = [&](int j) { return e < 2 ? rows[j].x : rows[j].y; };
+        const uint32_t pick = e & 1 ? 0x07060302u : 0x05040100u;
+        v_to[e * 64] = as_operand(__builtin_amdgcn_perm(word(1), word(0), pick), __builtin_amdgcn_perm(word(3), word(2), pick),
+                                  __builtin_amdgcn_perm(word(5), word(4), pick), __builtin_amdgcn_perm(word(7), word(6), pick));
+      }
+    } else {
+      if (wave & 1) unrolled<4>([&](auto e) { v_to[decltype(e)::value * 64] = quantized.template operand<4 + decltype(e)::value>(); });
+      else unrolled<4>([&](auto e) { v_to[decltype(e)::value * 64] = quantized.template operand<decltype(e)::value>(); });
+    }
+  }
+};
+
+template <typename Keys, int RB, int VB>
+__device__ __forceinline__ void shared_body(const ChunkAttentionArgs& a) {
+  constexpr int RT = kSharedRT;
+  __shared__ __attribute__((aligned(16))) uint8_t image[2][2][kImage];       // [page parity][keys, values]
+  __shared__ __attribute__((aligned(16))) uint8_t trig[Keys::kLdsBytes];
+  __shared__ float fold_m[kSharedWaves][kSharedRows], fold_l[kSharedWaves][kSharedRows];
+  const int tid = threadIdx.x, wave = uni(tid >> 6), lane = tid & 63, quarter = lane >> 4, col = lane & 15;
+  const int kvh = blockIdx.x % a.n_kv_heads, index = a.n_items - 1 - blockIdx.x / a.n_kv_heads;   // later tokens, which see more, first
+  const int split = blockIdx.y;
+  Item item;
+  if (!find_item(a, index, lane, item)) return;
+  const int first_position = item.len - item.n + item.first, last_position = first_position + item.count - 1;
+  const VisiblePages pages = visible_pages(a, first_position, last_position);
+  const int per = whole_rounds((pages.count() + a.n_splits - 1) / a.n_splits);
+  const int begin = uni(split * per), end = uni(min(begin + per, pages.count()));
+  if (split > 0 && begin >= end) return;
+
+  // wavefront = (rows 32 group .., part of each page): `groups` row groups, a power of two; a part is 4 / parts steps of 32 tokens, or
+  // (eight parts) one step of every other page
+  const int n_rows = item.count * a.group, needed = (n_rows + kSharedRows - 1) / kSharedRows;
+  const int groups = needed > 4 ? 8 : (needed > 2 ? 4 : needed), parts = kSharedWaves / groups;
+  const int row_group = uni(wave & (groups - 1)), part = uni(wave / groups);
+  const bool computes = uni(row_group * kSharedRows < n_rows ? 1 : 0);
+  const int step0 = uni(parts >= 4 ? part & 3 : part * (4 / parts)), step1 = uni(parts >= 4 ? step0 + 1 : step0 + 4 / parts);
+
+  int position[RT];
+  f16x8 q[RT][4];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int row = row_group * kSharedRows + 16 * rt + col, token = row / a.group, head = row - token * a.group;
+    const bool there = token < item.count;
+    position[rt] = there ? first_position + token : INT32_MAX;
+    const __half* const at = a.q + ((item.row0 + item.first + (there ? token : 0)) * a.n_q_heads + kvh * a.group + (there ? head : 0)) * kHeadDim;
+    const uint32_t sign = a.negate ? 0x80008000u : 0u;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      u32x2 x, y;
+      __builtin_memcpy(&x, at + 16 * quarter + 4 * ks, 8);
+      __builtin_memcpy(&y, at + kPairs + 16 * quarter + 4 * ks, 8);
+      q[rt][ks] = as_operand(__builtin_amdgcn_perm(y.x, x.x, 0x05040100u) ^ sign, __builtin_amdgcn_perm(y.x, x.x, 0x07060302u) ^ sign,
+                             __builtin_amdgcn_perm(y.y, x.y, 0x05040100u) ^ sign, __builtin_amdgcn_perm(y.y, x.y, 0x07060302u) ^ sign);
+    }
+  }
+  // positions of the wavefront's rows
+  const int wave_first = uni(first_position + row_group * kSharedRows / a.group);
+  const int wave_last = uni(min(last_position, first_position + (row_group * kSharedRows + kSharedRows - 1) / a.group));
+
+  const int tail_page = a.residual != nullptr && item.len % kGroup != 0 ? item.len / kGroup : -1;
+  const __amdgpu_buffer_rsrc_t tail_rows = make_rsrc(a.residual + (static_cast<int64_t>(item.seq) * a.n_kv_heads + kvh) * (kGroup * kHeadDim),
+                                                     tail_page >= 0 ? static_cast<uint32_t>(item.len % kGroup) * (kHeadDim * 2) : 0u);
+  const int32_t* const table = a.block_table + static_cast<int64_t>(item.seq) * a.max_pages_per_seq;
+  auto page_of = [&](int at) { return uni(at < pages.n_first ? at : pages.from + at - pages.n_first); };
+  auto id_of = [&](int at) {                                               // -1: masked, or past the end
+    if (at >= end) return -1;
+    const int page = page_of(at);
+    const int id = page < a.max_pages_per_seq ? uni(table[page]) : -1;
+    return id < 0 || id >= a.n_pool_pages ? -1 : id;
+  };
+
+  float m[RT], l[RT];
+  f32x4 acc[8][RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    m[rt] = kNegInf;
+    l[rt] = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e][rt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  Keys keys;
+  keys.init(trig, a, tid);
+  PageProducer<Keys, RB, VB> producer;
+  auto load_page = [&](int at, int id) {
+    const int page = page_of(at);
+    producer.load(a, kvh, id, page, tail_page, tail_rows, min(kGroup, item.len - page * kGroup), wave, lane);
+  };
+  // page `begin` into image[0]; page begin + 1 on its way
+  int id = id_of(begin), id1 = id_of(begin + 1);
+  if (begin < end) load_page(begin, id);
+  if constexpr (Keys::kGrouped) {
+    keys.build(producer.load_angle(a, kvh, id, lane), 0, tid);
+    keys.build(producer.load_angle(a, kvh, id1, lane), 1, tid);
+  }
+  __syncthreads();
+  if (begin < end) producer.store(keys, 0, image[0][0], image[0][1], wave, lane);
+  if (begin + 1 < end) load_page(begin + 1, id1);
+  __syncthreads();
+
+  for (int at = begin; at < end; ++at) {
+    const int parity = (at - begin) & 1, page = page_of(at);
+    const bool masked_page = id < 0;
+    id = id1;
+    if (at + 1 < end) {
+      producer.store(keys, parity ^ 1, image[parity ^ 1][0], image[parity ^ 1][1], wave, lane);
+      id1 = id_of(at + 2);
+      if (at + 2 < end) load_page(at + 2, id1);
+      if constexpr (Keys::kGrouped) {
+        // the table of this page's parity has been read (before the last barrier)
+        keys.build(producer.load_angle(a, kvh, id1, lane), parity, tid);
+      }
+    }
+    const bool mine = computes && !masked_page && (parts < 8 || (part >> 2) == parity);
+    if (mine) {
+      const f16x8* const k_image = reinterpret_cast<const f16x8*>(image[parity][0]) + lane;
+      const f16x8* const v_image = reinterpret_cast<const f16x8*>(image[parity][1]) + lane;
+#pragma unroll 1
+      for (int step = step0; step < step1; ++step) {
+        const int token0 = page * kGroup + 32 * step;
+        // nobody sees the step's tokens
+        if (token0 > wave_last || (a.window > 0 && token0 >= a.n_sinks && token0 + 31 <= wave_first - a.window)) continue;
+        const bool masks = token0 + 31 > wave_first || (a.window > 0 && token0 <= wave_last - a.window && token0 + 31 >= a.n_sinks);
+        f32x4 s[2][RT];
+#pragma unroll
+        for (int tile = 0; tile < 2; ++tile)
+#pragma unroll
+          for (int ks = 0; ks < 4; ++ks) {
+            const f16x8 k_op = k_image[((2 * step + tile) * 4 + ks) * 64];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+              const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+              s[tile][rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k_op, q[rt][ks], ks == 0 ? zero : s[tile][rt], 0, 0, 0);
+            }
+          }
+        if (masks) {
+#pragma unroll
+          for (int tile = 0; tile < 2; ++tile)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int token = token0 + 16 * tile + 4 * quarter + i;
+#pragma unroll
+              for (int rt = 0; rt < RT; ++rt) {
+                bool seen = token <= position[rt];
+                if (a.window > 0) seen = seen && (position[rt] - token < a.window || token < a.n_sinks);
+                if (!seen) s[tile][rt][i] = kNegInf;
+              }
+            }
+        }
+        float top[RT];
+        bool above = false;
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          float x = max3(s[0][rt][0], s[0][rt][1], s[0][rt][2]);
+          x = max3(x, s[0][rt][3], s[1][rt][0]);
+          x = max3(x, s[1][rt][1], s[1][rt][2]);
+          top[rt] = max2(x, s[1][rt][3]) * a.scale_log2;
+          above = above || top[rt] > m[rt] + kSlack;
+        }
+        if (__builtin_amdgcn_ballot_w64(above) != 0) {
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            float x = top[rt];
+            auto r = __builtin_amdgcn_permlane16_swap(f2u(x), f2u(x), false, false);
+            x = max2(u2f(r[0]), u2f(r[1]));
+            auto r2 = __builtin_amdgcn_permlane32_swap(f2u(x), f2u(x), false, false);
+            x = max3(u2f(r2[0]), u2f(r2[1]), m[rt]);
+            const float keep = x > kNegInf ? __builtin_amdgcn_exp2f(m[rt] - x) : 1.f;
+            m[rt] = x;
+            l[rt] *= keep;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e][rt] *= keep;
+          }
+        }
+        f16x8 p_op[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          const float off = m[rt] > kNegInf ? kLift - m[rt] : 0.f;
+          uint32_t w[4];
+#pragma unroll
+          for (int tile = 0; tile < 2; ++tile)
+#pragma unroll
+            for (int pair = 0; pair < 2; ++pair) {
+              const f16x2 p = to_half2(__builtin_amdgcn_exp2f(fmaf(s[tile][rt][2 * pair], a.scale_log2, off)),
+                                       __builtin_amdgcn_exp2f(fmaf(s[tile][rt][2 * pair + 1], a.scale_log2, off)));
+              w[2 * tile + pair] = h2u(p);
+              l[rt] = __builtin_amdgcn_fdot2(p, f16x2{static_cast<_Float16>(1.f), static_cast<_Float16>(1.f)}, l[rt], false);
+            }
+          p_op[rt] = as_operand(w[0], w[1], w[2], w[3]);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const f16x8 v_op = v_image[(step * 8 + e) * 64];
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) acc[e][rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v_op, p_op[rt], acc[e][rt], 0, 0, 0);
+        }
+      }
+    }
+    __syncthreads();
+  }
+
+  // ---- fold the parts of a row group ----
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) l[rt] = sum_rows(l[rt]);
+  if (parts > 1) {
+    if (quarter == 0) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        fold_m[wave][16 * rt + col] = m[rt];
+        fold_l[wave][16 * rt + col] = l[rt];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      float top = kNegInf, total = 0.f;
+      for (int p = 0; p < parts; ++p) top = fmaxf(top, fold_m[row_group + p * groups][16 * rt + col]);
+      for (int p = 0; p < parts; ++p)
+        total += top > kNegInf ? fold_l[row_group + p * groups][16 * rt + col] * __builtin_amdgcn_exp2f(fold_m[row_group + p * groups][16 * rt + col] - top) : 0.f;
+      const float weight = top > kNegInf ? __builtin_amdgcn_exp2f(m[rt] - top) : 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e][rt] *= weight;
+      m[rt] = top;
+      l[rt] = total;
+    }
+    f32x4* const room = reinterpret_cast<f32x4*>(&image[0][0][0]);           // 16 KB a wavefront
+    if (part > 0) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) room[(wave * 8 * RT + e * RT + rt) * 64 + lane] = acc[e][rt];
+    }
+    __syncthreads();
+    if (part > 0) return;
+    for (int p = 1; p < parts; ++p) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) acc[e][rt] += room[((row_group + p * groups) * 8 * RT + e * RT + rt) * 64 + lane];
+    }
+  }
+  if (!computes) return;
+  // lane: dims 32 quarter + 8 i + e of its rows
+  if (a.n_splits > 1) {
+    const int64_t slot = (static_cast<int64_t>(index) * a.n_kv_heads + kvh) * a.n_splits + split;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const int64_t row = slot * kTileRows + row_group * kSharedRows + 16 * rt + col;
+      float* const to = a.ws_acc + row * kHeadDim + 32 * quarter;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        *reinterpret_cast<f32x4*>(to + 8 * i) = f32x4{acc[0][rt][i], acc[1][rt][i], acc[2][rt][i], acc[3][rt][i]};
+        *reinterpret_cast<f32x4*>(to + 8 * i + 4) = f32x4{acc[4][rt][i], acc[5][rt][i], acc[6][rt][i], acc[7][rt][i]};
+      }
+      if (quarter == 0) {
+        a.ws_ml[row * 2] = m[rt];
+        a.ws_ml[row * 2 + 1] = l[rt];
+      }
+    }
+    return;
+  }
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int row = row_group * kSharedRows + 16 * rt + col, token = row / a.group, head = row - token * a.group;
+    if (token >= item.count) continue;
+    const float inv = l[rt] > 0.f ? 1.f / l[rt] : 0.f;
+    __half* const to = a.out + ((item.row0 + item.first + token) * a.n_q_heads + kvh * a.group + head) * kHeadDim + 32 * quarter;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<u32x4*>(to + 8 * i) = u32x4{h2u(to_half2(acc[0][rt][i] * inv, acc[1][rt][i] * inv)), h2u(to_half2(acc[2][rt][i] * inv, acc[3][rt][i] * inv)),
+                                                    h2u(to_half2(acc[4][rt][i] * inv, acc[5][rt][i] * inv)), h2u(to_half2(acc[6][rt][i] * inv, acc[7][rt][i] * inv))};
+  }
+}
+
 }  // namespace chunk
 }  // namespace
 }  // namespace pq
