@@ -14,7 +14,7 @@ namespace {
 namespace chunk {
 
 #define PQ_CHUNK_ATTR(rt) __launch_bounds__(kChunkWaves * 64) __attribute__((amdgpu_waves_per_eu(rt == 1 ? 2 : 1, rt == 1 ? 2 : 1)))
-#define PQ_SHARED_ATTR __launch_bounds__(kSharedWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
+#define PQ_SHARED_ATTR __launch_bounds__(kSharedWaves * 64) __attribute__((amdgpu_waves_per_eu(kSharedWaves / 4, kSharedWaves / 4)))
 
 template <int RB, int TB, int VB, bool kGrouped>
 __global__ PQ_SHARED_ATTR void pq_chunk_shared_kernel(const ChunkAttentionArgs a) {

@@ -543,36 +543,40 @@ __device__ __forceinline__ void attention_body(const ChunkAttentionArgs& a) {
 }
 
 // ---- many rows: operands shared through LDS -------------------------------------------------------------------
-// A work-group of 8 wavefronts serves up to 256 rows of one KV head.  Each page is unpacked once: wavefront w makes the key operands of
-// tile w (16 tokens) and half of the value operands of step w / 2 (32 tokens) and stores them as the matrix instructions
-// read them, 16 bytes a lane, while everybody computes with the page before; one barrier a page.  A wavefront has 32 rows,
-// or, where the work-group has fewer, shares them with others that take other tokens of the page.
-constexpr int kSharedWaves = 8;
-constexpr int kSharedRows = 32;                    // of a wavefront
-constexpr int kSharedRT = kSharedRows / 16;
+// A work-group of 16 wavefronts serves up to 256 rows of one KV head.  Each page is unpacked once: wavefront w makes half of the key
+// operands of tile w / 2 (16 tokens), and of the value operands of step w / 4 (32 tokens) half of the dims of one of the two tiles, and
+// stores them as the matrix instructions read them, 16 bytes a lane, while everybody computes with the page before; one barrier a
+// page.  A wavefront has 16 rows, or, where the work-group has fewer, shares them with others that take other tokens.
+//
+// The score product carries the scale (in the keys) and, as what its accumulators start from, kLift - m: what comes out is the
+// exponent.  Sums of weights are a matrix product too, with ones.
+//
+// Four wavefronts a SIMD, 128 registers each: while one waits for its matrix instructions or its LDS reads the others' exponentials
+// (16 cycles each, the largest part of the vector unit's work) run.
+constexpr int kSharedWaves = 16;
+constexpr int kSharedRows = 16;                    // of a wavefront
 constexpr int kTileRows = kSharedWaves * kSharedRows;
 constexpr int kImage = kGroup * kHeadDim * 2;      // bytes of a page's key or value operands
 
-// Key coordinates in fp32, rounded once.  trig: (cos, sin) of the angle levels.
+// Key coordinates are made in fp32 and rounded once.  trig<K>(): scale times (cos, sin) of the angle level of pair K (of the 8 that a
+// lane has).
 template <int RB, int TB>
 struct SharedUniformKeys {
   static constexpr int W = RB + TB, NA = 1 << TB;
   static constexpr int kLdsBytes = NA * 256;       // 32 copies of an entry: no bank conflicts
   static constexpr bool kGrouped = false;
-  uint32_t table, lane_at;
-  __device__ __forceinline__ void init(const uint8_t* lds, const ChunkAttentionArgs&, int tid) {
-    table = lds_addr(lds);
-    lane_at = (tid & 31) * 8;
+  uint32_t lane_at;
+  __device__ __forceinline__ void init(const uint8_t* lds, float scale, int tid) {
+    const uint32_t table = lds_addr(lds);
+    lane_at = table + (tid & 31) * 8;
     for (int i = tid; i < NA * 32; i += kSharedWaves * 64) {
-      const float turns = (static_cast<float>(i >> 5) + 0.5f) * (1.f / NA) - 0.5f;
-      *(PQ_LDS f32x2*)static_cast<uintptr_t>(table + i * 8) = f32x2{cosf(turns * 6.283185307179586f), sinf(turns * 6.283185307179586f)};
+      const float angle = ((static_cast<float>(i >> 5) + 0.5f) * (1.f / NA) - 0.5f) * 6.283185307179586f;
+      *(PQ_LDS f32x2*)static_cast<uintptr_t>(table + i * 8) = f32x2{cosf(angle) * scale, sinf(angle) * scale};
     }
   }
   __device__ __forceinline__ void build(uint32_t, int, int) {}
   template <int K>
-  __device__ __forceinline__ f32x2 trig(uint32_t angle, int) const {
-    return *(const PQ_LDS f32x2*)static_cast<uintptr_t>(table + lane_at + angle * 256);
-  }
+  __device__ __forceinline__ f32x2 trig(uint32_t angle, int) const { return *(const PQ_LDS f32x2*)static_cast<uintptr_t>(lane_at + angle * 256); }
 };
 // Grouped quantizer: the page's levels, as fp16, made by the work-group for the page after the next (two tables).
 template <int RB, int TB>
@@ -582,13 +586,15 @@ struct SharedGroupedKeys {
   static constexpr int kLdsBytes = 2 * kPageBytes;
   static constexpr bool kGrouped = true;
   uint32_t table, row;
-  __device__ __forceinline__ void init(const uint8_t* lds, const ChunkAttentionArgs&, int tid) {
+  float scale;
+  __device__ __forceinline__ void init(const uint8_t* lds, float scale_, int tid) {
     table = lds_addr(lds);
-    row = table + ((tid & 63) >> 4) * (16 * NA * 4);
+    row = table + (((tid & 63) >> 4) * 16 + ((tid >> 6) & 1) * 8) * (NA * 4);
+    scale = scale_;
   }
   // angle: {fp16 s, fp16 z} of pair `lane`
   __device__ __forceinline__ void build(uint32_t angle, int parity, int tid) {
-    const int lane = tid & 63, wave = tid >> 6;
+    const int lane = tid & 63, wave = uni(tid >> 6);
     const float level = static_cast<float>(lane & (NA - 1)) + 0.5f;
     constexpr int kPairsAtOnce = 64 >> TB;
     for (int it = wave; it < NA; it += kSharedWaves) {
@@ -600,7 +606,55 @@ struct SharedGroupedKeys {
   template <int K>
   __device__ __forceinline__ f32x2 trig(uint32_t angle, int parity) const {
     const f16x2 t = u2h(*(const PQ_LDS uint32_t*)static_cast<uintptr_t>(row + parity * kPageBytes + K * (NA * 4) + angle * 4));
-    return f32x2{static_cast<float>(t.x), static_cast<float>(t.y)};
+    return f32x2{static_cast<float>(t.x) * scale, static_cast<float>(t.y) * scale};
+  }
+};
+
+// A wavefront's part of the value operands: words 2 tile, + 1 (the lane's tokens of one tile) of dims 4 half .. + 3 of each slice.
+template <int VB>
+struct PartValues {
+  uint32_t word[2], par[4];                        // of the two token pairs; {s, z} of the four tokens
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rv, __amdgpu_buffer_rsrc_t rvp, int step, int tile, int half, int lane) {
+    const uint32_t quarter = lane >> 4, slice = lane & 15;
+    const u32x4 p = __builtin_amdgcn_raw_buffer_load_b128(rvp, quarter * 16, (32 * step + 16 * tile) * 4, kAuxCached);
+    par[0] = p.x; par[1] = p.y; par[2] = p.z; par[3] = p.w;
+    if constexpr (VB == 4) {
+      const uint32_t at = quarter * 256 + slice * 16 + half * 4, block = (8 * step + 4 * tile) * 256;
+      word[0] = buf_load4<kAuxCached>(rv, at, block);
+      word[1] = buf_load4<kAuxCached>(rv, at + 8, block);
+    } else {
+      const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(rv, (quarter >> 1) * 256 + slice * 16 + (quarter & 1) * 8, (4 * step + 2 * tile) * 256, kAuxCached);
+      word[0] = v.x;
+      word[1] = v.y;
+    }
+  }
+  template <int E>
+  __device__ __forceinline__ u32x2 operand(int half) const {
+    constexpr uint32_t kMask = ((1u << VB) - 1u) * 0x10001u;
+    const f16x2 base = {static_cast<_Float16>(1024.f), static_cast<_Float16>(1024.f)};
+    uint32_t w[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t x = VB == 2 ? word[i] >> (8 * half) : word[i];
+      w[i] = h2u(__builtin_elementwise_fma(u2h(((x >> (VB * E)) & kMask) | 0x64006400u) - base, u2h(__builtin_amdgcn_perm(par[2 * i + 1], par[2 * i], 0x05040100u)),
+                                           u2h(__builtin_amdgcn_perm(par[2 * i + 1], par[2 * i], 0x07060302u))));
+    }
+    return u32x2{w[0], w[1]};
+  }
+};
+template <>
+struct PartValues<16> {
+  u32x2 row[4];
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rv, __amdgpu_buffer_rsrc_t, int step, int tile, int half, int lane) {
+    const uint32_t voff = (lane >> 4) * 1024 + (lane & 15) * 16 + half * 8;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) row[j] = __builtin_amdgcn_raw_buffer_load_b64(rv, voff, (32 * step + 16 * tile + j) * 256, kAuxCached);
+  }
+  template <int E>
+  __device__ __forceinline__ u32x2 operand(int) const {
+    auto word = [&](int j) { return E < 2 ? row[j].x : row[j].y; };
+    constexpr uint32_t kPick = E & 1 ? 0x07060302u : 0x05040100u;
+    return u32x2{__builtin_amdgcn_perm(word(1), word(0), kPick), __builtin_amdgcn_perm(word(3), word(2), kPick)};
   }
 };
 
@@ -610,45 +664,46 @@ struct PageProducer {
   static constexpr int W = Keys::W;
   static constexpr uint32_t kCodesBytes = kBlocks * kGroup * 2 * W;
   static constexpr uint32_t kParamWords = kPairs * (Keys::kGrouped ? 2 : 1);
-  Unit<W / 2> unit;
-  uint32_t params[16], angle;
-  u32x2 rows[VB == 16 ? 8 : 1];
-  Values<VB == 16 ? 4 : VB> quantized;
-  u32x2 tail[8];                                    // un-quantized keys, x and y of four pairs, four times
+  uint32_t codes[2];                               // 8 symbols
+  uint32_t params[8];                              // {s, z} of their pairs; in the tail page un-quantized keys, x and y of four pairs twice
+  PartValues<VB> values;
   bool is_tail;
 
   // id < 0: masked, zeros everywhere
-  __device__ __forceinline__ void load(const ChunkAttentionArgs& a, int kvh, int id, int page, int tail_page, __amdgpu_buffer_rsrc_t tail_rows, int nv, int wave, int lane) {
-    const int quarter = lane >> 4, col = lane & 15;
+  __device__ __forceinline__ void load(const ChunkAttentionArgs& a, int kvh, int id, bool tail, __amdgpu_buffer_rsrc_t tail_rows, int nv, int wave, int lane) {
+    const int quarter = lane >> 4, col = lane & 15, half = wave & 1;
     const int64_t ph = static_cast<int64_t>(max(id, 0)) * a.n_kv_heads + kvh;
-    is_tail = page == tail_page;
+    is_tail = tail;
     const bool packed = id >= 0 && !is_tail;
     const __amdgpu_buffer_rsrc_t rc = make_rsrc(a.codes + ph * kCodesBytes, packed ? kCodesBytes : 0u);
     const __amdgpu_buffer_rsrc_t rp = make_rsrc(a.params + ph * kParamWords, packed ? kParamWords * 4u : 0u);
-    unit = load_unit<W>(rc, (quarter * kGroup + col) * (2 * W), static_cast<uint32_t>(16 * wave) * (2 * W));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint4 p = buf_load16<kAuxCached>(rp, quarter * 64, i * 16);
-      params[4 * i] = p.x; params[4 * i + 1] = p.y; params[4 * i + 2] = p.z; params[4 * i + 3] = p.w;
+    const uint32_t unit = (quarter * kGroup + col) * (2 * W), tile = static_cast<uint32_t>(16 * (wave >> 1)) * (2 * W);
+    if constexpr (W == 8) {
+      const u32x2 c = __builtin_amdgcn_raw_buffer_load_b64(rc, unit + half * 8, tile, kAuxCached);
+      codes[0] = c.x;
+      codes[1] = c.y;
+    } else {
+      const u32x2 c = __builtin_amdgcn_raw_buffer_load_b64(rc, unit + half * 4, tile, kAuxCached);       // 48 bits from bit 0, or from bit 16
+      codes[0] = half ? __builtin_amdgcn_alignbit(c.y, c.x, 16) : c.x;
+      codes[1] = half ? c.y >> 16 : c.y;
     }
-    if (is_tail) {
+    if (!is_tail) {
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) {
-        const uint32_t at = (16 * wave + col) * (kHeadDim * 2) + quarter * 32 + ks * 8;
-        tail[2 * ks] = __builtin_amdgcn_raw_buffer_load_b64(tail_rows, at, 0, kAuxCached);
-        tail[2 * ks + 1] = __builtin_amdgcn_raw_buffer_load_b64(tail_rows, at, kPairs * 2, kAuxCached);
+      for (int i = 0; i < 2; ++i) {
+        const uint4 p = buf_load16<kAuxCached>(rp, quarter * 64 + half * 32, i * 16);
+        params[4 * i] = p.x; params[4 * i + 1] = p.y; params[4 * i + 2] = p.z; params[4 * i + 3] = p.w;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t at = (16 * (wave >> 1) + col) * (kHeadDim * 2) + quarter * 32 + half * 16 + i * 8;
+        const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(tail_rows, at, 0, kAuxCached), y = __builtin_amdgcn_raw_buffer_load_b64(tail_rows, at, kPairs * 2, kAuxCached);
+        params[4 * i] = x.x; params[4 * i + 1] = x.y; params[4 * i + 2] = y.x; params[4 * i + 3] = y.y;
       }
     }
     const __amdgpu_buffer_rsrc_t rv = make_rsrc(static_cast<const uint8_t*>(a.values) + ph * Values<VB>::kPageBytes,
                                                 id < 0 ? 0u : (VB == 16 ? static_cast<uint32_t>(nv) * (kHeadDim * 2) : Values<VB>::kPageBytes));
-    if constexpr (VB == 16) {
-      const uint32_t voff = quarter * 1024 + col * 16 + (wave & 1) * 8;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) rows[j] = __builtin_amdgcn_raw_buffer_load_b64(rv, voff, (32 * (wave >> 1) + 16 * (j >> 2) + (j & 3)) * 256, kAuxCached);
-    } else {
-      const __amdgpu_buffer_rsrc_t rvp = make_rsrc(a.v_params + ph * kGroup, id < 0 ? 0u : static_cast<uint32_t>(nv) * 4u);
-      quantized.load(rv, rvp, wave >> 1, lane);
-    }
+    values.load(rv, make_rsrc(VB == 16 ? a.v_params : a.v_params + ph * kGroup, VB == 16 || id < 0 ? 0u : static_cast<uint32_t>(nv) * 4u), wave >> 2, (wave >> 1) & 1, half, lane);
   }
   // angle parameters, asked for a page earlier than the rest
   static __device__ __forceinline__ uint32_t load_angle(const ChunkAttentionArgs& a, int kvh, int id, int lane) {
@@ -656,49 +711,44 @@ struct PageProducer {
     return buf_load4<kAuxCached>(make_rsrc(a.params + ph * kParamWords, id < 0 ? 0u : kParamWords * 4u), lane * 4, kPairs * 4);
   }
 
-  __device__ __forceinline__ void store(const Keys& keys, int parity, uint8_t* key_image, uint8_t* value_image, int wave, int lane) const {
-    f16x8* const k_to = reinterpret_cast<f16x8*>(key_image) + wave * 4 * 64 + lane;
+  __device__ __forceinline__ void store(const Keys& keys, int parity, float scale, uint8_t* key_image, uint8_t* value_image, int wave, int lane) const {
+    f16x8* const k_to = reinterpret_cast<f16x8*>(key_image) + ((wave >> 1) * 4 + (wave & 1) * 2) * 64 + lane;
     if (is_tail) {
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) {
-        const u32x2 x = tail[2 * ks], y = tail[2 * ks + 1];
-        k_to[ks * 64] = as_operand(__builtin_amdgcn_perm(y.x, x.x, 0x05040100u), __builtin_amdgcn_perm(y.x, x.x, 0x07060302u),
-                                   __builtin_amdgcn_perm(y.y, x.y, 0x05040100u), __builtin_amdgcn_perm(y.y, x.y, 0x07060302u));
+      for (int i = 0; i < 2; ++i) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const f16x2 x = u2h(params[4 * i + (e >> 1)]), y = u2h(params[4 * i + 2 + (e >> 1)]);
+          w[e] = h2u(to_half2(static_cast<float>(x[e & 1]) * scale, static_cast<float>(y[e & 1]) * scale));
+        }
+        k_to[i * 64] = as_operand(w[0], w[1], w[2], w[3]);
       }
     } else {
-      unrolled<4>([&](auto ks_) {
-        constexpr int ks = decltype(ks_)::value;
+      Unit<W / 2> unit;
+      unit.d[0] = codes[0];
+      unit.d[1] = codes[1];
+      unrolled<2>([&](auto i_) {
+        constexpr int i = decltype(i_)::value;
         uint32_t w[4];
         unrolled<4>([&](auto e_) {
-          constexpr int e = decltype(e_)::value, K = 4 * ks + e;
+          constexpr int e = decltype(e_)::value, K = 4 * i + e;
           const uint32_t sym = symbol<W, K>(unit);
           const f32x2 t = keys.template trig<K>(sym >> RB, parity);
           const f16x2 sz = u2h(params[K]);
           const float s = static_cast<float>(sz.x), rho = fmaf(static_cast<float>(sym & ((1u << RB) - 1u)), s, fmaf(0.5f, s, static_cast<float>(sz.y)));
           w[e] = h2u(to_half2(rho * t.x, rho * t.y));
         });
-        k_to[ks * 64] = as_operand(w[0], w[1], w[2], w[3]);
+        k_to[i * 64] = as_operand(w[0], w[1], w[2], w[3]);
       });
     }
-    f16x8* const v_to = reinterpret_cast<f16x8*>(value_image) + ((wave >> 1) * 8 + (wave & 1) * 4) * 64 + lane;
-    if constexpr (VB == 16) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        auto word = [&](int j) { return e < 2 ? rows[j].x : rows[j].y; };
-        const uint32_t pick = e & 1 ? 0x07060302u : 0x05040100u;
-        v_to[e * 64] = as_operand(__builtin_amdgcn_perm(word(1), word(0), pick), __builtin_amdgcn_perm(word(3), word(2), pick),
-                                  __builtin_amdgcn_perm(word(5), word(4), pick), __builtin_amdgcn_perm(word(7), word(6), pick));
-      }
-    } else {
-      if (wave & 1) unrolled<4>([&](auto e) { v_to[decltype(e)::value * 64] = quantized.template operand<4 + decltype(e)::value>(); });
-      else unrolled<4>([&](auto e) { v_to[decltype(e)::value * 64] = quantized.template operand<decltype(e)::value>(); });
-    }
+    u32x2* const v_to = reinterpret_cast<u32x2*>(value_image) + (((wave >> 2) * 8 + (wave & 1) * 4) * 64 + lane) * 2 + ((wave >> 1) & 1);
+    unrolled<4>([&](auto e) { v_to[decltype(e)::value * 128] = values.template operand<decltype(e)::value>(wave & 1); });
   }
 };
 
 template <typename Keys, int RB, int VB>
 __device__ __forceinline__ void shared_body(const ChunkAttentionArgs& a) {
-  constexpr int RT = kSharedRT;
   __shared__ __attribute__((aligned(16))) uint8_t image[2][2][kImage];       // [page parity][keys, values]
   __shared__ __attribute__((aligned(16))) uint8_t trig[Keys::kLdsBytes];
   __shared__ float fold_m[kSharedWaves][kSharedRows], fold_l[kSharedWaves][kSharedRows];
@@ -713,30 +763,29 @@ __device__ __forceinline__ void shared_body(const ChunkAttentionArgs& a) {
   const int begin = uni(split * per), end = uni(min(begin + per, pages.count()));
   if (split > 0 && begin >= end) return;
 
-  // wavefront = (rows 32 group .., part of each page): `groups` row groups, a power of two; a part is 4 / parts steps of 32 tokens, or
-  // (eight parts) one step of every other page
+  // wavefront = (rows 16 row_group .., part): `groups` row groups, a power of two; a part is 4 / parts steps of 32 tokens of each page, or,
+  // from eight parts on, one step of every (parts / 4)-th page
   const int n_rows = item.count * a.group, needed = (n_rows + kSharedRows - 1) / kSharedRows;
-  const int groups = needed > 4 ? 8 : (needed > 2 ? 4 : needed), parts = kSharedWaves / groups;
+  const int groups = needed > 8 ? 16 : (needed > 4 ? 8 : (needed > 2 ? 4 : needed)), parts = kSharedWaves / groups;
   const int row_group = uni(wave & (groups - 1)), part = uni(wave / groups);
   const bool computes = uni(row_group * kSharedRows < n_rows ? 1 : 0);
   const int step0 = uni(parts >= 4 ? part & 3 : part * (4 / parts)), step1 = uni(parts >= 4 ? step0 + 1 : step0 + 4 / parts);
+  const int phase = part >> 2, phases = parts >= 4 ? parts / 4 : 1;          // a power of two
 
-  int position[RT];
-  f16x8 q[RT][4];
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const int row = row_group * kSharedRows + 16 * rt + col, token = row / a.group, head = row - token * a.group;
-    const bool there = token < item.count;
-    position[rt] = there ? first_position + token : INT32_MAX;
-    const __half* const at = a.q + ((item.row0 + item.first + (there ? token : 0)) * a.n_q_heads + kvh * a.group + (there ? head : 0)) * kHeadDim;
+  const int row = row_group * kSharedRows + col, row_token = row / a.group, row_head = row - row_token * a.group;
+  const bool row_there = row_token < item.count;
+  const int position = row_there ? first_position + row_token : INT32_MAX;
+  const int64_t row_at = ((item.row0 + item.first + (row_there ? row_token : 0)) * a.n_q_heads + kvh * a.group + (row_there ? row_head : 0)) * kHeadDim;
+  f16x8 q[4];
+  {
     const uint32_t sign = a.negate ? 0x80008000u : 0u;
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) {
       u32x2 x, y;
-      __builtin_memcpy(&x, at + 16 * quarter + 4 * ks, 8);
-      __builtin_memcpy(&y, at + kPairs + 16 * quarter + 4 * ks, 8);
-      q[rt][ks] = as_operand(__builtin_amdgcn_perm(y.x, x.x, 0x05040100u) ^ sign, __builtin_amdgcn_perm(y.x, x.x, 0x07060302u) ^ sign,
-                             __builtin_amdgcn_perm(y.y, x.y, 0x05040100u) ^ sign, __builtin_amdgcn_perm(y.y, x.y, 0x07060302u) ^ sign);
+      __builtin_memcpy(&x, a.q + row_at + 16 * quarter + 4 * ks, 8);
+      __builtin_memcpy(&y, a.q + row_at + kPairs + 16 * quarter + 4 * ks, 8);
+      q[ks] = as_operand(__builtin_amdgcn_perm(y.x, x.x, 0x05040100u) ^ sign, __builtin_amdgcn_perm(y.x, x.x, 0x07060302u) ^ sign,
+                         __builtin_amdgcn_perm(y.y, x.y, 0x05040100u) ^ sign, __builtin_amdgcn_perm(y.y, x.y, 0x07060302u) ^ sign);
     }
   }
   // positions of the wavefront's rows
@@ -755,21 +804,17 @@ __device__ __forceinline__ void shared_body(const ChunkAttentionArgs& a) {
     return id < 0 || id >= a.n_pool_pages ? -1 : id;
   };
 
-  float m[RT], l[RT];
-  f32x4 acc[8][RT];
+  // off = kLift - m (0 as long as the row has seen nothing); a score above `limit` makes the row's m rise
+  float off = 0.f, limit = kNegInf;
+  f32x4 acc[8], sums = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    m[rt] = kNegInf;
-    l[rt] = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e][rt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
+  for (int e = 0; e < 8; ++e) acc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
   Keys keys;
-  keys.init(trig, a, tid);
+  keys.init(trig, a.scale_log2, tid);
   PageProducer<Keys, RB, VB> producer;
   auto load_page = [&](int at, int id) {
     const int page = page_of(at);
-    producer.load(a, kvh, id, page, tail_page, tail_rows, min(kGroup, item.len - page * kGroup), wave, lane);
+    producer.load(a, kvh, id, page == tail_page, tail_rows, min(kGroup, item.len - page * kGroup), wave, lane);
   };
   // page `begin` into image[0]; page begin + 1 on its way
   int id = id_of(begin), id1 = id_of(begin + 1);
@@ -779,7 +824,7 @@ __device__ __forceinline__ void shared_body(const ChunkAttentionArgs& a) {
     keys.build(producer.load_angle(a, kvh, id1, lane), 1, tid);
   }
   __syncthreads();
-  if (begin < end) producer.store(keys, 0, image[0][0], image[0][1], wave, lane);
+  if (begin < end) producer.store(keys, 0, a.scale_log2, image[0][0], image[0][1], wave, lane);
   if (begin + 1 < end) load_page(begin + 1, id1);
   __syncthreads();
 
@@ -788,16 +833,13 @@ __device__ __forceinline__ void shared_body(const ChunkAttentionArgs& a) {
     const bool masked_page = id < 0;
     id = id1;
     if (at + 1 < end) {
-      producer.store(keys, parity ^ 1, image[parity ^ 1][0], image[parity ^ 1][1], wave, lane);
+      producer.store(keys, parity ^ 1, a.scale_log2, image[parity ^ 1][0], image[parity ^ 1][1], wave, lane);
       id1 = id_of(at + 2);
       if (at + 2 < end) load_page(at + 2, id1);
-      if constexpr (Keys::kGrouped) {
-        // the table of this page's parity has been read (before the last barrier)
-        keys.build(producer.load_angle(a, kvh, id1, lane), parity, tid);
-      }
+      // the table of this page's parity has been read (before the last barrier)
+      if constexpr (Keys::kGrouped) keys.build(producer.load_angle(a, kvh, id1, lane), parity, tid);
     }
-    const bool mine = computes && !masked_page && (parts < 8 || (part >> 2) == parity);
-    if (mine) {
+    if (computes && !masked_page && ((at - begin) & (phases - 1)) == phase) {
       const f16x8* const k_image = reinterpret_cast<const f16x8*>(image[parity][0]) + lane;
       const f16x8* const v_image = reinterpret_cast<const f16x8*>(image[parity][1]) + lane;
 #pragma unroll 1
@@ -806,155 +848,109 @@ __device__ __forceinline__ void shared_body(const ChunkAttentionArgs& a) {
         // nobody sees the step's tokens
         if (token0 > wave_last || (a.window > 0 && token0 >= a.n_sinks && token0 + 31 <= wave_first - a.window)) continue;
         const bool masks = token0 + 31 > wave_first || (a.window > 0 && token0 <= wave_last - a.window && token0 + 31 >= a.n_sinks);
-        f32x4 s[2][RT];
+        f32x4 s[2];
+        s[0] = s[1] = f32x4{off, off, off, off};
 #pragma unroll
-        for (int tile = 0; tile < 2; ++tile)
+        for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
-          for (int ks = 0; ks < 4; ++ks) {
-            const f16x8 k_op = k_image[((2 * step + tile) * 4 + ks) * 64];
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-              const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-              s[tile][rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k_op, q[rt][ks], ks == 0 ? zero : s[tile][rt], 0, 0, 0);
-            }
-          }
+          for (int tile = 0; tile < 2; ++tile) s[tile] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k_image[((2 * step + tile) * 4 + ks) * 64], q[ks], s[tile], 0, 0, 0);
         if (masks) {
 #pragma unroll
           for (int tile = 0; tile < 2; ++tile)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int token = token0 + 16 * tile + 4 * quarter + i;
-#pragma unroll
-              for (int rt = 0; rt < RT; ++rt) {
-                bool seen = token <= position[rt];
-                if (a.window > 0) seen = seen && (position[rt] - token < a.window || token < a.n_sinks);
-                if (!seen) s[tile][rt][i] = kNegInf;
-              }
+              bool seen = token <= position;
+              if (a.window > 0) seen = seen && (position - token < a.window || token < a.n_sinks);
+              if (!seen) s[tile][i] = kNegInf;
             }
         }
-        float top[RT];
-        bool above = false;
+        float top = max3(s[0][0], s[0][1], s[0][2]);
+        top = max3(top, s[0][3], s[1][0]);
+        top = max3(top, s[1][1], s[1][2]);
+        top = max2(top, s[1][3]);
+        if (__builtin_amdgcn_ballot_w64(top > limit) != 0) {
+          auto r = __builtin_amdgcn_permlane16_swap(f2u(top), f2u(top), false, false);
+          top = max2(u2f(r[0]), u2f(r[1]));
+          auto r2 = __builtin_amdgcn_permlane32_swap(f2u(top), f2u(top), false, false);
+          top = max2(u2f(r2[0]), u2f(r2[1]));
+          // the row's largest score goes to kLift, if it is above that or the row's first
+          const bool first = limit == kNegInf;
+          const float down = top > kNegInf && (first || top > kLift) ? kLift - top : 0.f;
+          if (top > kNegInf) limit = 15.f;
+          off += down;
+          const float keep = first ? 1.f : __builtin_amdgcn_exp2f(down);
+          sums *= keep;
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          float x = max3(s[0][rt][0], s[0][rt][1], s[0][rt][2]);
-          x = max3(x, s[0][rt][3], s[1][rt][0]);
-          x = max3(x, s[1][rt][1], s[1][rt][2]);
-          top[rt] = max2(x, s[1][rt][3]) * a.scale_log2;
-          above = above || top[rt] > m[rt] + kSlack;
+          for (int e = 0; e < 8; ++e) acc[e] *= keep;
+          s[0] += down;
+          s[1] += down;
         }
-        if (__builtin_amdgcn_ballot_w64(above) != 0) {
+        uint32_t w[4];
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt) {
-            float x = top[rt];
-            auto r = __builtin_amdgcn_permlane16_swap(f2u(x), f2u(x), false, false);
-            x = max2(u2f(r[0]), u2f(r[1]));
-            auto r2 = __builtin_amdgcn_permlane32_swap(f2u(x), f2u(x), false, false);
-            x = max3(u2f(r2[0]), u2f(r2[1]), m[rt]);
-            const float keep = x > kNegInf ? __builtin_amdgcn_exp2f(m[rt] - x) : 1.f;
-            m[rt] = x;
-            l[rt] *= keep;
+        for (int i = 0; i < 4; ++i)
+          w[i] = h2u(to_half2(__builtin_amdgcn_exp2f(s[i >> 1][2 * (i & 1)]), __builtin_amdgcn_exp2f(s[i >> 1][2 * (i & 1) + 1])));
+        const f16x8 p = as_operand(w[0], w[1], w[2], w[3]);
+        constexpr uint32_t kOnes = 0x3c003c00u;
+        sums = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_operand(kOnes, kOnes, kOnes, kOnes), p, sums, 0, 0, 0);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) acc[e][rt] *= keep;
-          }
-        }
-        f16x8 p_op[RT];
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          const float off = m[rt] > kNegInf ? kLift - m[rt] : 0.f;
-          uint32_t w[4];
-#pragma unroll
-          for (int tile = 0; tile < 2; ++tile)
-#pragma unroll
-            for (int pair = 0; pair < 2; ++pair) {
-              const f16x2 p = to_half2(__builtin_amdgcn_exp2f(fmaf(s[tile][rt][2 * pair], a.scale_log2, off)),
-                                       __builtin_amdgcn_exp2f(fmaf(s[tile][rt][2 * pair + 1], a.scale_log2, off)));
-              w[2 * tile + pair] = h2u(p);
-              l[rt] = __builtin_amdgcn_fdot2(p, f16x2{static_cast<_Float16>(1.f), static_cast<_Float16>(1.f)}, l[rt], false);
-            }
-          p_op[rt] = as_operand(w[0], w[1], w[2], w[3]);
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const f16x8 v_op = v_image[(step * 8 + e) * 64];
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt) acc[e][rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v_op, p_op[rt], acc[e][rt], 0, 0, 0);
-        }
+        for (int e = 0; e < 8; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v_image[(step * 8 + e) * 64], p, acc[e], 0, 0, 0);
       }
     }
     __syncthreads();
   }
 
   // ---- fold the parts of a row group ----
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) l[rt] = sum_rows(l[rt]);
+  float m = limit > kNegInf ? kLift - off : kNegInf, l = sums[0];
   if (parts > 1) {
     if (quarter == 0) {
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        fold_m[wave][16 * rt + col] = m[rt];
-        fold_l[wave][16 * rt + col] = l[rt];
-      }
+      fold_m[wave][col] = m;
+      fold_l[wave][col] = l;
     }
     __syncthreads();
+    float top = kNegInf, total = 0.f;
+    for (int p = 0; p < parts; ++p) top = fmaxf(top, fold_m[row_group + p * groups][col]);
+    for (int p = 0; p < parts; ++p) total += top > kNegInf ? fold_l[row_group + p * groups][col] * __builtin_amdgcn_exp2f(fold_m[row_group + p * groups][col] - top) : 0.f;
+    const float weight = top > kNegInf ? __builtin_amdgcn_exp2f(m - top) : 0.f;
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      float top = kNegInf, total = 0.f;
-      for (int p = 0; p < parts; ++p) top = fmaxf(top, fold_m[row_group + p * groups][16 * rt + col]);
-      for (int p = 0; p < parts; ++p)
-        total += top > kNegInf ? fold_l[row_group + p * groups][16 * rt + col] * __builtin_amdgcn_exp2f(fold_m[row_group + p * groups][16 * rt + col] - top) : 0.f;
-      const float weight = top > kNegInf ? __builtin_amdgcn_exp2f(m[rt] - top) : 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e][rt] *= weight;
-      m[rt] = top;
-      l[rt] = total;
-    }
-    f32x4* const room = reinterpret_cast<f32x4*>(&image[0][0][0]);           // 16 KB a wavefront
+    for (int e = 0; e < 8; ++e) acc[e] *= weight;
+    m = top;
+    l = total;
+    f32x4* const room = reinterpret_cast<f32x4*>(&image[0][0][0]);           // 8 KB a wavefront
     if (part > 0) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) room[(wave * 8 * RT + e * RT + rt) * 64 + lane] = acc[e][rt];
+      for (int e = 0; e < 8; ++e) room[(wave * 8 + e) * 64 + lane] = acc[e];
     }
     __syncthreads();
     if (part > 0) return;
     for (int p = 1; p < parts; ++p) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) acc[e][rt] += room[((row_group + p * groups) * 8 * RT + e * RT + rt) * 64 + lane];
+      for (int e = 0; e < 8; ++e) acc[e] += room[((row_group + p * groups) * 8 + e) * 64 + lane];
     }
   }
   if (!computes) return;
-  // lane: dims 32 quarter + 8 i + e of its rows
+  // lane: dims 32 quarter + 8 i + e of its row
   if (a.n_splits > 1) {
-    const int64_t slot = (static_cast<int64_t>(index) * a.n_kv_heads + kvh) * a.n_splits + split;
+    const int64_t slot_row = ((static_cast<int64_t>(index) * a.n_kv_heads + kvh) * a.n_splits + split) * kTileRows + row;
+    float* const to = a.ws_acc + slot_row * kHeadDim + 32 * quarter;
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const int64_t row = slot * kTileRows + row_group * kSharedRows + 16 * rt + col;
-      float* const to = a.ws_acc + row * kHeadDim + 32 * quarter;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        *reinterpret_cast<f32x4*>(to + 8 * i) = f32x4{acc[0][rt][i], acc[1][rt][i], acc[2][rt][i], acc[3][rt][i]};
-        *reinterpret_cast<f32x4*>(to + 8 * i + 4) = f32x4{acc[4][rt][i], acc[5][rt][i], acc[6][rt][i], acc[7][rt][i]};
-      }
-      if (quarter == 0) {
-        a.ws_ml[row * 2] = m[rt];
-        a.ws_ml[row * 2 + 1] = l[rt];
-      }
+    for (int i = 0; i < 4; ++i) {
+      *reinterpret_cast<f32x4*>(to + 8 * i) = f32x4{acc[0][i], acc[1][i], acc[2][i], acc[3][i]};
+      *reinterpret_cast<f32x4*>(to + 8 * i + 4) = f32x4{acc[4][i], acc[5][i], acc[6][i], acc[7][i]};
+    }
+    if (quarter == 0) {
+      a.ws_ml[slot_row * 2] = m;
+      a.ws_ml[slot_row * 2 + 1] = l;
     }
     return;
   }
+  if (!row_there) return;
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  __half* const to = a.out + row_at + 32 * quarter;
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const int row = row_group * kSharedRows + 16 * rt + col, token = row / a.group, head = row - token * a.group;
-    if (token >= item.count) continue;
-    const float inv = l[rt] > 0.f ? 1.f / l[rt] : 0.f;
-    __half* const to = a.out + ((item.row0 + item.first + token) * a.n_q_heads + kvh * a.group + head) * kHeadDim + 32 * quarter;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<u32x4*>(to + 8 * i) = u32x4{h2u(to_half2(acc[0][rt][i] * inv, acc[1][rt][i] * inv)), h2u(to_half2(acc[2][rt][i] * inv, acc[3][rt][i] * inv)),
-                                                    h2u(to_half2(acc[4][rt][i] * inv, acc[5][rt][i] * inv)), h2u(to_half2(acc[6][rt][i] * inv, acc[7][rt][i] * inv))};
-  }
+  for (int i = 0; i < 4; ++i)
+    *reinterpret_cast<u32x4*>(to + 8 * i) = u32x4{h2u(to_half2(acc[0][i] * inv, acc[1][i] * inv)), h2u(to_half2(acc[2][i] * inv, acc[3][i] * inv)),
+                                                  h2u(to_half2(acc[4][i] * inv, acc[5][i] * inv)), h2u(to_half2(acc[6][i] * inv, acc[7][i] * inv))};
 }
 
 }  // namespace chunk
