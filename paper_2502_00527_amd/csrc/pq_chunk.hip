@@ -8,6 +8,7 @@ namespace pq {
 namespace {
 
 constexpr int kJoinThreads = 256;
+constexpr int kMaxSplits = 64;                    // a lane each
 
 // out = sum over splits of 2^(m_c - M) acc_c / sum of 2^(m_c - M) l_c: a wavefront a row, two dims a lane.
 __global__ __launch_bounds__(kJoinThreads) void pq_chunk_join_kernel(const ChunkAttentionArgs a, int rows) {
@@ -17,35 +18,37 @@ __global__ __launch_bounds__(kJoinThreads) void pq_chunk_join_kernel(const Chunk
   if (!chunk::find_item(a, index, lane, item)) return;
   const int first_position = item.len - item.n + item.first;
   const int pages = chunk::visible_pages(a, first_position, first_position + item.count - 1).count();
-  const int per = whole_rounds((pages + a.n_splits - 1) / a.n_splits);
-  const int splits = max(1, per > 0 ? (pages + per - 1) / per : 1);
+  const int splits = max(1, (pages + a.pages_per_split - 1) / a.pages_per_split);
   const int64_t slot = (static_cast<int64_t>(index) * a.n_kv_heads + kvh) * a.n_splits;
   for (int row = uni(blockIdx.y * (kJoinThreads / 64) + (threadIdx.x >> 6)); row < rows; row += gridDim.y * (kJoinThreads / 64)) {
     const int token = row / a.group, head = row - token * a.group;
     if (token >= item.count) return;
-    float top = kNegInf;
-    for (int c = 0; c < splits; ++c) top = fmaxf(top, a.ws_ml[((slot + c) * rows + row) * 2]);
+    // a split a lane: its weight
+    const int64_t first = slot * rows + row;
+    const f32x2 ml = lane < splits ? reinterpret_cast<const f32x2*>(a.ws_ml)[first + static_cast<int64_t>(lane) * rows] : f32x2{kNegInf, 0.f};
+    float top = ml.x;
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    const float weight = top > kNegInf ? __builtin_amdgcn_exp2f(ml.x - top) : 0.f;
+    float l = weight * ml.y;
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) l += __shfl_xor(l, d);
     f32x2 sum = {0.f, 0.f};
-    float l = 0.f;
-    if (top > kNegInf) {
-#pragma unroll 4
-      for (int c = 0; c < splits; ++c) {
-        const int64_t at = (slot + c) * rows + row;
-        const float weight = __builtin_amdgcn_exp2f(a.ws_ml[at * 2] - top);
-        const f32x2 v = reinterpret_cast<const f32x2*>(a.ws_acc + at * kHeadDim)[lane];
-        sum.x = fmaf(weight, v.x, sum.x);
-        sum.y = fmaf(weight, v.y, sum.y);
-        l = fmaf(weight, a.ws_ml[at * 2 + 1], l);
-      }
+#pragma unroll 8
+    for (int c = 0; c < splits; ++c) {
+      const float w = u2f(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(f2u(weight)), c)));
+      const f32x2 v = reinterpret_cast<const f32x2*>(a.ws_acc + (first + static_cast<int64_t>(c) * rows) * kHeadDim)[lane];
+      sum.x = fmaf(w, v.x, sum.x);
+      sum.y = fmaf(w, v.y, sum.y);
     }
     const float inv = l > 0.f ? 1.f / l : 0.f;
     reinterpret_cast<uint32_t*>(a.out + ((item.row0 + item.first + token) * a.n_q_heads + kvh * a.group + head) * kHeadDim)[lane] = h2u(to_half2(sum.x * inv, sum.y * inv));
   }
 }
 
-// How a launch is shared out: items of 16 rows_of_16 query rows of a KV head, each one's pages in n_splits parts.
+// How a launch is shared out: items of 16 rows_of_16 query rows of a KV head, each one's pages in up to n_splits parts.
 struct ChunkLaunch {
-  int rows_of_16, tile_tokens, n_splits;
+  int rows_of_16, tile_tokens, n_splits, pages_per_split;
   int64_t n_items;
   size_t acc_bytes, bytes;     // of the workspace
 };
@@ -55,12 +58,33 @@ size_t round256(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
 ChunkLaunch plan_launch(const pq_layout* l, int32_t n_seqs, int32_t n_q_heads, int64_t n_tokens, int64_t max_pages) {
   ChunkLaunch p;
   const int64_t group = n_q_heads / l->n_kv_heads;
-  p.rows_of_16 = n_tokens * group <= 24 * static_cast<int64_t>(n_seqs) ? 1 : chunk::kTileRows / 16;
+  const int64_t rows_16 = (n_tokens * group + 16 * static_cast<int64_t>(n_seqs) - 1) / (16 * static_cast<int64_t>(n_seqs));   // of a sequence, in the mean
+  p.rows_of_16 = rows_16 <= 2 ? static_cast<int>(std::max<int64_t>(1, rows_16)) : chunk::kTileRows / 16;
   p.tile_tokens = static_cast<int>(16 * p.rows_of_16 / group);
   p.n_items = std::min<int64_t>(n_tokens, n_tokens / p.tile_tokens + n_seqs);
-  const int64_t units = std::max<int64_t>(1, p.n_items * l->n_kv_heads), resident = p.rows_of_16 == 1 ? 2 * kComputeUnits : kComputeUnits;
-  p.n_splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(64, std::min((resident + units - 1) / units, (max_pages + kWaveRound - 1) / kWaveRound))));
-  const size_t rows = p.n_splits > 1 ? static_cast<size_t>(units) * p.n_splits * 16 * p.rows_of_16 : 0;
+  // splits for what the items come to if chunks are alike
+  const int64_t of_seq = (n_tokens + n_seqs - 1) / n_seqs, units = n_seqs * ((of_seq + p.tile_tokens - 1) / p.tile_tokens) * l->n_kv_heads;
+  const int64_t pages = std::max<int64_t>(max_pages, 1);
+  int64_t splits = 1;
+  if (p.rows_of_16 <= 2) {
+    splits = std::min((3 * kComputeUnits + units - 1) / units, (pages + 1) / 2);
+  } else {
+    // A compute unit has one work-group: rounds of them, in pages of time.  Starting and ending a work-group takes as long as three
+    // pages, writing and joining the parts of 256 work-groups as 3.3
+    double best = 0.;
+    for (int64_t k = 1; k <= std::min<int64_t>(kMaxSplits, (pages + kWaveRound - 1) / kWaveRound); ++k) {
+      const double rounds = static_cast<double>((units * k + kComputeUnits - 1) / kComputeUnits);
+      const double cost = rounds * (static_cast<double>((pages + k - 1) / k) + 3.) + (k > 1 ? 2. + 3.3 * static_cast<double>(units * k) / kComputeUnits : 0.);
+      if (k == 1 || cost < best) {
+        best = cost;
+        splits = k;
+      }
+    }
+  }
+  splits = std::max<int64_t>(1, std::min<int64_t>(splits, kMaxSplits));
+  p.pages_per_split = static_cast<int>((pages + splits - 1) / splits);
+  p.n_splits = static_cast<int>((pages + p.pages_per_split - 1) / p.pages_per_split);
+  const size_t rows = p.n_splits > 1 ? static_cast<size_t>(p.n_items) * l->n_kv_heads * p.n_splits * 16 * p.rows_of_16 : 0;
   p.acc_bytes = round256(rows * kHeadDim * sizeof(float));
   p.bytes = std::max<size_t>(256, p.acc_bytes + round256(rows * 2 * sizeof(float)));
   return p;
@@ -143,6 +167,7 @@ extern "C" int pq_chunk_attention(const pq_layout* layout, const void* q, pq_dty
   a.tile_tokens = p.tile_tokens;
   a.n_items = static_cast<int32_t>(p.n_items);
   a.n_splits = p.n_splits;
+  a.pages_per_split = p.pages_per_split;
   a.table_index = key_table_index(layout);
   // (above zero, so that masked scores stay -inf whatever the scale is)
   a.scale_log2 = std::max(static_cast<float>(std::fabs(static_cast<double>(sm_scale)) * 1.4426950408889634074), 1.17549435e-38f);
