@@ -389,7 +389,8 @@ size_t pq_chunk_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_t
  *                 scratch.  Calls that overlap need one each, captured ones too
  *
  * Softmax statistics and sums are fp32.  Reconstructed keys, probabilities and de-quantized values enter the matrix products as
- * fp16, each rounded once (keys of the uniform grid from two products).  Keys, and values of all tokens of a page that is seen, must be finite.
+ * fp16, each rounded once; keys (made in fp32; the levels of the grouped quantizer are fp16 too) with the scale in them, times sm_scale
+ * log2(e): that product has to lie in fp16's range.  Keys, and values of all tokens of a page that is seen, must be finite.
  * n_tokens == 0 is a no-op.
  */
 int pq_chunk_attention(const pq_layout* layout, const void* q, pq_dtype q_dtype, int64_t n_tokens, int32_t n_seqs,

@@ -53,6 +53,11 @@ struct ChunkLaunch {
   size_t acc_bytes, bytes;     // of the workspace
 };
 
+// Threads of a grid dimension: HIP takes 2^32 - 1.
+bool launch_fits(const pq_layout* l, const ChunkLaunch& p) {
+  return p.n_items * l->n_kv_heads < (int64_t{1} << 32) / (p.rows_of_16 <= 2 ? 256 : 1024);
+}
+
 size_t round256(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
 
 ChunkLaunch plan_launch(const pq_layout* l, int32_t n_seqs, int32_t n_q_heads, int64_t n_tokens, int64_t max_pages) {
@@ -65,14 +70,19 @@ ChunkLaunch plan_launch(const pq_layout* l, int32_t n_seqs, int32_t n_q_heads, i
   // splits for what the items come to if chunks are alike
   const int64_t of_seq = (n_tokens + n_seqs - 1) / n_seqs, units = n_seqs * ((of_seq + p.tile_tokens - 1) / p.tile_tokens) * l->n_kv_heads;
   const int64_t pages = std::max<int64_t>(max_pages, 1);
-  int64_t splits = 1;
-  if (p.rows_of_16 <= 2) {
-    splits = std::min((3 * kComputeUnits + units - 1) / units, (pages + 1) / 2);
-  } else {
+  // At most this many splits, a number that only grows with the pages: the workspace has room for it, whatever a window leaves of them.
+  // (The number taken is no such bound: 10 splits of 21 pages come to 7 of 3, of 20 pages to 10 of 2.)  Eight rounds of work-groups
+  // need 270 MB.
+  int64_t most;
+  if (p.rows_of_16 <= 2) most = std::min((3 * kComputeUnits + units - 1) / units, (pages + 1) / 2);
+  else most = std::min(8 * kComputeUnits / units, (pages + kWaveRound - 1) / kWaveRound);
+  most = std::max<int64_t>(1, std::min<int64_t>(most, kMaxSplits));
+  int64_t splits = most;
+  if (p.rows_of_16 > 2) {
     // A compute unit has one work-group: rounds of them, in pages of time.  Starting and ending a work-group takes as long as three
     // pages, writing and joining the parts of 256 work-groups as 3.3
     double best = 0.;
-    for (int64_t k = 1; k <= std::min<int64_t>(kMaxSplits, (pages + kWaveRound - 1) / kWaveRound); ++k) {
+    for (int64_t k = 1; k <= most; ++k) {
       const double rounds = static_cast<double>((units * k + kComputeUnits - 1) / kComputeUnits);
       const double cost = rounds * (static_cast<double>((pages + k - 1) / k) + 3.) + (k > 1 ? 2. + 3.3 * static_cast<double>(units * k) / kComputeUnits : 0.);
       if (k == 1 || cost < best) {
@@ -81,10 +91,9 @@ ChunkLaunch plan_launch(const pq_layout* l, int32_t n_seqs, int32_t n_q_heads, i
       }
     }
   }
-  splits = std::max<int64_t>(1, std::min<int64_t>(splits, kMaxSplits));
   p.pages_per_split = static_cast<int>((pages + splits - 1) / splits);
   p.n_splits = static_cast<int>((pages + p.pages_per_split - 1) / p.pages_per_split);
-  const size_t rows = p.n_splits > 1 ? static_cast<size_t>(p.n_items) * l->n_kv_heads * p.n_splits * 16 * p.rows_of_16 : 0;
+  const size_t rows = most > 1 ? static_cast<size_t>(p.n_items) * l->n_kv_heads * most * 16 * p.rows_of_16 : 0;
   p.acc_bytes = round256(rows * kHeadDim * sizeof(float));
   p.bytes = std::max<size_t>(256, p.acc_bytes + round256(rows * 2 * sizeof(float)));
   return p;
@@ -95,7 +104,7 @@ int check_chunk_shape(const pq_layout* l, int32_t n_seqs, int32_t n_q_heads, int
   if (l->n_kv_heads <= 0 || n_q_heads % l->n_kv_heads != 0) return PQ_ERR_INVALID_ARG;
   if (!layout_supported(l)) return PQ_ERR_UNSUPPORTED;
   if (n_q_heads / l->n_kv_heads > 16) return PQ_ERR_UNSUPPORTED;
-  // one grid dimension of at most 2^24 work-groups of 256 threads
+  // (launch_fits() has the last word)
   if (n_seqs > (1 << 20) || n_tokens >= (int64_t{1} << 31) || (n_tokens + n_seqs) * l->n_kv_heads >= (int64_t{1} << 24)) return PQ_ERR_UNSUPPORTED;
   return PQ_OK;
 }
@@ -107,7 +116,8 @@ using namespace pq;
 
 extern "C" size_t pq_chunk_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_t n_q_heads, int64_t n_tokens, int32_t max_seq_len) {
   if (check_chunk_shape(layout, n_seqs, n_q_heads, n_tokens, max_seq_len) != PQ_OK) return 0;
-  return plan_launch(layout, n_seqs, n_q_heads, n_tokens, (static_cast<int64_t>(max_seq_len) + kGroup - 1) / kGroup).bytes;
+  const ChunkLaunch p = plan_launch(layout, n_seqs, n_q_heads, n_tokens, (static_cast<int64_t>(max_seq_len) + kGroup - 1) / kGroup);
+  return launch_fits(layout, p) ? p.bytes : 0;
 }
 
 extern "C" int pq_chunk_attention(const pq_layout* layout, const void* q, pq_dtype q_dtype, int64_t n_tokens, int32_t n_seqs,
@@ -136,6 +146,7 @@ extern "C" int pq_chunk_attention(const pq_layout* layout, const void* q, pq_dty
   if (window >= max_seq_len) window = 0;
   n_sinks = window > 0 ? std::min(n_sinks, max_seq_len) : 0;
   const ChunkLaunch most = plan_launch(layout, n_seqs, n_q_heads, n_tokens, seq_pages);
+  if (!launch_fits(layout, most)) return PQ_ERR_UNSUPPORTED;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < most.bytes) return PQ_ERR_WORKSPACE;
   int64_t pages = seq_pages;
   if (window > 0) pages = std::min<int64_t>(pages, (static_cast<int64_t>(n_sinks) + kGroup - 1) / kGroup + (static_cast<int64_t>(window) + most.tile_tokens) / kGroup + 2);

@@ -12,10 +12,11 @@
 // 16 pairs, four pairs (x, y) an instruction -- and values as whole rows, lane (slice of 8 dims l % 16, tokens 4 (l / 16) .. + 3 of
 // both tiles): dim e of every slice is one instruction.
 //
-// Rounding.  Queries are fp16; reconstructed keys, probabilities and de-quantized values are rounded to fp16 for the
-// matrix unit, like the output: each 2^-12 of itself in the mean, where the cache's own quantization is 2^-4.  Sums, m and l are
-// fp32.  Probabilities are taken times 2^kLift, so that weights down to 2^-21 of the largest keep all their bits.
-// m is raised only when a score is 2^(15 - kLift) above it (the product then still fits fp16), and then by all lanes of the row.
+// Rounding.  Queries are fp16; reconstructed keys (made in fp32, the softmax's scale in them), probabilities and de-quantized values
+// are rounded to fp16 for the matrix unit, like the output: each 2^-12 of itself in the mean, where the cache's own quantization is
+// 2^-4.  Sums, m and l are fp32.  The score product starts from kLift - m, so that what comes out is the exponent of a weight times
+// 2^kLift: weights down to 2^-21 of the largest keep all their bits, and m is raised only when a score is 2^(15 - kLift) above it (the
+// weight then still fits fp16), and then by all lanes of the row.
 #pragma once
 #include "pq_decode_matrix.hpp"
 
