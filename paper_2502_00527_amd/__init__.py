@@ -411,6 +411,14 @@ def pq_score_keys(layout: Layout, q, codes_pool, params_pool, block_table, seq_l
     _check(st, "pq_score_keys")
 
 
+def _on_current_device(**tensors) -> None:
+    """Calls go to the current stream of the current device, where all of a call's tensors have to be."""
+    import torch
+    for name, t in tensors.items():
+        if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != torch.cuda.current_device():
+            raise PolarQuantError(f"{name} is on {t.device}, not on the current device (cuda:{torch.cuda.current_device()})")
+
+
 def pq_plan_pages(layout: Layout, seq_lens, new_lens, free_pages, block_table, starts, slots, lens_after, counts) -> None:
     """Pages and slots of a batch's new tokens; see include/polarquant.h.  seq_lens, new_lens, lens_after int32 [n_seqs], starts
     int32 [n_seqs + 1], counts int32 [2], free_pages int32 [n_free], block_table int32 [n_seqs, width], slots int64 [bound of the
@@ -420,6 +428,8 @@ def pq_plan_pages(layout: Layout, seq_lens, new_lens, free_pages, block_table, s
         return
     import torch
     i32 = (torch.int32,)
+    _on_current_device(seq_lens=seq_lens, new_lens=new_lens, free_pages=free_pages, block_table=block_table, starts=starts, slots=slots,
+                       lens_after=lens_after, counts=counts)
     n = seq_lens.numel()
     if new_lens.numel() != n or lens_after.numel() != n or starts.numel() != n + 1 or counts.numel() < 2:
         raise PolarQuantError("new_lens and lens_after must be [n_seqs], starts [n_seqs + 1], counts [2]")
@@ -457,6 +467,8 @@ def pq_append_chunk(layout: Layout, keys, values, starts, seq_lens, slots, resid
             "pq_append_chunk"):
         return
     import torch
+    _on_current_device(keys=keys, values=values, starts=starts, seq_lens=seq_lens, slots=slots, residual=residual, block_table=block_table,
+                       codes_pool=codes_pool, params_pool=params_pool, v_pool=v_pool, v_params=v_params)
     _rows(keys, layout, "keys", (torch.float16, torch.float32))
     n = _per_sequence(starts, seq_lens, block_table)
     n_pool_pages = _key_pool_pages(layout, codes_pool, params_pool)
@@ -465,7 +477,7 @@ def pq_append_chunk(layout: Layout, keys, values, starts, seq_lens, slots, resid
     v_ptr = vp_ptr = slot_ptr = None
     if values is not None:
         _rows(values, layout, "values", (torch.float16,))
-        if values.shape[0] != keys.shape[0] or slots.numel() != keys.shape[0]:
+        if slots is None or values.shape[0] != keys.shape[0] or slots.numel() != keys.shape[0]:
             raise PolarQuantError("values and slots must have as many rows as keys")
         v_args = (values.data_ptr(), values.stride(0), values.stride(1))
         slot_ptr = _dev_ptr(slots, "slots", (torch.int64,))
@@ -500,6 +512,8 @@ def pq_chunk_attention(layout: Layout, q, starts, codes_pool, params_pool, v_poo
             v_bits, v_params, window, n_sinks), "pq_chunk_attention"):
         return
     import torch
+    _on_current_device(q=q, starts=starts, codes_pool=codes_pool, params_pool=params_pool, v_pool=v_pool, block_table=block_table, seq_lens=seq_lens,
+                       out=out, workspace=workspace, residual=residual, v_params=v_params)
     n = _per_sequence(starts, seq_lens, block_table)
     c = _decode_common(layout, q, codes_pool, params_pool, v_pool, block_table, seq_lens, v_bits, v_params)
     if out.shape != q.shape:
@@ -527,6 +541,8 @@ def pq_window_attention(layout: Layout, q, codes_pool, params_pool, v_pool, bloc
             residual, v_bits, v_params), "pq_window_attention"):
         return
     import torch
+    _on_current_device(q=q, codes_pool=codes_pool, params_pool=params_pool, v_pool=v_pool, block_table=block_table, seq_lens=seq_lens, out=out,
+                       workspace=workspace, residual=residual, v_params=v_params)
     c = _decode_common(layout, q, codes_pool, params_pool, v_pool, block_table, seq_lens, v_bits, v_params)
     if block_table.dim() != 2 or block_table.shape[0] != c["n_seqs"] or seq_lens.numel() != c["n_seqs"] or out.shape != q.shape:
         raise PolarQuantError("block_table must be [n_seqs, pages], seq_lens [n_seqs], out of q's shape")

@@ -70,12 +70,13 @@ int32_t integer32(int64_t v) {
   return static_cast<int32_t>(v);
 }
 
-// torch's current stream on its current device, as a hipStream_t
+// torch's current stream on its current device, as a hipStream_t; the device's number, too
 PyObject *get_device = nullptr, *get_raw_stream = nullptr;
-void* current_stream() {
+void* current_stream(long* number = nullptr) {
   if (!get_device || !get_raw_stream) throw Decline{};
   PyObject* const device = PyObject_CallNoArgs(get_device);
   if (!device) throw Decline{};
+  if (number) *number = PyLong_AsLong(device);
   PyObject* const stream = PyObject_CallOneArg(get_raw_stream, device);
   Py_DECREF(device);
   if (!stream) throw Decline{};
@@ -83,6 +84,14 @@ void* current_stream() {
   Py_DECREF(stream);
   if (!p && PyErr_Occurred()) throw Decline{};
   return p;
+}
+// The same, if that is the device of all the tensors.
+template <typename... Tensors>
+void* stream_of(const Tensors&... tensors) {
+  long device = -1;
+  void* const stream = current_stream(&device);
+  if (!((tensors.device().index() == device) && ...)) throw Decline{};
+  return stream;
 }
 int64_t pages(size_t bytes, size_t page) { return static_cast<int64_t>(bytes / (page > 0 ? page : 1)); }
 
@@ -250,17 +259,23 @@ int32_t sequences(const at::Tensor& starts, const at::Tensor& lens, const at::Te
   if (starts.numel() != lens.numel() + 1 || table.dim() != 2 || table.size(0) != lens.numel()) throw Decline{};
   return integer32(lens.numel());
 }
-void* residual_of(PyObject* o, const pq_layout* l, int32_t n_seqs) {
+void* residual_of(PyObject* o, const pq_layout* l, int32_t n_seqs, const at::Tensor& beside) {
   const at::Tensor& t = contiguous_tensor(o, at::kHalf);
-  if (t.numel() < static_cast<int64_t>(n_seqs) * l->n_kv_heads * l->group_tokens * l->head_dim) throw Decline{};
+  if (t.device() != beside.device() || t.numel() < static_cast<int64_t>(n_seqs) * l->n_kv_heads * l->group_tokens * l->head_dim) throw Decline{};
   return t.data_ptr();
 }
 // The value pool and its parameters, which hold at least n_pages pages.
 struct ValuePool {
+  const at::Tensor& tensor;
   void *pool, *params = nullptr;
-  ValuePool(const pq_layout* l, PyObject* v_pool, PyObject* v_params, int32_t v_bits, int64_t n_pages) {
-    const at::Tensor& v = contiguous_tensor(v_pool, v_bits == 16 ? at::kHalf : at::kByte);
-    if (v_bits != 16) params = contiguous_tensor(v_params, at::kHalf).data_ptr();
+  ValuePool(const pq_layout* l, PyObject* v_pool, PyObject* v_params, int32_t v_bits, int64_t n_pages)
+      : tensor(contiguous_tensor(v_pool, v_bits == 16 ? at::kHalf : at::kByte)) {
+    const at::Tensor& v = tensor;
+    if (v_bits != 16) {
+      const at::Tensor& p = contiguous_tensor(v_params, at::kHalf);
+      if (p.device() != v.device()) throw Decline{};
+      params = p.data_ptr();
+    }
     if (pages(bytes_of(v), v_bits == 16 ? pq_values_bytes_per_page(l) : pq_vq_bytes_per_page(l, v_bits)) < n_pages) throw Decline{};
     pool = v.data_ptr();
   }
@@ -281,7 +296,7 @@ PyObject* plan_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int32_t *const lp = ints(lens), *const np = ints(fresh), *const fp = ints(free_pages), *const tp = ints(table), *const sp = ints(starts),
             *const ap = ints(after), *const cp = ints(counts);
     int64_t* const slot = static_cast<int64_t*>(slots.data_ptr());
-    void* const stream = current_stream();
+    void* const stream = stream_of(lens, fresh, free_pages, table, starts, slots, after, counts);
     return without_lock([&] { return pq_plan_pages(l, lp, np, n_seqs, fp, n_free, tp, width, sp, slot, most, ap, cp, stream); });
   });
 }
@@ -296,7 +311,7 @@ PyObject* append_chunk(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const pq_dtype kind = float_kind(keys);
     const at::Tensor &starts = contiguous_tensor(a[3], at::kInt), &lens = contiguous_tensor(a[4], at::kInt), &table = contiguous_tensor(a[7], at::kInt);
     const int32_t n_seqs = sequences(starts, lens, table), width = integer32(table.size(1)), v_bits = integer32(integer(a[11]));
-    void* const residual = residual_of(a[6], l, n_seqs);
+    void* const residual = residual_of(a[6], l, n_seqs, keys);
     const at::Tensor &codes = contiguous_tensor(a[8]), &params = contiguous_tensor(a[9]);
     const int64_t n_pages = key_pool_pages(l, codes, params), tokens = keys.size(0), key_token = keys.stride(0), key_head = keys.stride(1);
     void *vp = nullptr, *pool = nullptr, *pool_params = nullptr;
@@ -307,6 +322,7 @@ PyObject* append_chunk(PyObject*, PyObject* const* a, Py_ssize_t n) {
       const at::Tensor& slots = contiguous_tensor(a[5], at::kLong);
       if (values.scalar_type() != at::kHalf || values.stride(2) != 1 || values.size(0) != tokens || slots.numel() != tokens) throw Decline{};
       const ValuePool v(l, a[10], a[12], v_bits, n_pages);
+      stream_of(values, slots, v.tensor);
       vp = values.data_ptr();
       v_token = values.stride(0);
       v_head = values.stride(1);
@@ -314,7 +330,8 @@ PyObject* append_chunk(PyObject*, PyObject* const* a, Py_ssize_t n) {
       pool = v.pool;
       pool_params = v.params;
     }
-    void *const kp = keys.data_ptr(), *const cp = codes.data_ptr(), *const pp = params.data_ptr(), *const stream = current_stream();
+    void *const kp = keys.data_ptr(), *const cp = codes.data_ptr(), *const pp = params.data_ptr(),
+         *const stream = stream_of(keys, starts, lens, table, codes, params);
     const int32_t *const sp = ints(starts), *const lp = ints(lens), *const tp = ints(table);
     return without_lock([&] {
       return pq_append_chunk(l, kp, kind, key_token, key_head, vp, v_token, v_head, tokens, n_seqs, sp, lp, slot, residual, tp, width, cp, pp, pool,
@@ -342,9 +359,9 @@ PyObject* chunk_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const float sm_scale = static_cast<float>(PyFloat_AS_DOUBLE(a[9]));
     const at::Tensor &out = contiguous_tensor(a[10], at::kHalf), &workspace = contiguous_tensor(a[11]);
     if (out.sizes() != q.sizes()) throw Decline{};
-    void* const residual = a[12] == Py_None ? nullptr : residual_of(a[12], l, n_seqs);
+    void* const residual = a[12] == Py_None ? nullptr : residual_of(a[12], l, n_seqs, q);
     void *const qp = q.data_ptr(), *const cp = codes.data_ptr(), *const pp = params.data_ptr(), *const op = out.data_ptr(), *const ws = workspace.data_ptr(),
-         *const stream = current_stream();
+         *const stream = stream_of(q, codes, params, v.tensor, starts, table, lens, out, workspace);
     const int32_t *const sp = ints(starts), *const tp = ints(table), *const lp = ints(lens);
     const size_t ws_bytes = bytes_of(workspace);
     return without_lock([&] {
@@ -373,8 +390,9 @@ PyObject* window_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const float sm_scale = static_cast<float>(PyFloat_AS_DOUBLE(a[10]));
     const at::Tensor &out = contiguous_tensor(a[11], at::kFloat), &workspace = contiguous_tensor(a[12]);
     if (out.sizes() != q.sizes()) throw Decline{};
-    void* const residual = a[13] == Py_None ? nullptr : residual_of(a[13], l, n_seqs);
-    void *const qp = q.data_ptr(), *const cp = codes.data_ptr(), *const pp = params.data_ptr(), *const ws = workspace.data_ptr(), *const stream = current_stream();
+    void* const residual = a[13] == Py_None ? nullptr : residual_of(a[13], l, n_seqs, q);
+    void *const qp = q.data_ptr(), *const cp = codes.data_ptr(), *const pp = params.data_ptr(), *const ws = workspace.data_ptr(),
+         *const stream = stream_of(q, codes, params, v.tensor, table, lens, out, workspace);
     float* const op = static_cast<float*>(out.data_ptr());
     const int32_t *const tp = ints(table), *const lp = ints(lens);
     const size_t ws_bytes = bytes_of(workspace);
