@@ -1,5 +1,5 @@
 // Host side of pq_chunk_attention: checks, how a launch is shared out, and the kernel that joins the parts of rows whose pages
-// were split.  The attention kernels are in pq_chunk_kernels.hpp.
+// were cut into parts.  The attention kernels are in pq_chunk_kernels.hpp.
 #include <algorithm>
 
 #include "pq_chunk_kernels.hpp"
@@ -7,95 +7,116 @@
 namespace pq {
 namespace {
 
-constexpr int kJoinThreads = 256;
-constexpr int kMaxSplits = 64;                    // a lane each
+constexpr int kJoinRows = 16;                     // of a work-group, 16 lanes each
 
-// out = sum over splits of 2^(m_c - M) acc_c / sum of 2^(m_c - M) l_c: a wavefront a row, two dims a lane.
-__global__ __launch_bounds__(kJoinThreads) void pq_chunk_join_kernel(const ChunkAttentionArgs a, int rows) {
-  const int lane = threadIdx.x & 63;
-  const int kvh = blockIdx.x % a.n_kv_heads, index = blockIdx.x / a.n_kv_heads;
-  chunk::Item item;
-  if (!chunk::find_item(a, index, lane, item)) return;
-  const int first_position = item.len - item.n + item.first;
-  const int pages = chunk::visible_pages(a, first_position, first_position + item.count - 1).count();
-  const int splits = max(1, (pages + a.pages_per_split - 1) / a.pages_per_split);
-  const int64_t slot = (static_cast<int64_t>(index) * a.n_kv_heads + kvh) * a.n_splits;
-  for (int row = uni(blockIdx.y * (kJoinThreads / 64) + (threadIdx.x >> 6)); row < rows; row += gridDim.y * (kJoinThreads / 64)) {
-    const int token = row / a.group, head = row - token * a.group;
-    if (token >= item.count) return;
-    // a split a lane: its weight
-    const int64_t first = slot * rows + row;
-    const f32x2 ml = lane < splits ? reinterpret_cast<const f32x2*>(a.ws_ml)[first + static_cast<int64_t>(lane) * rows] : f32x2{kNegInf, 0.f};
-    float top = ml.x;
+// out = sum over parts of 2^(m_c - M) acc_c / sum of 2^(m_c - M) l_c, eight dims a lane.
+__global__ __launch_bounds__(16 * kJoinRows) void pq_chunk_join_kernel(const ChunkAttentionArgs a, int rows) {
+  const int kvh = blockIdx.x % a.n_kv_heads, unit = blockIdx.x / a.n_kv_heads;
+  const chunk::i32x4 noted = *reinterpret_cast<const chunk::i32x4*>(a.ws_units + static_cast<int64_t>(unit) * 4);
+  const int row0 = uni(noted.x), count = uni(noted.y), parts = uni(noted.z);
+  const int row = blockIdx.y * kJoinRows + (threadIdx.x >> 4), slice = threadIdx.x & 15;
+  const int token = row / a.group, head = row - token * a.group;
+  if (parts == 0 || token >= count) return;
+  const int64_t stride = static_cast<int64_t>(a.n_kv_heads) * rows, first = (static_cast<int64_t>(unit) * a.n_kv_heads + kvh) * rows + row;
+  const f32x2* const ml = reinterpret_cast<const f32x2*>(a.ws_ml) + first;
+  const f32x4* const acc = reinterpret_cast<const f32x4*>(a.ws_acc + first * kHeadDim) + 2 * slice;
+  // the weights: parts `slice`, slice + 16, ..
+  float m[chunk::kMaxParts / 16], w[chunk::kMaxParts / 16], top = kNegInf, l = 0.f;
 #pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    const float weight = top > kNegInf ? __builtin_amdgcn_exp2f(ml.x - top) : 0.f;
-    float l = weight * ml.y;
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) l += __shfl_xor(l, d);
-    f32x2 sum = {0.f, 0.f};
-#pragma unroll 8
-    for (int c = 0; c < splits; ++c) {
-      const float w = u2f(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(f2u(weight)), c)));
-      const f32x2 v = reinterpret_cast<const f32x2*>(a.ws_acc + (first + static_cast<int64_t>(c) * rows) * kHeadDim)[lane];
-      sum.x = fmaf(w, v.x, sum.x);
-      sum.y = fmaf(w, v.y, sum.y);
-    }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    reinterpret_cast<uint32_t*>(a.out + ((item.row0 + item.first + token) * a.n_q_heads + kvh * a.group + head) * kHeadDim)[lane] = h2u(to_half2(sum.x * inv, sum.y * inv));
+  for (int i = 0; i < chunk::kMaxParts / 16; ++i) {
+    const f32x2 part = slice + 16 * i < parts ? ml[(slice + 16 * i) * stride] : f32x2{kNegInf, 0.f};
+    m[i] = part.x;
+    w[i] = part.y;
+    top = fmaxf(top, m[i]);
   }
+#pragma unroll
+  for (int d = 8; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+#pragma unroll
+  for (int i = 0; i < chunk::kMaxParts / 16; ++i) {
+    m[i] = top > kNegInf ? __builtin_amdgcn_exp2f(m[i] - top) : 0.f;
+    l = fmaf(m[i], w[i], l);
+  }
+#pragma unroll
+  for (int d = 8; d >= 1; d >>= 1) l += __shfl_xor(l, d);
+  f32x4 sum[2] = {};
+#pragma unroll
+  for (int i = 0; i < chunk::kMaxParts / 16; ++i)
+    for (int c0 = 16 * i; c0 < min(parts, 16 * i + 16); c0 += 4) {
+#pragma unroll
+      for (int c = c0; c < c0 + 4; ++c) {          // (past the last part: weight 0, and the last one's row)
+        const float weight = __shfl(m[i], (threadIdx.x & 48) | (c & 15));
+        const f32x4 *const v = acc + min(c, parts - 1) * stride * (kHeadDim / 4), v0 = v[0], v1 = v[1];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          sum[0][k] = fmaf(weight, v0[k], sum[0][k]);
+          sum[1][k] = fmaf(weight, v1[k], sum[1][k]);
+        }
+      }
+    }
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  u32x4 out;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) out[i] = h2u(to_half2(sum[i >> 1][2 * (i & 1)] * inv, sum[i >> 1][2 * (i & 1) + 1] * inv));
+  reinterpret_cast<u32x4*>(a.out + ((static_cast<int64_t>(row0) + token) * a.n_q_heads + kvh * a.group + head) * kHeadDim)[slice] = out;
 }
 
-// How a launch is shared out: items of 16 rows_of_16 query rows of a KV head, each one's pages in up to n_splits parts.
+// A launch: items of 16 rows_of_16 query rows of a KV head; the kernels cut the pages that they see into parts, if `cuts`.
+//
+// Up to 32 rows a sequence (in the mean) are the few-rows kernel's, which makes its operands for 16 or 32 rows itself; more are the
+// shared one's, which unpacks a page once for 256.  16 sequences of 4000 tokens, 4 query heads per KV head, microseconds: 8 new tokens each
+// (32 rows) 44, 16 (64 rows) 55, 64 103 -- a page costs the few-rows kernel twice as much for 32 rows as for 16 and would
+// cost it again for each 32 more.
 struct ChunkLaunch {
-  int rows_of_16, tile_tokens, n_splits, pages_per_split;
-  int64_t n_items;
-  size_t acc_bytes, bytes;     // of the workspace
+  int rows_of_16, tile_tokens, cuts, parts;
+  int64_t n_items, n_units;    // of a KV head
+  size_t acc_bytes, ml_bytes, bytes;   // of the workspace
 };
 
 // Threads of a grid dimension: HIP takes 2^32 - 1.
 bool launch_fits(const pq_layout* l, const ChunkLaunch& p) {
-  return p.n_items * l->n_kv_heads < (int64_t{1} << 32) / (p.rows_of_16 <= 2 ? 256 : 1024);
+  return p.n_units * l->n_kv_heads < (int64_t{1} << 32) / (p.rows_of_16 <= 2 ? 256 : 1024);
 }
 
 size_t round256(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
 
-ChunkLaunch plan_launch(const pq_layout* l, int32_t n_seqs, int32_t n_q_heads, int64_t n_tokens, int64_t max_pages) {
+ChunkLaunch plan_launch(const pq_layout* l, int32_t n_seqs, int32_t n_q_heads, int64_t n_tokens, int64_t max_pages, bool windowed) {
   ChunkLaunch p;
   const int64_t group = n_q_heads / l->n_kv_heads;
   const int64_t rows_16 = (n_tokens * group + 16 * static_cast<int64_t>(n_seqs) - 1) / (16 * static_cast<int64_t>(n_seqs));   // of a sequence, in the mean
   p.rows_of_16 = rows_16 <= 2 ? static_cast<int>(std::max<int64_t>(1, rows_16)) : chunk::kTileRows / 16;
   p.tile_tokens = static_cast<int>(16 * p.rows_of_16 / group);
-  p.n_items = std::min<int64_t>(n_tokens, n_tokens / p.tile_tokens + n_seqs);
-  // splits for what the items come to if chunks are alike
-  const int64_t of_seq = (n_tokens + n_seqs - 1) / n_seqs, units = n_seqs * ((of_seq + p.tile_tokens - 1) / p.tile_tokens) * l->n_kv_heads;
-  const int64_t pages = std::max<int64_t>(max_pages, 1);
-  // At most this many splits, a number that only grows with the pages: the workspace has room for it, whatever a window leaves of them.
-  // (The number taken is no such bound: 10 splits of 21 pages come to 7 of 3, of 20 pages to 10 of 2.)  Eight rounds of work-groups
-  // need 270 MB.
-  int64_t most;
-  if (p.rows_of_16 <= 2) most = std::min((3 * kComputeUnits + units - 1) / units, (pages + 1) / 2);
-  else most = std::min(8 * kComputeUnits / units, (pages + kWaveRound - 1) / kWaveRound);
-  most = std::max<int64_t>(1, std::min<int64_t>(most, kMaxSplits));
-  int64_t splits = most;
-  if (p.rows_of_16 > 2) {
-    // A compute unit has one work-group: rounds of them, in pages of time.  Starting and ending a work-group takes as long as three
-    // pages, writing and joining the parts of 256 work-groups as 3.3
+  p.n_items = std::min<int64_t>(n_tokens, (n_tokens + static_cast<int64_t>(n_seqs) * (p.tile_tokens - 1)) / p.tile_tokens);
+  // what the items come to if chunks are alike
+  const int64_t of_seq = (n_tokens + n_seqs - 1) / n_seqs, units = n_seqs * ((of_seq + p.tile_tokens - 1) / p.tile_tokens), heads = l->n_kv_heads;
+  // Places for parts.  Many rows: empty places cost time, each a compute unit's for what it takes to see that it is empty
+  const bool few = p.rows_of_16 <= 2;
+  const int64_t rounds = few ? 2 : (n_seqs == 1 ? 8 : (units * heads <= kComputeUnits ? 2 : 4)), places = rounds * kComputeUnits / heads;
+  const int64_t least = few ? chunk::kFewLeast : chunk::kSharedLeast;
+  // (the workspace's size only grows with the pages, so that it is enough for whatever a window leaves of them)
+  p.parts = 0;
+  p.cuts = units < places && max_pages > least ? 1 : 0;
+  p.n_units = p.cuts ? std::max(p.n_items, std::min(places, p.n_items * std::min<int64_t>((max_pages + least - 1) / least, chunk::kMaxParts))) : p.n_items;
+  const size_t rows = p.cuts ? static_cast<size_t>(p.n_units * heads) * 16 * p.rows_of_16 : 0;
+  p.acc_bytes = round256(rows * kHeadDim * sizeof(float));
+  p.ml_bytes = round256(rows * 2 * sizeof(float));
+  p.bytes = std::max<size_t>(256, p.acc_bytes + p.ml_bytes + (p.cuts ? round256(p.n_units * 4 * sizeof(int32_t)) : 0));
+  if (few || !p.cuts) return p;
+  // Where items are alike as far as the host can tell, no more places than the kernel's rule (find_cut) would take, if it cuts at all
+  if (n_seqs == 1 || windowed || units * heads >= 2 * kComputeUnits) {
+    int64_t parts = 1;
     double best = 0.;
-    for (int64_t k = 1; k <= most; ++k) {
-      const double rounds = static_cast<double>((units * k + kComputeUnits - 1) / kComputeUnits);
-      const double cost = rounds * (static_cast<double>((pages + k - 1) / k) + 3.) + (k > 1 ? 2. + 3.3 * static_cast<double>(units * k) / kComputeUnits : 0.);
-      if (k == 1 || cost < best) {
-        best = cost;
-        splits = k;
+    for (int64_t k = 1; k <= std::min<int64_t>({p.n_units / units, (max_pages + least - 1) / least, chunk::kMaxParts}); ++k) {
+      const double n = static_cast<double>(units * heads * k) / kComputeUnits;
+      const double time = std::ceil(n) * (static_cast<double>(max_pages) / static_cast<double>(k) + 3.) + (k > 1 ? 2. + 3.3 * n : 0.);
+      if (k == 1 || time < best) {
+        best = time;
+        parts = k;
       }
     }
+    if (parts == 1) p.cuts = 0;
+    else if (n_seqs == 1) p.parts = static_cast<int>(parts);
+    p.n_units = std::max(p.n_items, std::min(p.n_units, units * parts));
   }
-  p.pages_per_split = static_cast<int>((pages + splits - 1) / splits);
-  p.n_splits = static_cast<int>((pages + p.pages_per_split - 1) / p.pages_per_split);
-  const size_t rows = most > 1 ? static_cast<size_t>(p.n_items) * l->n_kv_heads * most * 16 * p.rows_of_16 : 0;
-  p.acc_bytes = round256(rows * kHeadDim * sizeof(float));
-  p.bytes = std::max<size_t>(256, p.acc_bytes + round256(rows * 2 * sizeof(float)));
   return p;
 }
 
@@ -116,7 +137,7 @@ using namespace pq;
 
 extern "C" size_t pq_chunk_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_t n_q_heads, int64_t n_tokens, int32_t max_seq_len) {
   if (check_chunk_shape(layout, n_seqs, n_q_heads, n_tokens, max_seq_len) != PQ_OK) return 0;
-  const ChunkLaunch p = plan_launch(layout, n_seqs, n_q_heads, n_tokens, (static_cast<int64_t>(max_seq_len) + kGroup - 1) / kGroup);
+  const ChunkLaunch p = plan_launch(layout, n_seqs, n_q_heads, n_tokens, (static_cast<int64_t>(max_seq_len) + kGroup - 1) / kGroup, false);
   return launch_fits(layout, p) ? p.bytes : 0;
 }
 
@@ -145,12 +166,12 @@ extern "C" int pq_chunk_attention(const pq_layout* layout, const void* q, pq_dty
   // a window as long as the longest sequence hides nothing
   if (window >= max_seq_len) window = 0;
   n_sinks = window > 0 ? std::min(n_sinks, max_seq_len) : 0;
-  const ChunkLaunch most = plan_launch(layout, n_seqs, n_q_heads, n_tokens, seq_pages);
+  const ChunkLaunch most = plan_launch(layout, n_seqs, n_q_heads, n_tokens, seq_pages, false);
   if (!launch_fits(layout, most)) return PQ_ERR_UNSUPPORTED;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < most.bytes) return PQ_ERR_WORKSPACE;
   int64_t pages = seq_pages;
   if (window > 0) pages = std::min<int64_t>(pages, (static_cast<int64_t>(n_sinks) + kGroup - 1) / kGroup + (static_cast<int64_t>(window) + most.tile_tokens) / kGroup + 2);
-  const ChunkLaunch p = plan_launch(layout, n_seqs, n_q_heads, n_tokens, pages);
+  const ChunkLaunch p = plan_launch(layout, n_seqs, n_q_heads, n_tokens, pages, window > 0);
 
   ChunkAttentionArgs a = {};
   a.q = static_cast<const __half*>(q);
@@ -165,6 +186,7 @@ extern "C" int pq_chunk_attention(const pq_layout* layout, const void* q, pq_dty
   a.out = static_cast<__half*>(out);
   a.ws_acc = static_cast<float*>(workspace);
   a.ws_ml = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + p.acc_bytes);
+  a.ws_units = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(workspace) + p.acc_bytes + p.ml_bytes);
   a.n_tokens = n_tokens;
   a.n_pool_pages = n_pool_pages;
   a.n_seqs = n_seqs;
@@ -177,21 +199,23 @@ extern "C" int pq_chunk_attention(const pq_layout* layout, const void* q, pq_dty
   a.n_sinks = n_sinks;
   a.tile_tokens = p.tile_tokens;
   a.n_items = static_cast<int32_t>(p.n_items);
-  a.n_splits = p.n_splits;
-  a.pages_per_split = p.pages_per_split;
+  a.n_units = static_cast<int32_t>(p.n_units);
+  a.cuts = p.cuts;
+  a.parts = p.parts;
+  a.longest_first = p.rows_of_16 > 2 && n_seqs > 1 && n_seqs <= 64 ? 1 : 0;
   a.table_index = key_table_index(layout);
   // (above zero, so that masked scores stay -inf whatever the scale is)
   a.scale_log2 = std::max(static_cast<float>(std::fabs(static_cast<double>(sm_scale)) * 1.4426950408889634074), 1.17549435e-38f);
   a.negate = sm_scale < 0.f ? 1 : 0;
-  const dim3 grid(static_cast<uint32_t>(p.n_items * layout->n_kv_heads), p.n_splits);
+  const dim3 grid(static_cast<uint32_t>(p.n_units * layout->n_kv_heads));
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   if (v_bits == 16) launch_chunk_v16(layout, p.rows_of_16, a, grid, stream);
   else if (v_bits == 4) launch_chunk_v4(layout, p.rows_of_16, a, grid, stream);
   else launch_chunk_v2(layout, p.rows_of_16, a, grid, stream);
   hipError_t e = hipGetLastError();
-  if (e == hipSuccess && p.n_splits > 1) {
+  if (e == hipSuccess && p.cuts) {
     const int rows = 16 * p.rows_of_16;
-    hipLaunchKernelGGL(pq_chunk_join_kernel, dim3(grid.x, rows / (kJoinThreads / 64)), dim3(kJoinThreads), 0, stream, a, rows);
+    hipLaunchKernelGGL(pq_chunk_join_kernel, dim3(grid.x, rows / kJoinRows), dim3(16 * kJoinRows), 0, stream, a, rows);
     e = hipGetLastError();
   }
   return e == hipSuccess ? PQ_OK : record_hip_error(e);

@@ -33,8 +33,9 @@ struct ChunkAttentionArgs {
   const int32_t* starts;
   const int32_t* seq_lens;     // with the chunk
   __half* out;                 // [n_tokens][n_q_heads][d]
-  float* ws_acc;               // [item][KV head][split][row][d], un-normalised
-  float* ws_ml;                // [item][KV head][split][row][2]
+  float* ws_acc;               // [unit][KV head][row][d], un-normalised
+  float* ws_ml;                // [unit][KV head][row][2]
+  int32_t* ws_units;           // [unit][4]: note_unit()
   int64_t n_tokens;
   int64_t n_pool_pages;
   int32_t n_seqs;
@@ -47,8 +48,10 @@ struct ChunkAttentionArgs {
   int32_t n_sinks;
   int32_t tile_tokens;         // of an item
   int32_t n_items;             // at most
-  int32_t n_splits;            // of an item's pages, at most ...
-  int32_t pages_per_split;     // ... this long each
+  int32_t n_units;             // places for parts of items, of a KV head
+  int32_t cuts;                // whether items may be cut:
+  int32_t parts;               // alike, into so many parts; 0: by what the sequences hold
+  int32_t longest_first;
   int32_t table_index;
   float scale_log2;            // > 0
   int32_t negate;              // the queries
@@ -62,42 +65,144 @@ bool launch_chunk_v2(const pq_layout* l, int rows_of_16, const ChunkAttentionArg
 namespace {
 namespace chunk {
 
-constexpr int kLift = 7;
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 
-// A work-group's part of the launch: tokens [first, first + count) of a sequence's chunk.
-struct Item {
-  int seq, first, count;
-  int64_t row0;                // of the chunk in q and out
-  int len;                     // tokens of the sequence, the chunk with them
-  int n;                       // tokens of the chunk
-};
+constexpr int kLift = 7;
+constexpr int kMaxParts = 64;                      // of an item: a lane each when they are joined
+constexpr int kFewLeast = 2, kSharedLeast = 4;     // pages of a part
 
 // Chunks are non-decreasing ranges of [0, n_tokens]; whatever `starts` holds, rows stay within.
 __device__ __forceinline__ void chunk_range(const ChunkAttentionArgs& a, int s, int64_t& first, int64_t& end) {
   first = min(max(static_cast<int64_t>(a.starts[s]), int64_t{0}), a.n_tokens);
   end = min(max(static_cast<int64_t>(a.starts[s + 1]), first), a.n_tokens);
 }
+__device__ __forceinline__ int sequence_len(const ChunkAttentionArgs& a, int s) { return min(max(a.seq_lens[s], 0), a.max_seq_len); }
 
-// Finds item `index`: sequences in order, each one's tiles in order.  Every wavefront does it for itself, 64 sequences at a time.
-__device__ __forceinline__ bool find_item(const ChunkAttentionArgs& a, int index, int lane, Item& item) {
+// ---- how a launch is shared out: by every wavefront alike, a sequence a lane, from what the sequences really hold --------------------
+// Items are tiles of tile_tokens of a sequence's chunk; the pages that one sees are cut into parts of alike length, a work-group each.
+// A sequence's tiles see about the same pages, so they have the same number of parts.  Lengths are known here only, and max_seq_len may be far
+// above them: cut by what there is, and with many rows the longest first, 12 chunks of 1 .. 700 tokens over up to 8192 take 403 us, cut
+// by the host as if all were as long as the longest 483; 16 x 5 tokens over 500 .. 6000 41 against 46.  Where all are alike
+// that costs 1 .. 3 us a work-group (16 x 128 tokens over 4000 164 against 153).
+struct Sequence {
+  int index, tiles, pages;     // pages: what a tile sees at most
+};
+__device__ __forceinline__ Sequence sequence_of(const ChunkAttentionArgs& a, int s) {
+  Sequence x = {s, 0, 0};
+  if (s < a.n_seqs) {
+    int64_t first, end;
+    chunk_range(a, s, first, end);
+    const int len = sequence_len(a, s);
+    x.tiles = static_cast<int>((static_cast<uint32_t>(end - first) + a.tile_tokens - 1) / a.tile_tokens);
+    x.pages = pages_of_len(len);
+    // (the first query's window and the others' tokens: n tokens in a row lie in (n + 126) / 128 + 1 pages at most)
+    if (a.window > 0)
+      x.pages = min(x.pages, pages_of_len(min(a.n_sinks, len)) + static_cast<int>((static_cast<uint32_t>(a.window) + a.tile_tokens + 125u) / kGroup) + 1);
+  }
+  return x;
+}
+// Parts of a sequence's items for a longest part of 1 / `cut` pages; 0: one.  (Whatever the rounding, everybody has the same number.)
+__device__ __forceinline__ int parts_of(int pages, float cut) { return max(1, static_cast<int>(ceilf(static_cast<float>(pages) * cut))); }
+__device__ __forceinline__ float cut_to(int per) { return 0.99999f * __builtin_amdgcn_rcpf(static_cast<float>(per)); }
+
+// Sums and extremes over the launch's sequences; lane sums are cut off at kMost, so that the wavefront's is an int.
+constexpr int kMost = 1 << 24;
+template <typename F>
+__device__ __forceinline__ int total(const ChunkAttentionArgs& a, const Sequence& mine, int lane, F of) {
+  int sum = of(mine);
+  for (int s0 = 64; s0 < a.n_seqs; s0 += 64) sum = min(sum + of(sequence_of(a, s0 + lane)), kMost);
+  return wave_sum(sum);
+}
+__device__ __forceinline__ int count_units(const ChunkAttentionArgs& a, const Sequence& mine, int lane, float cut) {
+  return total(a, mine, lane, [&](const Sequence& x) { return min(x.tiles, kMost / kMaxParts) * parts_of(x.pages, cut); });
+}
+struct Load {
+  int items, work, longest, shortest;              // work: pages of all items
+  __device__ __forceinline__ Load(const ChunkAttentionArgs& a, const Sequence& mine, int lane) {
+    uint32_t high = mine.tiles > 0 ? mine.pages : 0, low = mine.tiles > 0 ? mine.pages : kMost;
+    for (int s0 = 64; s0 < a.n_seqs; s0 += 64) {
+      const Sequence x = sequence_of(a, s0 + lane);
+      high = max(high, x.tiles > 0 ? static_cast<uint32_t>(x.pages) : 0u);
+      low = min(low, x.tiles > 0 ? static_cast<uint32_t>(x.pages) : static_cast<uint32_t>(kMost));
+    }
+    longest = static_cast<int>(wave_max_u32(high));
+    shortest = kMost - static_cast<int>(wave_max_u32(kMost - low));
+    items = total(a, mine, lane, [](const Sequence& x) { return x.tiles; });
+    work = total(a, mine, lane, [](const Sequence& x) { return min(x.tiles, kMost / 1024) * min(x.pages, 1024); });
+  }
+};
+
+// Few rows: work-groups that run at once, with parts as alike as can be -- the shortest that fit.  0: no cuts.
+__device__ __forceinline__ float find_fitting_cut(const ChunkAttentionArgs& a, const Sequence& mine, int lane) {
+  const Load load(a, mine, lane);
+  const int least = max(kFewLeast, (load.longest + kMaxParts - 1) / kMaxParts);
+  if (load.items == 0 || load.items >= a.n_units) return 0.f;
+  int per = max(least, static_cast<int>(ceilf(static_cast<float>(load.work) * __builtin_amdgcn_rcpf(static_cast<float>(a.n_units)) * 0.99999f)));
+  for (int i = 0; i < 16 && per < load.longest; ++i) {
+    if (count_units(a, mine, lane, cut_to(per)) <= a.n_units) return cut_to(per);
+    per += 1 + (per >> 4);
+  }
+  return 0.f;
+}
+
+// Many rows: candidate `index` of 16, and what it takes.  A compute unit has one work-group, and the longest come first: they end together,
+// as far as the length of the shortest ones allows.  In pages of time: starting and ending a work-group takes as long as three, writing
+// and joining 256 parts as 3.3.
+__device__ __forceinline__ float judge_cut(const ChunkAttentionArgs& a, const Sequence& mine, int index, int lane, uint32_t& time) {
+  const Load load(a, mine, lane);
+  const int least = max(kSharedLeast, (load.longest + kMaxParts - 1) / kMaxParts);
+  const float heads = static_cast<float>(a.n_kv_heads) * (1.f / kComputeUnits), longest = static_cast<float>(load.longest), shortest = static_cast<float>(load.shortest);
+  // 1 .. 16 parts of the longest items, or, with few items, up to 8 rounds' worth
+  const float more = fmaxf(1.f, 0.5f * __builtin_amdgcn_rcpf(fmaxf(static_cast<float>(load.items), 1.f) * heads)), parts = floorf(static_cast<float>(index + 1) * more);
+  const float cut = index == 0 ? 0.f : cut_to(max(least, static_cast<int>(ceilf(longest * __builtin_amdgcn_rcpf(parts) * 0.99999f))));
+  const int n = count_units(a, mine, lane, cut), parts_long = parts_of(load.longest, cut);
+  const float rounds = static_cast<float>(n) * heads;
+  const float part_long = longest * __builtin_amdgcn_rcpf(static_cast<float>(parts_long)), part_short = shortest * __builtin_amdgcn_rcpf(static_cast<float>(parts_of(load.shortest, cut)));
+  float t = fmaxf(part_long + 3.f, static_cast<float>(load.work) * heads + 3.f * rounds + (ceilf(rounds) - rounds) * (part_short + 3.f));
+  if (parts_long > 1) t += 2.f + 3.3f * rounds;
+  time = index > 0 && n > a.n_units ? 0x7f000000u : f2u(t);                   // (positive floats are in order as integers)
+  return cut;
+}
+
+// A work-group's part of the launch: part `part` of tokens [first, first + count) of a sequence's chunk.
+struct Item {
+  int seq, first, count;
+  int64_t row0;                // of the chunk in q and out
+  int len;                     // tokens of the sequence, the chunk with them
+  int n;                       // tokens of the chunk
+  int unit, part, parts;       // unit: the part's
+};
+
+// The sequences by their pages, the longest ones first (n_seqs <= 64): lane l gets the one of rank l.
+__device__ __forceinline__ Sequence longest_first(const ChunkAttentionArgs& a, const Sequence& mine, int lane) {
+  int rank = lane < a.n_seqs ? 0 : lane;
+  for (int s = 0; s < a.n_seqs; ++s) {
+    const int other = __builtin_amdgcn_readlane(mine.pages, s);
+    if (lane < a.n_seqs) rank += other > mine.pages || (other == mine.pages && s > lane) ? 1 : 0;
+  }
+  return {__builtin_amdgcn_ds_permute(4 * rank, mine.index), __builtin_amdgcn_ds_permute(4 * rank, mine.tiles), __builtin_amdgcn_ds_permute(4 * rank, mine.pages)};
+}
+// Finds part `unit` of the launch: sequences in order, `mine` the lane's of the first 64; the later tiles of one first.
+__device__ __forceinline__ bool find_item(const ChunkAttentionArgs& a, const Sequence& mine, float cut, int unit, int lane, Item& item) {
   int before = 0;
   for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
-    const int s = s0 + lane;
-    int64_t first = 0, end = 0;
-    if (s < a.n_seqs) chunk_range(a, s, first, end);
-    const int tiles = static_cast<int>((static_cast<uint32_t>(end - first) + a.tile_tokens - 1) / a.tile_tokens);
-    const int upto = before + wave_prefix(tiles);
-    const uint64_t past = __builtin_amdgcn_ballot_w64(upto > index);
+    const Sequence x = s0 == 0 ? mine : sequence_of(a, s0 + lane);
+    const int parts = parts_of(x.pages, cut), units = x.tiles * parts, upto = before + wave_prefix(units);
+    const uint64_t past = __builtin_amdgcn_ballot_w64(upto > unit);
     if (past != 0) {
-      const int at = __builtin_ctzll(past);
-      item.seq = s0 + at;
-      const int tile = index - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(tiles, at));
+      const int at = __builtin_ctzll(past), place = unit - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(units, at));
+      item.seq = __builtin_amdgcn_readlane(x.index, at);
+      item.unit = unit;
+      item.parts = __builtin_amdgcn_readlane(parts, at);
+      const int from_last = place / item.parts;
+      item.part = place - from_last * item.parts;
+      int64_t first, end;
       chunk_range(a, item.seq, first, end);
       item.row0 = first;
       item.n = static_cast<int>(end - first);
-      item.first = tile * a.tile_tokens;
+      item.first = (__builtin_amdgcn_readlane(x.tiles, at) - 1 - from_last) * a.tile_tokens;
       item.count = min(a.tile_tokens, item.n - item.first);
-      item.len = min(max(a.seq_lens[item.seq], 0), a.max_seq_len);
+      item.len = sequence_len(a, item.seq);
       return true;
     }
     before = __builtin_amdgcn_readlane(upto, 63);
@@ -108,16 +213,31 @@ __device__ __forceinline__ bool find_item(const ChunkAttentionArgs& a, int index
 // Pages that an item's rows see: the sinks' [0, n_first) and [from, from + n_rest).
 struct VisiblePages {
   int n_first, from, n_rest;
-  __device__ __forceinline__ int count() const { return n_first + n_rest; }
-};
-__device__ __forceinline__ VisiblePages visible_pages(const ChunkAttentionArgs& a, int first_position, int last_position) {
-  VisiblePages v = {0, 0, pages_of_len(last_position + 1)};
-  if (a.window > 0) {
-    const int sinks = min(pages_of_len(a.n_sinks), v.n_rest);
-    const int begin = max(0, first_position - a.window + 1) / kGroup;
-    if (begin > sinks) v = {sinks, begin, max(0, v.n_rest - begin)};
+  __device__ __forceinline__ VisiblePages(const ChunkAttentionArgs& a, const Item& item) : n_first(0), from(0) {
+    const int first_position = item.len - item.n + item.first;
+    n_rest = pages_of_len(first_position + item.count);
+    if (a.window > 0) {
+      const int sinks = min(pages_of_len(a.n_sinks), n_rest), begin = max(0, first_position - a.window + 1) / kGroup;
+      if (begin > sinks) {
+        n_first = sinks;
+        from = begin;
+        n_rest = max(0, n_rest - begin);
+      }
+    }
   }
-  return v;
+  __device__ __forceinline__ int count() const { return n_first + n_rest; }
+  // of the item's parts, the last of which may be shorter or missing
+  __device__ __forceinline__ int part_len(const Item& item) const { return max(1, (count() + item.parts - 1) / item.parts); }
+};
+
+// What the parts' join has to know of a unit: rows from `row` on, the number of parts if it is the first of several, otherwise 0.
+__device__ __forceinline__ void note_unit(const ChunkAttentionArgs& a, int kvh, int unit, int row, int count, int parts) {
+  if (a.cuts && kvh == 0) *reinterpret_cast<i32x4*>(a.ws_units + static_cast<int64_t>(unit) * 4) = i32x4{row, count, parts, 0};
+}
+__device__ __forceinline__ void note_unit(const ChunkAttentionArgs& a, int kvh, const Item& item, const VisiblePages& pages) {
+  const int part_len = pages.part_len(item);
+  note_unit(a, kvh, item.unit, static_cast<int>(item.row0) + item.first, item.count,
+            item.part == 0 && item.parts > 1 ? max(1, (pages.count() + part_len - 1) / part_len) : 0);
 }
 
 template <int N, typename F>
@@ -298,7 +418,7 @@ struct Rows {
     for (int rt = 0; rt < RT; ++rt) acc[e][rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v_op, p[rt], acc[e][rt], 0, 0, 0);
   }
   __device__ __forceinline__ float top(int rt) const { return limit[rt] > kNegInf ? kLift - off[rt] : kNegInf; }
-  // The lane's 32 dims of a row, 32 (l / 16) + 8 i + e: a split's part, or the output.
+  // The lane's 32 dims of a row, 32 (l / 16) + 8 i + e: a part of its pages, or the output.
   __device__ __forceinline__ void store_part(const ChunkAttentionArgs& a, int rt, int64_t row, float m, float l, int quarter) const {
     float* const to = a.ws_acc + row * kHeadDim + 32 * quarter;
 #pragma unroll
@@ -341,17 +461,16 @@ __device__ __forceinline__ f16x8 query_operand(const ChunkAttentionArgs& a, int6
                     __builtin_amdgcn_perm(y.y, x.y, 0x05040100u) ^ sign, __builtin_amdgcn_perm(y.y, x.y, 0x07060302u) ^ sign);
 }
 
-// The pages of a work-group's split, and what is known of each.
-struct SplitPages {
+// The pages of a work-group's part, and what is known of each.
+struct PartPages {
   VisiblePages pages;
   const int32_t* table;
   int64_t n_pool_pages;
   int begin, end, width, tail_page, len;
-  __device__ __forceinline__ SplitPages(const ChunkAttentionArgs& a, const Item& item, int split) {
-    const int first_position = item.len - item.n + item.first;
-    pages = visible_pages(a, first_position, first_position + item.count - 1);
-    begin = uni(split * a.pages_per_split);
-    end = uni(min(begin + a.pages_per_split, pages.count()));
+  __device__ __forceinline__ PartPages(const ChunkAttentionArgs& a, const Item& item) : pages(a, item) {
+    const int part_len = pages.part_len(item);
+    begin = uni(item.part * part_len);
+    end = uni(min(begin + part_len, pages.count()));
     table = a.block_table + static_cast<int64_t>(item.seq) * a.max_pages_per_seq;
     n_pool_pages = a.n_pool_pages;
     width = a.max_pages_per_seq;
@@ -455,12 +574,16 @@ __device__ __forceinline__ void few_body(const ChunkAttentionArgs& a) {
   __shared__ __attribute__((aligned(16))) f16x8 query[RT][4][64];
   __shared__ float fold_m[kFewWaves][RT * 16], fold_l[kFewWaves][RT * 16];
   const int tid = threadIdx.x, wave = uni(tid >> 6), lane = tid & 63, quarter = lane >> 4, col = lane & 15;
-  const int kvh = blockIdx.x % a.n_kv_heads, index = a.n_items - 1 - blockIdx.x / a.n_kv_heads;   // later tokens, which see more, first
-  const int split = blockIdx.y;
+  const int kvh = blockIdx.x % a.n_kv_heads;
   Item item;
-  if (!find_item(a, index, lane, item)) return;
-  const SplitPages pages(a, item, split);
-  if (split > 0 && pages.begin >= pages.end) return;
+  const Sequence mine = sequence_of(a, lane);
+  if (!find_item(a, mine, a.cuts ? find_fitting_cut(a, mine, lane) : 0.f, blockIdx.x / a.n_kv_heads, lane, item)) {
+    if (tid == 0) note_unit(a, kvh, blockIdx.x / a.n_kv_heads, 0, 0, 0);
+    return;
+  }
+  const PartPages pages(a, item);
+  if (tid == 0) note_unit(a, kvh, item, pages.pages);
+  if (item.part > 0 && pages.begin >= pages.end) return;
   const int first_position = item.len - item.n + item.first, last_position = first_position + item.count - 1;
 
   // a page on its way: the wavefront's two tiles of keys, the parameters of pair `lane`; and values, of the next page or the next two
@@ -628,8 +751,9 @@ __device__ __forceinline__ void few_body(const ChunkAttentionArgs& a) {
   if (wave != 0) return;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    if (a.n_splits > 1) {
-      rows.store_part(a, rt, ((static_cast<int64_t>(index) * a.n_kv_heads + kvh) * a.n_splits + split) * (16 * RT) + 16 * rt + col, top[rt], total[rt], quarter);
+    if (item.parts > 1) {
+      if (16 * rt + col < item.count * a.group)
+        rows.store_part(a, rt, (static_cast<int64_t>(item.unit) * a.n_kv_heads + kvh) * (16 * RT) + 16 * rt + col, top[rt], total[rt], quarter);
     } else {
       const RowPlace place(a, item, kvh, 16 * rt + col);
       if (place.there) rows.store_out(rt, a.out + place.at, total[rt], quarter);
@@ -782,13 +906,34 @@ __device__ __forceinline__ void shared_body(const ChunkAttentionArgs& a) {
   __shared__ __attribute__((aligned(16))) uint8_t tables[Trig::kTableBytes * (Trig::kGrouped ? 2 : 1)];
   __shared__ float fold_m[kSharedWaves][kSharedRows], fold_l[kSharedWaves][kSharedRows];
   const int tid = threadIdx.x, wave = uni(tid >> 6), lane = tid & 63, quarter = lane >> 4, col = lane & 15;
-  const int kvh = blockIdx.x % a.n_kv_heads, index = a.n_items - 1 - blockIdx.x / a.n_kv_heads;   // later tokens, which see more, first
-  const int split = blockIdx.y;
+  const int kvh = blockIdx.x % a.n_kv_heads;
   Item item;
-  if (!find_item(a, index, lane, item)) return;
-  const SplitPages pages(a, item, split);
+  Sequence mine = sequence_of(a, lane);
+  float cut = 0.f;
+  if (a.parts > 0) {
+    cut = cut_to(max(kSharedLeast, (mine.pages + a.parts - 1) / a.parts));    // (of lane 0, the only sequence or one as long as all)
+    cut = u2f(static_cast<uint32_t>(uni(static_cast<int>(f2u(cut)))));
+  } else if (a.cuts) {
+    // a candidate a wavefront
+    uint32_t time;
+    const float candidate = judge_cut(a, mine, wave, lane, time);
+    if (lane == 0) {
+      fold_m[0][wave] = candidate;
+      fold_l[0][wave] = u2f((time & ~15u) | wave);
+    }
+    __syncthreads();
+    cut = fold_m[0][~wave_max_u32(~f2u(fold_l[0][col])) & 15u];
+    __syncthreads();                                                          // (fold_m and fold_l are used again)
+  }
+  if (a.longest_first) mine = longest_first(a, mine, lane);
+  if (!find_item(a, mine, cut, blockIdx.x / a.n_kv_heads, lane, item)) {
+    if (tid == 0) note_unit(a, kvh, blockIdx.x / a.n_kv_heads, 0, 0, 0);
+    return;
+  }
+  const PartPages pages(a, item);
+  if (tid == 0) note_unit(a, kvh, item, pages.pages);
   const int begin = pages.begin, end = pages.end;
-  if (split > 0 && begin >= end) return;
+  if (item.part > 0 && begin >= end) return;
   const int first_position = item.len - item.n + item.first, last_position = first_position + item.count - 1;
 
   // wavefront = (rows 16 row_group .., part): `groups` row groups, a power of two; a part is 4 / parts steps of 32 tokens of each page, or,
@@ -898,8 +1043,8 @@ __device__ __forceinline__ void shared_body(const ChunkAttentionArgs& a) {
     }
   }
   if (!computes) return;
-  if (a.n_splits > 1) rows.store_part(a, 0, ((static_cast<int64_t>(index) * a.n_kv_heads + kvh) * a.n_splits + split) * kTileRows + row, m, l, quarter);
-  else if (place.there) rows.store_out(0, a.out + place.at, l, quarter);
+  if (item.parts > 1 && row < n_rows) rows.store_part(a, 0, (static_cast<int64_t>(item.unit) * a.n_kv_heads + kvh) * kTileRows + row, m, l, quarter);
+  else if (item.parts == 1 && place.there) rows.store_out(0, a.out + place.at, l, quarter);
 }
 
 }  // namespace chunk

@@ -328,3 +328,25 @@ def test_overlapping_calls_of_two_graphs():
                 graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+@pytest.mark.parametrize("starts", [[0, 0, 0, 0], [7, 7, 7, 7], [0, 40, 0, 40], [40, 0, 40, 0], [-5, 3, 90, 20], [0, 1 << 30, 1 << 30, 1 << 30]])
+@pytest.mark.parametrize("rows", [40, 2])
+def test_starts_that_are_no_ranges_of_the_rows(starts, rows):
+    """Empty chunks alone, and starts that the documentation does not allow: nothing outside the tensors is touched, and a call
+    with proper ones afterwards, in the same workspace, is right."""
+    c = Cache([2000, 900, 1200], 2)
+    pq = c.pq
+    q = _queries(rows, 8, 3)
+    size = pq.pq_chunk_workspace_bytes(c.layout, 3, 8, rows, c.max_seq_len)
+    guarded, out = torch.full((size + 4096,), 0x5A, dtype=torch.uint8, device=DEV), torch.full((rows + 40, 8, D), 3.0, dtype=torch.float16, device=DEV)
+    proper = [0, rows // 2, rows // 2, rows]
+    for s in (starts, proper, starts, proper):
+        out.fill_(3.0)
+        pq.pq_chunk_attention(c.layout, q, _ints(s), c.codes, c.params, c.v_pool, c.block_table, c.seq_lens, c.max_seq_len, float(c.sm_scale), out[:rows],
+                              guarded[:size], c.residual)
+        torch.cuda.synchronize()
+        assert bool((guarded[size:] == 0x5A).all()) and bool((out[rows:] == 3.0).all())
+        if len(set(starts)) == 1 and s is starts:
+            assert bool((out == 3.0).all())
+    assert torch.equal(out[:rows], _attend(c, q, proper))
