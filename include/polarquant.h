@@ -355,7 +355,8 @@ int pq_plan_pages(const pq_layout* layout, const int32_t* seq_lens, const int32_
  *   residual      device fp16 [n_seqs][n_kv_heads][g][d] (16-byte aligned)
  *   v_pool, v_bits, v_params_pool   as in pq_decode_attention; quantized values as pq_encode_values makes them, and only the
  *                 named slots are written
- *   A group whose page index is >= max_pages_per_seq or whose page id is outside the pool is not encoded.
+ *   A group whose page index is >= max_pages_per_seq or whose page id is outside the pool is not encoded.  A page that
+ *   two sequences complete in one call holds a mixture of both.
  *
  * n_tokens == 0 or n_seqs == 0 is a no-op.
  */

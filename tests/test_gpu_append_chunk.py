@@ -169,8 +169,10 @@ def test_a_captured_step_is_replayed():
         results = []
         rows = [torch.from_numpy(rng.standard_normal((room, heads, D))).to(DEV).half() for _ in range(2)]
         for way in (graph.replay, step):
-            for x in (table.fill_(39), slots, starts, after, counts, residual, *cache[:3]):
-                x.zero_() if x is not table else None
+            # (pages of their own for the tokens before: in one page of three sequences the last to write would be seen)
+            table.copy_(_ints(np.arange(seqs * width).reshape(seqs, width) + 40 - seqs * width))
+            for x in (slots, starts, after, counts, residual, *cache[:3]):
+                x.zero_()
             lens.copy_(_ints(before))
             new.copy_(_ints(fresh))
             keys.copy_(rows[0])
