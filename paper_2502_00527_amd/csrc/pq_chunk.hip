@@ -101,7 +101,7 @@ ChunkLaunch plan_launch(const pq_layout* l, int32_t n_seqs, int32_t n_q_heads, i
   p.ml_bytes = round256(rows * 2 * sizeof(float));
   p.bytes = std::max<size_t>(256, p.acc_bytes + p.ml_bytes + (p.cuts ? round256(p.n_units * 4 * sizeof(int32_t)) : 0));
   if (few || !p.cuts) return p;
-  // Where items are alike as far as the host can tell, no more places than the kernel's rule (find_cut) would take, if it cuts at all
+  // Where items are alike as far as the host can tell, no more places than the kernel's rule (judge_cut) would take, if it cuts at all
   if (n_seqs == 1 || windowed || units * heads >= 2 * kComputeUnits) {
     int64_t parts = 1;
     double best = 0.;

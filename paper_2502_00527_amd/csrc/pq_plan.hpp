@@ -219,7 +219,9 @@ inline int32_t window_bound(int32_t max_seq_len, int32_t window, int32_t n_sinks
   const int64_t pages = (static_cast<int64_t>(n_sinks) + kGroup - 1) / kGroup + (static_cast<int64_t>(window) + kGroup - 1) / kGroup + 1;
   return static_cast<int32_t>(std::min<int64_t>(max_seq_len, pages * kGroup));
 }
-// Its chunks: most sequences are as long as the window lets them be, so that they are alike, and as many as start at once.
+// Its chunks: most sequences are as long as the window lets them be, so that they are alike, and as many as start at once.  (One sequence of
+// 10 pages 13.5 us; in one chunk of a wide work-group 16.5.  48 sequences of up to 18 pages, 4-bit values, a chunk each 35.5, cut in two
+// or three 43 and 47.)
 inline ChunkPlan plan_window(const pq_layout* l, int32_t n_seqs, int32_t bound) {
   const int64_t pages = (static_cast<int64_t>(bound) + kGroup - 1) / kGroup, units = static_cast<int64_t>(n_seqs) * l->n_kv_heads;
   const int64_t most = std::max<int64_t>(1, kResidentGroups / units);
