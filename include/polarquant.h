@@ -367,7 +367,8 @@ int pq_append_chunk(const pq_layout* layout, const void* keys, pq_dtype key_dtyp
                     void* codes_pool, void* params_pool, void* v_pool, int32_t v_bits, void* v_params_pool,
                     int64_t n_pool_pages, void* hip_stream);
 
-/* Bytes of scratch pq_chunk_attention needs (256-byte aligned device memory), whatever its window; 0 on invalid arguments. */
+/* Bytes of scratch pq_chunk_attention needs (256-byte aligned device memory), whatever its window and for any smaller max_seq_len: 273 MB at
+ * most; 0 on invalid arguments. */
 size_t pq_chunk_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_t n_q_heads, int64_t n_tokens,
                                 int32_t max_seq_len);
 
@@ -379,6 +380,8 @@ size_t pq_chunk_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_t
  *
  *   q             device fp16 [n_tokens][n_q_heads][d], post-RoPE (16-byte aligned; PQ_F32: PQ_ERR_UNSUPPORTED).  Query head h reads
  *                 KV head h / (n_q_heads / n_kv_heads); the ratio may be 1 .. 16
+ *   n_tokens      rows of q and out.  Which kernel runs goes by n_tokens / n_seqs: padding beyond what the chunks need is
+ *                 not computed, but a call sized for it may get the kernel for many rows
  *   starts        device int32 [n_seqs + 1] (pq_plan_pages); non-decreasing, within [0, n_tokens]
  *   seq_lens      device int32 [n_seqs]: lengths WITH the chunks (pq_plan_pages' lens_after); above max_seq_len they are
  *                 treated as max_seq_len.  A query that would stand before the sequence's first token gets a row of zeros

@@ -61,7 +61,7 @@ __global__ __launch_bounds__(256) void pq_read_stream_kernel(const probe_u32x4* 
 
 using namespace pq;
 
-extern "C" int pq_version(void) { return 102; }
+extern "C" int pq_version(void) { return 103; }
 
 extern "C" const char* pq_strerror(int status) {
   switch (status) {

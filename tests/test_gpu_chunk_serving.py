@@ -350,3 +350,20 @@ def test_starts_that_are_no_ranges_of_the_rows(starts, rows):
         if len(set(starts)) == 1 and s is starts:
             assert bool((out == 3.0).all())
     assert torch.equal(out[:rows], _attend(c, q, proper))
+
+
+@pytest.mark.parametrize("kv_heads,seqs,most_len,most_new", [(1, 100, 3000, 3), (1, 90, 2500, 60), (2, 64, 4000, 40), (2, 65, 4000, 40), (1, 3, 30000, 90), (8, 5, 6000, 7), (1, 200, 600, 9)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (700, 5)])
+def test_ragged_batches_cut_by_their_lengths(kv_heads, seqs, most_len, most_new, window, sinks):
+    """More sequences than a wavefront has lanes, as many, and fewer; a bound far above the lengths, as a captured call has it."""
+    rng = np.random.default_rng(seqs)
+    new = rng.integers(0, most_new + 1, seqs)
+    new[0] = most_new
+    lens = np.maximum(rng.integers(0, most_len + 1, seqs), new)
+    lens[-1] = most_len
+    c = Cache([int(x) for x in lens], kv_heads)
+    wide = torch.full((seqs, 400), -1, dtype=torch.int32, device=DEV)
+    wide[:, :c.block_table.shape[1]] = c.block_table
+    _check(c, [int(x) for x in new], 4, window, sinks)
+    c.block_table = wide
+    _check(c, [int(x) for x in new], 4, window, sinks, max_seq_len=400 * G)
