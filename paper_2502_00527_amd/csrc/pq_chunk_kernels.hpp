@@ -82,7 +82,7 @@ __device__ __forceinline__ int sequence_len(const ChunkAttentionArgs& a, int s) 
 // Items are tiles of tile_tokens of a sequence's chunk; the pages that one sees are cut into parts of alike length, a work-group each.
 // A sequence's tiles see about the same pages, so they have the same number of parts.  Lengths are known here only, and max_seq_len may be far
 // above them: cut by what there is, and with many rows the longest first, 12 chunks of 1 .. 700 tokens over up to 8192 take 403 us, cut
-// by the host as if all were as long as the longest 483; 16 x 5 tokens over 500 .. 6000 41 against 46.  Where all are alike
+// by the host as if all were as long as the longest 483; 16 x 5 tokens over 500 .. 6000 41 against 46 (37 now).  Where all are alike
 // that costs 1 .. 3 us a work-group (16 x 128 tokens over 4000 164 against 153).
 struct Sequence {
   int index, tiles, pages;     // pages: what a tile sees at most
@@ -586,7 +586,8 @@ __device__ __forceinline__ void few_body(const ChunkAttentionArgs& a) {
   if (item.part > 0 && pages.begin >= pages.end) return;
   const int first_position = item.len - item.n + item.first, last_position = first_position + item.count - 1;
 
-  // a page on its way: the wavefront's two tiles of keys, the parameters of pair `lane`; and values, of the next page or the next two
+  // A page on its way: the wavefront's two tiles of keys, the parameters of pair `lane`; and values, of the next page or the next two.  (32
+  // rows and fp16 values: two pages of them need scratch, 38.7 us against 37.0 for 16 x 5 tokens over 500 .. 6000.)
   constexpr int kValuesAhead = VB == 16 && RT == 2 ? 1 : 2;
   struct Page {
     Unit<W / 2> units[2];
@@ -632,6 +633,8 @@ __device__ __forceinline__ void few_body(const ChunkAttentionArgs& a) {
   rows.clear();
   __syncthreads();
 
+  // One way through for pages that are seen and that are not: with a second copy of the loads the accumulators moved between registers
+  // at its ends (41.0 us against 37.0).
   auto attend = [&](int at, Page& p, const Page& following, Values<VB>& v) {
     auto load_next = [&] {
       if constexpr (kValuesAhead == 1) load_values(at + 1, following.id, v);
@@ -639,72 +642,70 @@ __device__ __forceinline__ void few_body(const ChunkAttentionArgs& a) {
       if constexpr (kValuesAhead == 2) load_values(at + 2, p.id, v);
     };
     const int page = pages.page(at), token0 = page * kGroup + 32 * wave;
-    // nobody sees these tokens
-    if (p.id < 0 || token0 > last_position || (a.window > 0 && token0 >= a.n_sinks && token0 + 31 <= first_position - a.window)) {
-      load_next();
-      return;
-    }
-    const bool masks = token0 + 31 > first_position || (a.window > 0 && token0 <= last_position - a.window && token0 + 31 >= a.n_sinks);
-    f32x4 s[2][RT];
-    auto scores = [&](int tile, const f16x8 (&k_op)[4]) {
-      uint32_t query_at = lds_addr(&query[0][0][0]) + lane * 16;
-      asm volatile("" : "+v"(query_at));                                    // (read for each tile, not kept)
+    // otherwise nobody sees these tokens
+    if (p.id >= 0 && token0 <= last_position && (a.window == 0 || token0 < a.n_sinks || token0 + 31 > first_position - a.window)) {
+      const bool masks = token0 + 31 > first_position || (a.window > 0 && token0 <= last_position - a.window && token0 + 31 >= a.n_sinks);
+      f32x4 s[2][RT];
+      auto scores = [&](int tile, const f16x8 (&k_op)[4]) {
+        uint32_t query_at = lds_addr(&query[0][0][0]) + lane * 16;
+        asm volatile("" : "+v"(query_at));                                    // (read for each tile, not kept)
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks)
+        for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-          s[tile][rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k_op[ks], *(const PQ_LDS f16x8*)static_cast<uintptr_t>(query_at + (rt * 4 + ks) * 1024),
-                                                               ks == 0 ? rows.start(rt) : s[tile][rt], 0, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
-    };
-    f16x8 k_op[4];
-    if (page != pages.tail_page) {
-      wave_lds_sync();                                                      // the page before has been read
-      page_params[wave][lane] = p.par;
-      if constexpr (kGrouped) trig.build(p.angle, 0, 0, 1, lane);
-      wave_lds_sync();
-      uint32_t params[16];
+          for (int rt = 0; rt < RT; ++rt)
+            s[tile][rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k_op[ks], *(const PQ_LDS f16x8*)static_cast<uintptr_t>(query_at + (rt * 4 + ks) * 1024),
+                                                                 ks == 0 ? rows.start(rt) : s[tile][rt], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      f16x8 k_op[4];
+      if (page != pages.tail_page) {
+        wave_lds_sync();                                                      // the page before has been read
+        page_params[wave][lane] = p.par;
+        if constexpr (kGrouped) trig.build(p.angle, 0, 0, 1, lane);
+        wave_lds_sync();
+        uint32_t params[16];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const u32x4 four = *reinterpret_cast<const u32x4*>(&page_params[wave][16 * quarter + 4 * i]);
-        params[4 * i] = four.x; params[4 * i + 1] = four.y; params[4 * i + 2] = four.z; params[4 * i + 3] = four.w;
-      }
-#pragma unroll
-      for (int tile = 0; tile < 2; ++tile) {
-        unrolled<4>([&](auto ks_) {
-          constexpr int ks = decltype(ks_)::value;
-          uint32_t w[4];
-          unrolled<4>([&](auto e_) {
-            constexpr int K = 4 * ks + decltype(e_)::value;
-            w[decltype(e_)::value] = trig.template pair<K>(p.units[tile], params[K], 0);
-          });
-          k_op[ks] = as_operand(w[0], w[1], w[2], w[3]);
-        });
-        scores(tile, k_op);
-      }
-    } else {
-#pragma unroll
-      for (int tile = 0; tile < 2; ++tile) {
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-          const uint32_t offset = (32 * wave + 16 * tile + col) * (kHeadDim * 2) + quarter * 32 + ks * 8;
-          k_op[ks] = plain_pairs(__builtin_amdgcn_raw_buffer_load_b64(tail_rows, offset, 0, kAuxCached),
-                                 __builtin_amdgcn_raw_buffer_load_b64(tail_rows, offset, kPairs * 2, kAuxCached), a.scale_log2);
+        for (int i = 0; i < 4; ++i) {
+          const u32x4 four = *reinterpret_cast<const u32x4*>(&page_params[wave][16 * quarter + 4 * i]);
+          params[4 * i] = four.x; params[4 * i + 1] = four.y; params[4 * i + 2] = four.z; params[4 * i + 3] = four.w;
         }
-        scores(tile, k_op);
+#pragma unroll
+        for (int tile = 0; tile < 2; ++tile) {
+          unrolled<4>([&](auto ks_) {
+            constexpr int ks = decltype(ks_)::value;
+            uint32_t w[4];
+            unrolled<4>([&](auto e_) {
+              constexpr int K = 4 * ks + decltype(e_)::value;
+              w[decltype(e_)::value] = trig.template pair<K>(p.units[tile], params[K], 0);
+            });
+            k_op[ks] = as_operand(w[0], w[1], w[2], w[3]);
+          });
+          scores(tile, k_op);
+        }
+      } else {
+#pragma unroll
+        for (int tile = 0; tile < 2; ++tile) {
+#pragma unroll
+          for (int ks = 0; ks < 4; ++ks) {
+            const uint32_t offset = (32 * wave + 16 * tile + col) * (kHeadDim * 2) + quarter * 32 + ks * 8;
+            k_op[ks] = plain_pairs(__builtin_amdgcn_raw_buffer_load_b64(tail_rows, offset, 0, kAuxCached),
+                                   __builtin_amdgcn_raw_buffer_load_b64(tail_rows, offset, kPairs * 2, kAuxCached), a.scale_log2);
+          }
+          scores(tile, k_op);
+        }
       }
+      if (masks) rows.mask(a, s, token0, position, quarter);
+      rows.settle(s);
+      f16x8 weights[RT];
+      rows.weights(s, weights);
+      unrolled<8>([&](auto e) { rows.add(decltype(e)::value, v.template operand<decltype(e)::value>(), weights); });
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if (masks) rows.mask(a, s, token0, position, quarter);
-    rows.settle(s);
-    f16x8 weights[RT];
-    rows.weights(s, weights);
-    unrolled<8>([&](auto e) { rows.add(decltype(e)::value, v.template operand<decltype(e)::value>(), weights); });
-    __builtin_amdgcn_sched_barrier(0);
     load_next();
   };
   for (int at = pages.begin; at < pages.end; at += 2) {
     attend(at, p[0], p[1], values[0]);
-    if (at + 1 < pages.end) attend(at + 1, p[1], p[0], values[kValuesAhead - 1]);
+    attend(at + 1, p[1], p[0], values[kValuesAhead - 1]);                   // (no page is past the last one, and seen by nobody)
   }
 
   // ---- fold the wavefronts ----
