@@ -64,7 +64,7 @@ __global__ __launch_bounds__(16 * kJoinRows) void pq_chunk_join_kernel(const Chu
 //
 // Up to 32 rows a sequence (in the mean) are the few-rows kernel's, which makes its operands for 16 or 32 rows itself; more are the
 // shared one's, which unpacks a page once for 256.  16 sequences of 4000 tokens, 4 query heads per KV head, microseconds: 8 new tokens each
-// (32 rows) 44, 16 (64 rows) 55, 64 103 -- a page costs the few-rows kernel twice as much for 32 rows as for 16 and would
+// (32 rows) 39, 16 (64 rows) 54, 64 102 -- a page costs the few-rows kernel twice as much for 32 rows as for 16 and would
 // cost it again for each 32 more.
 struct ChunkLaunch {
   int rows_of_16, tile_tokens, cuts, parts;

@@ -76,7 +76,6 @@ __device__ __forceinline__ void chunk_range(const ChunkAttentionArgs& a, int s, 
   first = min(max(static_cast<int64_t>(a.starts[s]), int64_t{0}), a.n_tokens);
   end = min(max(static_cast<int64_t>(a.starts[s + 1]), first), a.n_tokens);
 }
-__device__ __forceinline__ int sequence_len(const ChunkAttentionArgs& a, int s) { return min(max(a.seq_lens[s], 0), a.max_seq_len); }
 
 // ---- how a launch is shared out: by every wavefront alike, a sequence a lane, from what the sequences really hold --------------------
 // Items are tiles of tile_tokens of a sequence's chunk; the pages that one sees are cut into parts of alike length, a work-group each.
@@ -85,19 +84,22 @@ __device__ __forceinline__ int sequence_len(const ChunkAttentionArgs& a, int s) 
 // by the host as if all were as long as the longest 483; 16 x 5 tokens over 500 .. 6000 41 against 46 (37 now).  Where all are alike
 // that costs 1 .. 3 us a work-group (16 x 128 tokens over 4000 164 against 153).
 struct Sequence {
-  int index, tiles, pages;     // pages: what a tile sees at most
+  int index, first, n, len;    // its chunk's first row and tokens, its tokens
+  int tiles, pages;            // pages: what a tile sees at most
 };
 __device__ __forceinline__ Sequence sequence_of(const ChunkAttentionArgs& a, int s) {
-  Sequence x = {s, 0, 0};
+  Sequence x = {s, 0, 0, 0, 0, 0};
   if (s < a.n_seqs) {
     int64_t first, end;
     chunk_range(a, s, first, end);
-    const int len = sequence_len(a, s);
-    x.tiles = static_cast<int>((static_cast<uint32_t>(end - first) + a.tile_tokens - 1) / a.tile_tokens);
-    x.pages = pages_of_len(len);
+    x.first = static_cast<int>(first);                                     // (rows are below 2^31)
+    x.n = static_cast<int>(end - first);
+    x.len = min(max(a.seq_lens[s], 0), a.max_seq_len);
+    x.tiles = static_cast<int>((static_cast<uint32_t>(x.n) + a.tile_tokens - 1) / a.tile_tokens);
+    x.pages = pages_of_len(x.len);
     // (the first query's window and the others' tokens: n tokens in a row lie in (n + 126) / 128 + 1 pages at most)
     if (a.window > 0)
-      x.pages = min(x.pages, pages_of_len(min(a.n_sinks, len)) + static_cast<int>((static_cast<uint32_t>(a.window) + a.tile_tokens + 125u) / kGroup) + 1);
+      x.pages = min(x.pages, pages_of_len(min(a.n_sinks, x.len)) + static_cast<int>((static_cast<uint32_t>(a.window) + a.tile_tokens + 125u) / kGroup) + 1);
   }
   return x;
 }
@@ -180,7 +182,8 @@ __device__ __forceinline__ Sequence longest_first(const ChunkAttentionArgs& a, c
     const int other = __builtin_amdgcn_readlane(mine.pages, s);
     if (lane < a.n_seqs) rank += other > mine.pages || (other == mine.pages && s > lane) ? 1 : 0;
   }
-  return {__builtin_amdgcn_ds_permute(4 * rank, mine.index), __builtin_amdgcn_ds_permute(4 * rank, mine.tiles), __builtin_amdgcn_ds_permute(4 * rank, mine.pages)};
+  auto to_rank = [&](int x) { return __builtin_amdgcn_ds_permute(4 * rank, x); };
+  return {to_rank(mine.index), to_rank(mine.first), to_rank(mine.n), to_rank(mine.len), to_rank(mine.tiles), to_rank(mine.pages)};
 }
 // Finds part `unit` of the launch: sequences in order, `mine` the lane's of the first 64; the later tiles of one first.
 __device__ __forceinline__ bool find_item(const ChunkAttentionArgs& a, const Sequence& mine, float cut, int unit, int lane, Item& item) {
@@ -196,13 +199,11 @@ __device__ __forceinline__ bool find_item(const ChunkAttentionArgs& a, const Seq
       item.parts = __builtin_amdgcn_readlane(parts, at);
       const int from_last = place / item.parts;
       item.part = place - from_last * item.parts;
-      int64_t first, end;
-      chunk_range(a, item.seq, first, end);
-      item.row0 = first;
-      item.n = static_cast<int>(end - first);
+      item.row0 = __builtin_amdgcn_readlane(x.first, at);
+      item.n = __builtin_amdgcn_readlane(x.n, at);
       item.first = (__builtin_amdgcn_readlane(x.tiles, at) - 1 - from_last) * a.tile_tokens;
       item.count = min(a.tile_tokens, item.n - item.first);
-      item.len = sequence_len(a, item.seq);
+      item.len = __builtin_amdgcn_readlane(x.len, at);
       return true;
     }
     before = __builtin_amdgcn_readlane(upto, 63);
