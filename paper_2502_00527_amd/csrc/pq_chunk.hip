@@ -198,7 +198,6 @@ extern "C" int pq_chunk_attention(const pq_layout* layout, const void* q, pq_dty
   a.window = window;
   a.n_sinks = n_sinks;
   a.tile_tokens = p.tile_tokens;
-  a.n_items = static_cast<int32_t>(p.n_items);
   a.n_units = static_cast<int32_t>(p.n_units);
   a.cuts = p.cuts;
   a.parts = p.parts;
@@ -209,9 +208,8 @@ extern "C" int pq_chunk_attention(const pq_layout* layout, const void* q, pq_dty
   a.negate = sm_scale < 0.f ? 1 : 0;
   const dim3 grid(static_cast<uint32_t>(p.n_units * layout->n_kv_heads));
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  if (v_bits == 16) launch_chunk_v16(layout, p.rows_of_16, a, grid, stream);
-  else if (v_bits == 4) launch_chunk_v4(layout, p.rows_of_16, a, grid, stream);
-  else launch_chunk_v2(layout, p.rows_of_16, a, grid, stream);
+  const auto launch = v_bits == 16 ? launch_chunk_v16 : (v_bits == 4 ? launch_chunk_v4 : launch_chunk_v2);
+  if (!launch(layout, p.rows_of_16, a, grid, stream)) return PQ_ERR_UNSUPPORTED;
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && p.cuts) {
     const int rows = 16 * p.rows_of_16;

@@ -47,7 +47,6 @@ struct ChunkAttentionArgs {
   int32_t window;              // 0: none
   int32_t n_sinks;
   int32_t tile_tokens;         // of an item
-  int32_t n_items;             // at most
   int32_t n_units;             // places for parts of items, of a KV head
   int32_t cuts;                // whether items may be cut:
   int32_t parts;               // alike, into so many parts; 0: by what the sequences hold
@@ -68,7 +67,7 @@ namespace chunk {
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kLift = 7;
-constexpr int kMaxParts = 64;                      // of an item: a lane each when they are joined
+constexpr int kMaxParts = 64;                      // of an item: four a lane when they are joined
 constexpr int kFewLeast = 2, kSharedLeast = 4;     // pages of a part
 
 // Chunks are non-decreasing ranges of [0, n_tokens]; whatever `starts` holds, rows stay within.
