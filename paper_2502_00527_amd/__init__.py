@@ -255,14 +255,25 @@ def pq_encode_keys(layout: Layout, keys, page_ids, codes_pool, params_pool) -> N
     _check(st, "pq_encode_keys")
 
 
-def _value_pool(layout, v_pool, v_bits, v_params):
-    """Pointers of the value pool and its parameters, and the pages it holds."""
+def _check_value_params(layout: Layout, v_params, n_pages: int, name: str) -> None:
+    if v_params.numel() * v_params.element_size() < n_pages * pq_vq_params_bytes_per_page(layout):
+        raise PolarQuantError(f"{name} holds the parameters of fewer than {n_pages} pages")
+
+
+def _value_pool(layout, v_pool, v_bits, v_params, n_pages):
+    """Pointers of the value pool and its parameters, which hold at least n_pages pages."""
     import torch
     if v_bits == 16:
-        return (_dev_ptr(v_pool, "v_pool", (torch.float16,)), None,
-                v_pool.numel() * v_pool.element_size() // max(1, pq_values_bytes_per_page(layout)))
-    return (_dev_ptr(v_pool, "v_pool", (torch.uint8,)), _dev_ptr(v_params, "v_params", (torch.float16,)),
-            v_pool.numel() // max(1, pq_vq_bytes_per_page(layout, v_bits)))
+        ptrs = _dev_ptr(v_pool, "v_pool", (torch.float16,)), None
+        n_v_pages = v_pool.numel() * v_pool.element_size() // max(1, pq_values_bytes_per_page(layout))
+    else:
+        ptrs = _dev_ptr(v_pool, "v_pool", (torch.uint8,)), _dev_ptr(v_params, "v_params", (torch.float16,))
+        n_v_pages = v_pool.numel() // max(1, pq_vq_bytes_per_page(layout, v_bits))
+    if n_v_pages < n_pages:
+        raise PolarQuantError("value pool holds fewer pages than the codes pool")
+    if v_bits != 16:
+        _check_value_params(layout, v_params, n_pages, "v_params")
+    return ptrs
 
 
 def _decode_common(layout, q, codes_pool, params_pool, v_pool, block_table, seq_lens, v_bits=16, v_params=None):
@@ -270,9 +281,7 @@ def _decode_common(layout, q, codes_pool, params_pool, v_pool, block_table, seq_
     if q.dim() != 3 or q.shape[2] != layout.head_dim:
         raise PolarQuantError("q must be [n_seqs, n_q_heads, head_dim]")
     n_pool_pages = _key_pool_pages(layout, codes_pool, params_pool)
-    v_ptr, vp_ptr, n_v_pages = _value_pool(layout, v_pool, v_bits, v_params)
-    if n_v_pages < n_pool_pages:
-        raise PolarQuantError("value pool holds fewer pages than the codes pool")
+    v_ptr, vp_ptr = _value_pool(layout, v_pool, v_bits, v_params, n_pool_pages)
     return dict(
         q=_dev_ptr(q, "q"), qk=_float_kind(q, "q"), n_seqs=q.shape[0], n_q=q.shape[1],
         codes=_dev_ptr(codes_pool, "codes_pool"), params=_dev_ptr(params_pool, "params_pool"),
@@ -364,7 +373,10 @@ def pq_encode_values(layout: Layout, v_bits: int, values, page_ids, vq_pool, vq_
         raise PolarQuantError("values must be [n_tokens, n_kv_heads, head_dim]")
     if values.dtype != torch.float16 or values.stride(2) != 1 or not values.is_cuda:
         raise PolarQuantError("values must be a device fp16 tensor with a contiguous last dimension")
-    n_pool_pages = vq_pool.numel() // max(1, pq_vq_bytes_per_page(layout, v_bits))
+    page_bytes = pq_vq_bytes_per_page(layout, v_bits)                     # 0: no such width, which the library refuses
+    n_pool_pages = vq_pool.numel() // max(1, page_bytes)
+    if page_bytes > 0:
+        _check_value_params(layout, vq_params, n_pool_pages, "vq_params")
     st = load_library().pq_encode_values(
         ctypes.byref(layout), v_bits, values.data_ptr(), values.stride(0), values.stride(1), values.shape[0],
         _dev_ptr(page_ids, "page_ids", (torch.int32,)), _dev_ptr(vq_pool, "vq_pool", (torch.uint8,)),
@@ -481,9 +493,7 @@ def pq_append_chunk(layout: Layout, keys, values, starts, seq_lens, slots, resid
             raise PolarQuantError("values and slots must have as many rows as keys")
         v_args = (values.data_ptr(), values.stride(0), values.stride(1))
         slot_ptr = _dev_ptr(slots, "slots", (torch.int64,))
-        v_ptr, vp_ptr, n_v_pages = _value_pool(layout, v_pool, v_bits, v_params)
-        if n_v_pages < n_pool_pages:
-            raise PolarQuantError("value pool holds fewer pages than the codes pool")
+        v_ptr, vp_ptr = _value_pool(layout, v_pool, v_bits, v_params, n_pool_pages)
     st = load_library().pq_append_chunk(
         ctypes.byref(layout), keys.data_ptr(), _float_kind(keys, "keys"), keys.stride(0), keys.stride(1), *v_args, keys.shape[0], n,
         _dev_ptr(starts, "starts", (torch.int32,)), _dev_ptr(seq_lens, "seq_lens", (torch.int32,)), slot_ptr,

@@ -101,6 +101,11 @@ int64_t key_pool_pages(const pq_layout* l, const at::Tensor& codes, const at::Te
   if (bytes_of(params) < static_cast<size_t>(n) * pq_params_bytes_per_page(l)) throw Decline{};
   return n;
 }
+// Parameters of quantized values, of at least n_pages pages.
+void* value_params(const pq_layout* l, const at::Tensor& params, int64_t n_pages) {
+  if (bytes_of(params) < static_cast<size_t>(n_pages) * pq_vq_params_bytes_per_page(l)) throw Decline{};
+  return params.data_ptr();
+}
 void check_rows(const at::Tensor& t, const pq_layout* l, bool heads) {
   if (t.dim() != 3 || t.size(2) != l->head_dim || (heads && t.size(1) != l->n_kv_heads)) throw Decline{};
 }
@@ -142,7 +147,7 @@ PyObject* decode_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (v_bits == 16) {
       v_pages = pages(bytes_of(v), pq_values_bytes_per_page(l));
     } else {
-      v_params = contiguous_tensor(a[14], at::kHalf).data_ptr();
+      v_params = value_params(l, contiguous_tensor(a[14], at::kHalf), n_pages);
       v_pages = pages(bytes_of(v), pq_vq_bytes_per_page(l, v_bits));
     }
     if (v_pages < n_pages) throw Decline{};
@@ -229,7 +234,7 @@ PyObject* encode_values(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int32_t* const ids = static_cast<const int32_t*>(contiguous_tensor(a[3], at::kInt).data_ptr());
     const at::Tensor &pool = contiguous_tensor(a[4], at::kByte), &params = contiguous_tensor(a[5], at::kHalf);
     const int64_t n_pages = pages(bytes_of(pool), pq_vq_bytes_per_page(l, v_bits));
-    void *const vp = values.data_ptr(), *const qp = pool.data_ptr(), *const pp = params.data_ptr(), *const stream = current_stream();
+    void *const vp = values.data_ptr(), *const qp = pool.data_ptr(), *const pp = value_params(l, params, n_pages), *const stream = current_stream();
     const int64_t token_stride = values.stride(0), head_stride = values.stride(1), tokens = values.size(0);
     return without_lock([&] { return pq_encode_values(l, v_bits, vp, token_stride, head_stride, tokens, ids, qp, pp, n_pages, stream); });
   });
@@ -274,7 +279,7 @@ struct ValuePool {
     if (v_bits != 16) {
       const at::Tensor& p = contiguous_tensor(v_params, at::kHalf);
       if (p.device() != v.device()) throw Decline{};
-      params = p.data_ptr();
+      params = value_params(l, p, n_pages);
     }
     if (pages(bytes_of(v), v_bits == 16 ? pq_values_bytes_per_page(l) : pq_vq_bytes_per_page(l, v_bits)) < n_pages) throw Decline{};
     pool = v.data_ptr();
