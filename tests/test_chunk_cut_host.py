@@ -115,3 +115,23 @@ def test_every_page_is_in_one_part(lib, seed):
 def test_chunks_that_are_shorter_than_the_rows_and_sequences_without(lib):
     Launch(lib, [5000, 0, 700], [5, 0, 3], 8, rows=64).check()
     Launch(lib, [40, 300], [60, 0], 2).check()                          # a chunk longer than its sequence
+
+
+def fitting(launch):
+    """The shortest parts that fit the launch's places, by trying all lengths."""
+    pages = [((n + G - 1) // G, len([1 for s, _ in launch.tiles if s == seq])) for seq, n in enumerate(launch.lens)]
+    longest = max(p for p, _ in pages)
+    for per in range(max(FEW_LEAST, -(-longest // MOST_PARTS)), longest):
+        if sum(tiles * max(1, -(-p // per)) for p, tiles in pages) <= launch.units:
+            return per
+    return longest
+
+
+@pytest.mark.parametrize("kv_heads,seqs,lens", [*[(8, n, [1024 * G] + [G] * (n - 1)) for n in (46, 48, 50, 56, 60, 61, 62)], (32, 13, [4000 * G] + [3 * G] * 12),
+                                                (1, 400, [2000 * G] + [G] * 399), (8, 4, [8192 * G] * 4), (8, 40, [700 * G, 300 * G] + [2 * G] * 38),
+                                                (2, 200, [3000 * G] * 3 + [100] * 197)])
+def test_one_long_sequence_among_short_ones_is_cut_as_far_as_there_are_places(lib, kv_heads, seqs, lens):
+    """Few rows: parts are within a step of the search (1 / 16) of the shortest ones that fit."""
+    launch = Launch(lib, lens, [1] * seqs, kv_heads).check()
+    assert launch.rows_of_16 == 1 and launch.cuts
+    assert launch.longest_part() <= fitting(launch) * 17 / 16 + 2, (launch.longest_part(), fitting(launch))
