@@ -294,6 +294,7 @@ int pq_decode_merges_in_kernel(const pq_layout* layout, int32_t n_seqs, int32_t 
  *   seq_lens      device int32 [n_seqs]; a negative length skips the sequence
  *   A group whose page index is >= max_pages_per_seq or whose page id is outside the pool is not
  *   encoded (nothing is written to the pools).
+ *   Tokens that are dropped again: see "chunks of new tokens" below.
  */
 int pq_append_keys(const pq_layout* layout, const void* new_keys, pq_dtype key_dtype, int32_t n_seqs,
                    void* residual, const int32_t* seq_lens, const int32_t* block_table,
@@ -310,6 +311,18 @@ int pq_append_keys(const pq_layout* layout, const void* new_keys, pq_dtype key_d
  * Nothing is read back by the host between them, and all three may be captured in a graph.  The tokens of a batch are
  * rows [0, n_tokens) of its tensors, sequence s's chunk is rows [starts[s], starts[s + 1]); a
  * sequence may have none.  Rows from starts[n_seqs] on (padding) belong to nobody.
+ *
+ * Tokens that are dropped again (drafts that were not accepted): the next calls are given lower lengths.  The residual buffer
+ * holds the keys of ONE incomplete group, so that after an append (or several pq_append_keys) a length may go back
+ *   - to anywhere in the incomplete group that the append has left, and
+ *   - to the end of any complete group (a multiple of g),
+ * but not into a group that the append has completed: the keys of the group behind it stand in the first rows of the
+ * buffer by then, and attention would take them for the other group's.  Nothing reports that.  Where drafts may complete
+ * a group, they are appended and attended to with a COPY of the residual buffer; when it is known which are accepted, these alone, their rows
+ * gathered, are appended to the buffer itself, from the same seq_lens (values == NULL: theirs have been filed).  What is left then is what the accepted
+ * tokens alone would have left, whatever was dropped.
+ * Pages whose tokens were all dropped, block_table[s][ceil(len / g)] and on, are the caller's to use again:
+ * pq_plan_pages takes new ones when tokens reach there.
  */
 
 /*
