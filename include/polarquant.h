@@ -355,6 +355,8 @@ int pq_plan_pages(const pq_layout* layout, const int32_t* seq_lens, const int32_
  * pq_append_chunk -- pq_append_keys for any number of new tokens per sequence, and their values.  The caches' keys are
  * byte for byte what pq_append_keys makes of the same keys token by token: complete groups in the packed pages, the
  * rest as fp16 rows in the residual buffer, whose rows behind the last token are left as they were.
+ * PQ_F32 keys are rounded to fp16 first, as pq_append_keys rounds them; pq_encode_keys takes them as they are, so that the
+ * same fp32 prompt may get other codes and parameters there.
  *
  *   keys          device, PQ_F16 or PQ_F32, element i of KV head h of row n at keys[n * key_token_stride + h *
  *                 key_head_stride + i] (strides in elements, multiples of 16 bytes; 16-byte aligned)
