@@ -395,8 +395,11 @@ size_t pq_chunk_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_t
  *
  *   q             device fp16 [n_tokens][n_q_heads][d], post-RoPE (16-byte aligned; PQ_F32: PQ_ERR_UNSUPPORTED).  Query head h reads
  *                 KV head h / (n_q_heads / n_kv_heads); the ratio may be 1 .. 16
- *   n_tokens      rows of q and out.  Which kernel runs goes by n_tokens / n_seqs: padding beyond what the chunks need is
- *                 not computed, but a call sized for it may get the kernel for many rows
+ *   n_tokens      rows of q and out.  Which kernel runs goes by n_tokens / n_seqs, for the whole batch: padding beyond what the chunks need is
+ *                 not computed, but a call sized for it may get the kernel for many rows, and single tokens beside long chunks
+ *                 take longer than in a call of their own (63 of them and a chunk of 1024, all over 4000 tokens: 251 us against 111 + 111).
+ *                 With the single tokens' a sequences first: one call over these with n_tokens = their rows, and one with starts + a, seq_lens + a,
+ *                 block_table and residual_keys from sequence a on, and q, out and n_tokens as they are
  *   starts        device int32 [n_seqs + 1] (pq_plan_pages); non-decreasing, within [0, n_tokens]
  *   seq_lens      device int32 [n_seqs]: lengths WITH the chunks (pq_plan_pages' lens_after); above max_seq_len they are
  *                 treated as max_seq_len.  A query that would stand before the sequence's first token gets a row of zeros
@@ -410,6 +413,8 @@ size_t pq_chunk_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_t
  * Softmax statistics and sums are fp32.  Reconstructed keys, probabilities and de-quantized values enter the matrix products as
  * fp16, each rounded once; keys (made in fp32; the levels of the grouped quantizer are fp16 too) with the scale in them, times sm_scale
  * log2(e): that product has to lie in fp16's range.  Keys, and values of all tokens of a page that is seen, must be finite.
+ * Long sequences are cut into parts, by the lengths that the device finds, while a batch has few tiles of rows: below 512 / n_kv_heads sequences of up to 32
+ * rows (new tokens times query heads per KV head) each, for instance.  In larger batches one sequence far longer than the others is a work-group's alone.
  * n_tokens == 0 is a no-op.
  */
 int pq_chunk_attention(const pq_layout* layout, const void* q, pq_dtype q_dtype, int64_t n_tokens, int32_t n_seqs,

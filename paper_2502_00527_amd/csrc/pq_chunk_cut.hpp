@@ -15,9 +15,10 @@ __device__ __forceinline__ void chunk_range(const ChunkAttentionArgs& a, int s, 
 }
 
 // ---- how a launch is shared out: by every wavefront alike, a sequence a lane, from what the sequences really hold --------------------
-// Items are tiles of tile_tokens of a sequence's chunk; the pages that one sees are cut into parts of alike length, a work-group each.
-// A sequence's tiles see about the same pages, so they have the same number of parts.  Lengths are known here only, and max_seq_len may be far
-// above them: cut by what there is, and with many rows the longest first, 12 chunks of 1 .. 700 tokens over up to 8192 take 403 us, cut
+// Items are tiles of tile_tokens of a sequence's chunk; the pages that one sees are cut into parts of alike length, a work-group each, in
+// launches that the host lets be cut (plan_launch: few items).  A sequence's tiles are taken to see the same pages, its chunk's last tile's, and have the same
+// number of parts: a chunk with little before it sees half of that in the mean.  Lengths are known here only, and max_seq_len may be far
+// above them: cut by what there is, and with many rows and up to 64 sequences the longest first, 12 chunks of 1 .. 700 tokens over up to 8192 take 403 us, cut
 // by the host as if all were as long as the longest 483; 16 x 5 tokens over 500 .. 6000 41 against 46 (37 now).  Where all are alike
 // that costs 1 .. 3 us a work-group (16 x 128 tokens over 4000 164 against 153).
 struct Sequence {
