@@ -444,6 +444,126 @@ int pq_window_attention(const pq_layout* layout, const void* q, pq_dtype q_dtype
                         size_t workspace_bytes, void* hip_stream);
 
 /*
+ * ---- long caches under a budget of pages --------------------------------------------------------
+ * A step may read a part of a long cache (pq_sparse_attention: each KV head the pages that its queries are likely to
+ * look at), or a cache may keep a part of what came in (pq_evict_pages: the pages that have been looked at most).  Both go
+ * by whole pages, the groups of the quantizer.  All of these calls may be captured in a graph, and none is read back by the host.
+ *
+ * Bounds of a page (bounds pool, bound scales pool), of one KV head: with lo_i and hi_i the smallest and largest element of channel i
+ * of the reconstructed keys over the page's tokens, in blocks of 32 channels -- block b is pairs 16 b .. 16 b + 15, both coordinates --
+ *   M_b = largest |lo_i|, |hi_i|,  scale_b = M_b / 127,  c_i = round((lo_i + hi_i) / 2 * (127 / M_b)),  w_i = round((hi_i - lo_i) / 2 * (127 / M_b))
+ *   (c_i = w_i = 0 where M_b < 2^-100; every operation rounded to fp32, round half to even; cos and sin of an angle level are
+ *   taken in float64 and rounded once)
+ *   bounds pool : [page][kv_head][block 4]{int8 c of 16 x, c of 16 y, w of 16 x, w of 16 y}
+ *   scales pool : [page][kv_head][block 4] fp32
+ */
+size_t pq_bounds_bytes_per_page(const pq_layout* layout);
+size_t pq_bound_scales_bytes_per_page(const pq_layout* layout);
+
+/*
+ * pq_bound_pages -- bounds of the pages that sequences have completed: of sequence s its groups floor(lens_before[s] / g) ..
+ * floor(lens_after[s] / g) - 1, from their packed codes (after pq_encode_keys, pq_append_keys or pq_append_chunk).
+ * An incomplete group has none: pq_select_pages always takes the last page.
+ *
+ *   lens_before     device int32 [n_seqs], or NULL: 0; a negative length counts as 0
+ *   lens_after      device int32 [n_seqs]
+ *   max_new_tokens  host-known upper bound of lens_after - lens_before; groups past what so many tokens can complete get no bounds
+ *   bounds, bound_scales   device (16-byte aligned), written for the named pages only; page ids outside [0, n_pool_pages) are skipped, and so are
+ *                   pages past max_pages_per_seq
+ * n_seqs == 0 or max_new_tokens == 0 is a no-op.
+ */
+int pq_bound_pages(const pq_layout* layout, const void* codes_pool, const void* params_pool, int64_t n_pool_pages,
+                   const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* lens_before, const int32_t* lens_after,
+                   int32_t n_seqs, int32_t max_new_tokens, void* bounds, void* bound_scales, void* hip_stream);
+
+/* Bytes of scratch pq_select_pages needs (256-byte aligned device memory); 0 on invalid arguments. */
+size_t pq_select_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_t max_seq_len);
+
+/*
+ * pq_select_pages -- the pages that each KV head of each sequence reads for the present queries: the first n_first, the last n_last, and of the
+ * others those of the largest scores, n_selected in all (all pages of a sequence that has no more).  The score of a page is, up to rounding
+ * and a factor of 127, the largest q . k that a key within its bounds could have with any of the KV head's queries.  In whole numbers, with
+ * m_b = largest |q_i| of a block over the KV head's query heads, q8_i = round(q_i * (127 / m_b)) (0 where m_b < 2^-100) and
+ * u_b = m_b scale_b:  (n_0 u_0 + n_1 u_1) + (n_2 u_2 + n_3 u_3),  n_b = sum over the block of q8_i c_i + |q8_i| w_i,  the largest of the query
+ * heads; every operation rounded to fp32, so that the choice does not depend on how a launch is shared out.  Among equals the first pages.
+ *
+ *   q               device [n_seqs][n_q_heads][d], q_dtype PQ_F16 or PQ_F32 (16-byte aligned); n_q_heads / n_kv_heads 1 .. 16
+ *   bounds, bound_scales   of every page but the last n_last and the first n_first
+ *   block_table, seq_lens, max_seq_len, n_pool_pages   as in pq_decode_attention.  A page whose entry is outside the pool scores -infinity
+ *   n_selected      >= n_first + n_last;  n_first >= 0, n_last >= 1
+ *   selected        device int32 [n_seqs][n_kv_heads][n_selected], written: page * n_kv_heads + kv_head of each chosen page in the order of
+ *                   the sequence, -1 if the entry is outside the pool and behind the last one.  That is a block table of n_seqs *
+ *                   n_kv_heads sequences over the same pools seen as n_pool_pages * n_kv_heads pages of one KV head
+ *   selected_lens   device int32 [n_seqs][n_kv_heads], written: tokens in the chosen pages (the last of them is the sequence's last)
+ *   workspace       >= pq_select_workspace_bytes(...); contents are scratch.  Calls that overlap need one each, captured ones too
+ * n_seqs * n_kv_heads <= 65535, n_pool_pages * n_kv_heads < 2^31 (PQ_ERR_UNSUPPORTED beyond).
+ */
+int pq_select_pages(const pq_layout* layout, const void* q, pq_dtype q_dtype, int32_t n_seqs, int32_t n_q_heads, const void* bounds,
+                    const void* bound_scales, int64_t n_pool_pages, const int32_t* block_table, int32_t max_pages_per_seq,
+                    const int32_t* seq_lens, int32_t max_seq_len, int32_t n_selected, int32_t n_first, int32_t n_last,
+                    int32_t* selected, int32_t* selected_lens, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Bytes of scratch pq_sparse_attention needs (256-byte aligned device memory); 0 on invalid arguments. */
+size_t pq_sparse_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_t n_q_heads, int32_t max_seq_len, int32_t n_selected);
+
+/*
+ * pq_sparse_attention -- pq_select_pages, and decode attention over the chosen pages.  Arguments as in pq_select_pages and
+ * pq_decode_attention (raw scores apart); results are pq_decode_attention's over the tokens of the chosen pages, in precision too.  A sequence of
+ * no more than n_selected pages gets attention over all of it.
+ *   bounds, bound_scales   both NULL: `selected` and `selected_lens` are given, as pq_select_pages wrote them for the same lengths (the choice
+ *                   of another layer, say); block_table, seq_lens, n_first and n_last are then not looked at (the first two may be NULL)
+ *   workspace       >= pq_sparse_workspace_bytes(...)
+ */
+int pq_sparse_attention(const pq_layout* layout, const void* q, pq_dtype q_dtype, int32_t n_seqs, int32_t n_q_heads, const void* codes_pool,
+                        const void* params_pool, const void* v_pool, int32_t v_bits, const void* v_params_pool, const void* bounds,
+                        const void* bound_scales, int64_t n_pool_pages, const int32_t* block_table, int32_t max_pages_per_seq,
+                        const int32_t* seq_lens, int32_t max_seq_len, int32_t n_selected, int32_t n_first, int32_t n_last, float sm_scale,
+                        int32_t* selected, int32_t* selected_lens, float* out, const void* residual_keys, void* workspace,
+                        size_t workspace_bytes, void* hip_stream);
+
+/* Bytes of scratch pq_decode_attention_weights needs (256-byte aligned device memory); 0 on invalid arguments. */
+size_t pq_weights_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_t n_q_heads, int32_t max_seq_len);
+
+/*
+ * pq_decode_attention_weights -- pq_decode_attention, and what it looked at: the softmax weights of each page's tokens, summed over them and over
+ * all query heads, are added to what earlier steps left,
+ *   weights[s][p] = decay * weights_before[s][p] + sum over query heads and tokens of page p
+ *
+ *   weights_before  device fp32 [n_seqs][weights_stride], or NULL: 0 (decay == 0 does not read it either); may be `weights`
+ *   weights         device fp32 [n_seqs][weights_stride], written for the pages that a sequence has, others are left as they were;
+ *                   weights_stride >= ceil(max_seq_len / g)
+ *   the others      as in pq_decode_attention (raw scores apart), `out` in its precision; weights are sums of fp32 exponentials
+ *   workspace       >= pq_weights_workspace_bytes(...).  Calls that overlap need one each, captured ones too
+ */
+int pq_decode_attention_weights(const pq_layout* layout, const void* q, pq_dtype q_dtype, int32_t n_seqs, int32_t n_q_heads,
+                                const void* codes_pool, const void* params_pool, const void* v_pool, int32_t v_bits,
+                                const void* v_params_pool, int64_t n_pool_pages, const int32_t* block_table, int32_t max_pages_per_seq,
+                                const int32_t* seq_lens, int32_t max_seq_len, float sm_scale, float* out, const float* weights_before,
+                                float decay, float* weights, int64_t weights_stride, const void* residual_keys, void* workspace,
+                                size_t workspace_bytes, void* hip_stream);
+
+/*
+ * pq_evict_pages -- sequences of more than n_kept pages give up those of the smallest weights, but for the first n_first, the last n_last and an
+ * incomplete one, until n_kept are left (or all that are spared).  Among equal weights the first pages go; a NaN counts as
+ * the largest weight.  The other pages move together in the order they had; later calls see a shorter sequence.  The keys keep the positions
+ * they were rotated to, and so does the residual buffer's group: lengths change by multiples of g.
+ *
+ *   block_table     device int32 [n_seqs][max_pages_per_seq]
+ *   seq_lens        device int32 [n_seqs]; a length <= 0 has no pages; one of more than max_pages_per_seq pages gives up none
+ *   weights         device fp32 [n_seqs][weights_stride], weights_stride >= max_pages_per_seq (pq_decode_attention_weights)
+ *   table_after, weights_after   like block_table and weights, and may be them (otherwise they may not overlap); written for the pages that a sequence
+ *                   had: those that are left, then -1 and weights of 0
+ *   lens_after      device int32 [n_seqs], written: tokens that are left; not seq_lens
+ *   freed           device int32 [n_freed], written: block-table entries of the pages given up, sequence by sequence and in each from its
+ *                   beginning, as they were (-1 where a page was missing); as far as n_freed.  free_pages of a later pq_plan_pages
+ *   counts          device int32 [1], written: pages given up
+ * n_seqs <= 65535.  No workspace; calls that overlap share nothing but their outputs.
+ */
+int pq_evict_pages(const pq_layout* layout, const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* seq_lens, int32_t n_seqs,
+                   const float* weights, int64_t weights_stride, int32_t n_kept, int32_t n_first, int32_t n_last, int32_t* table_after,
+                   int32_t* lens_after, float* weights_after, int32_t* freed, int32_t n_freed, int32_t* counts, void* hip_stream);
+
+/*
  * pq_score_keys -- the query-key product alone: raw scores q . k~ of every cached token
  * through the lookup table (Section 3.3, Appendix A).  This is the operation whose latency
  * the paper reports in Section 5.2 (query-key multiplication kernel).  Arguments as in

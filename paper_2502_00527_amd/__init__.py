@@ -32,6 +32,8 @@ __all__ = [
     "pq_decode_attention_static", "PQ_STATIC_SCRATCH_BYTES",
     "pq_plan_pages", "pq_append_chunk", "pq_chunk_attention", "pq_chunk_workspace_bytes",
     "pq_window_attention", "pq_window_workspace_bytes",
+    "pq_bounds_bytes_per_page", "pq_bound_scales_bytes_per_page", "pq_bound_pages", "pq_select_pages", "pq_select_workspace_bytes",
+    "pq_sparse_attention", "pq_sparse_workspace_bytes", "pq_decode_attention_weights", "pq_weights_workspace_bytes", "pq_evict_pages",
 ]
 
 PQ_F16, PQ_F32 = 0, 1
@@ -103,6 +105,23 @@ _SIGNATURES = {
     "pq_window_attention": (c_int, [_LP, c_void_p, c_int, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_void_p, c_int64,
                                     c_void_p, c_int32, c_void_p, c_int32, c_int32, c_int32, c_float, c_void_p, c_void_p, c_void_p,
                                     c_size_t, c_void_p]),
+    "pq_bounds_bytes_per_page": (c_size_t, [_LP]),
+    "pq_bound_scales_bytes_per_page": (c_size_t, [_LP]),
+    "pq_bound_pages": (c_int, [_LP, c_void_p, c_void_p, c_int64, c_void_p, c_int32, c_void_p, c_void_p, c_int32, c_int32, c_void_p,
+                               c_void_p, c_void_p]),
+    "pq_select_workspace_bytes": (c_size_t, [_LP, c_int32, c_int32]),
+    "pq_select_pages": (c_int, [_LP, c_void_p, c_int, c_int32, c_int32, c_void_p, c_void_p, c_int64, c_void_p, c_int32, c_void_p, c_int32,
+                                c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "pq_sparse_workspace_bytes": (c_size_t, [_LP, c_int32, c_int32, c_int32, c_int32]),
+    "pq_sparse_attention": (c_int, [_LP, c_void_p, c_int, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_void_p, c_void_p,
+                                    c_void_p, c_int64, c_void_p, c_int32, c_void_p, c_int32, c_int32, c_int32, c_int32, c_float, c_void_p,
+                                    c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "pq_weights_workspace_bytes": (c_size_t, [_LP, c_int32, c_int32, c_int32]),
+    "pq_decode_attention_weights": (c_int, [_LP, c_void_p, c_int, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_void_p, c_int64,
+                                            c_void_p, c_int32, c_void_p, c_int32, c_float, c_void_p, c_void_p, c_float, c_void_p, c_int64,
+                                            c_void_p, c_void_p, c_size_t, c_void_p]),
+    "pq_evict_pages": (c_int, [_LP, c_void_p, c_int32, c_void_p, c_int32, c_void_p, c_int64, c_int32, c_int32, c_int32, c_void_p, c_void_p,
+                               c_void_p, c_void_p, c_int32, c_void_p, c_void_p]),
     "pq_probe_read_stream": (c_int, [c_void_p, c_size_t, c_void_p, c_void_p]),
 }
 
@@ -133,6 +152,7 @@ class _ByCtypes:
 
     decode_attention = score_keys = encode_keys = encode_values = append_keys = _decline
     plan_pages = append_chunk = chunk_attention = window_attention = _decline
+    bound_pages = select_pages = sparse_attention = decode_attention_weights = evict_pages = _decline
 
 
 def _marshaller():
@@ -563,6 +583,203 @@ def pq_window_attention(layout: Layout, q, codes_pool, params_pool, v_pool, bloc
         None if residual is None else _dev_ptr(residual, "residual", (torch.float16,)),
         _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream())
     _check(st, "pq_window_attention")
+
+
+def pq_bounds_bytes_per_page(layout: Layout) -> int:
+    return load_library().pq_bounds_bytes_per_page(ctypes.byref(layout))
+
+
+def pq_bound_scales_bytes_per_page(layout: Layout) -> int:
+    return load_library().pq_bound_scales_bytes_per_page(ctypes.byref(layout))
+
+
+def _bound_pools(layout: Layout, bounds, bound_scales, n_pages: int):
+    """Pointers of the bounds and their scales, which hold at least n_pages pages."""
+    import torch
+    ptrs = _dev_ptr(bounds, "bounds", (torch.int8,)), _dev_ptr(bound_scales, "bound_scales", (torch.float32,))
+    if (bounds.numel() < n_pages * pq_bounds_bytes_per_page(layout)
+            or bound_scales.numel() * 4 < n_pages * pq_bound_scales_bytes_per_page(layout)):
+        raise PolarQuantError(f"bounds and bound_scales must hold {n_pages} pages")
+    return ptrs
+
+
+def _one_row_each(n: int, block_table, seq_lens) -> None:
+    if block_table.dim() != 2 or block_table.shape[0] != n or seq_lens.numel() != n:
+        raise PolarQuantError("block_table must be [n_seqs, pages], seq_lens [n_seqs]")
+
+
+def pq_bound_pages(layout: Layout, codes_pool, params_pool, block_table, lens_before, lens_after, max_new_tokens: int, bounds,
+                   bound_scales) -> None:
+    """Bounds of the pages that sequences have completed; see include/polarquant.h.  lens_before (or None) and lens_after int32
+    [n_seqs]; `bounds` int8 and `bound_scales` fp32, of as many pages as the pools: [pages, n_kv_heads, 4, 64] and
+    [pages, n_kv_heads, 4]."""
+    if _done((_calls or _marshaller()).bound_pages(
+            layout, codes_pool, params_pool, block_table, lens_before, lens_after, max_new_tokens, bounds, bound_scales), "pq_bound_pages"):
+        return
+    import torch
+    i32 = (torch.int32,)
+    _on_current_device(codes_pool=codes_pool, params_pool=params_pool, block_table=block_table, lens_before=lens_before, lens_after=lens_after,
+                       bounds=bounds, bound_scales=bound_scales)
+    n = lens_after.numel()
+    _one_row_each(n, block_table, lens_after)
+    if lens_before is not None and lens_before.numel() != n:
+        raise PolarQuantError("lens_before must be [n_seqs]")
+    n_pool_pages = _key_pool_pages(layout, codes_pool, params_pool)
+    b_ptr, s_ptr = _bound_pools(layout, bounds, bound_scales, n_pool_pages)
+    st = load_library().pq_bound_pages(
+        ctypes.byref(layout), _dev_ptr(codes_pool, "codes_pool"), _dev_ptr(params_pool, "params_pool"), n_pool_pages,
+        _dev_ptr(block_table, "block_table", i32), block_table.shape[1],
+        None if lens_before is None else _dev_ptr(lens_before, "lens_before", i32), _dev_ptr(lens_after, "lens_after", i32), n,
+        max_new_tokens, b_ptr, s_ptr, _stream())
+    _check(st, "pq_bound_pages")
+
+
+def pq_select_workspace_bytes(layout: Layout, n_seqs: int, max_seq_len: int) -> int:
+    return load_library().pq_select_workspace_bytes(ctypes.byref(layout), n_seqs, max_seq_len)
+
+
+def _selection(layout: Layout, n_seqs: int, selected, selected_lens):
+    """Pointers of a choice of pages, and how many pages a row has."""
+    import torch
+    ptrs = _dev_ptr(selected, "selected", (torch.int32,)), _dev_ptr(selected_lens, "selected_lens", (torch.int32,))
+    if selected.dim() != 3 or tuple(selected.shape[:2]) != (n_seqs, layout.n_kv_heads) or selected_lens.numel() != n_seqs * layout.n_kv_heads:
+        raise PolarQuantError("selected must be [n_seqs, n_kv_heads, pages], selected_lens [n_seqs, n_kv_heads]")
+    return *ptrs, selected.shape[2]
+
+
+def pq_select_pages(layout: Layout, q, bounds, bound_scales, block_table, seq_lens, max_seq_len: int, n_first: int, n_last: int, selected,
+                    selected_lens, workspace) -> None:
+    """The pages that each KV head reads for the present queries; see include/polarquant.h.  q [n_seqs, n_q_heads, d] fp16/fp32;
+    `selected` int32 [n_seqs, n_kv_heads, n_selected] and `selected_lens` int32 [n_seqs, n_kv_heads] are written; `workspace` a uint8
+    device tensor of at least pq_select_workspace_bytes(...) bytes."""
+    if _done((_calls or _marshaller()).select_pages(
+            layout, q, bounds, bound_scales, block_table, seq_lens, max_seq_len, n_first, n_last, selected, selected_lens, workspace),
+            "pq_select_pages"):
+        return
+    import torch
+    i32 = (torch.int32,)
+    _on_current_device(q=q, bounds=bounds, bound_scales=bound_scales, block_table=block_table, seq_lens=seq_lens, selected=selected,
+                       selected_lens=selected_lens, workspace=workspace)
+    if q.dim() != 3 or q.shape[2] != layout.head_dim:
+        raise PolarQuantError("q must be [n_seqs, n_q_heads, head_dim]")
+    _one_row_each(q.shape[0], block_table, seq_lens)
+    n_pool_pages = bounds.numel() // max(1, pq_bounds_bytes_per_page(layout))
+    b_ptr, s_ptr = _bound_pools(layout, bounds, bound_scales, n_pool_pages)
+    sel_ptr, len_ptr, n_selected = _selection(layout, q.shape[0], selected, selected_lens)
+    st = load_library().pq_select_pages(
+        ctypes.byref(layout), _dev_ptr(q, "q"), _float_kind(q, "q"), q.shape[0], q.shape[1], b_ptr, s_ptr, n_pool_pages,
+        _dev_ptr(block_table, "block_table", i32), block_table.shape[1], _dev_ptr(seq_lens, "seq_lens", i32), max_seq_len, n_selected,
+        n_first, n_last, sel_ptr, len_ptr, _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream())
+    _check(st, "pq_select_pages")
+
+
+def pq_sparse_workspace_bytes(layout: Layout, n_seqs: int, n_q_heads: int, max_seq_len: int, n_selected: int) -> int:
+    return load_library().pq_sparse_workspace_bytes(ctypes.byref(layout), n_seqs, n_q_heads, max_seq_len, n_selected)
+
+
+def pq_sparse_attention(layout: Layout, q, codes_pool, params_pool, v_pool, bounds, bound_scales, block_table, seq_lens, max_seq_len: int,
+                        n_first: int, n_last: int, sm_scale: float, selected, selected_lens, out, workspace, residual=None,
+                        v_bits: int = 16, v_params=None) -> None:
+    """pq_select_pages, and decode attention over the chosen pages; see include/polarquant.h.  `out` fp32 [n_seqs, n_q_heads, d].  With
+    bounds and bound_scales None, `selected` and `selected_lens` are given (and block_table and seq_lens may be None)."""
+    if _done((_calls or _marshaller()).sparse_attention(
+            layout, q, codes_pool, params_pool, v_pool, bounds, bound_scales, block_table, seq_lens, max_seq_len, n_first, n_last, sm_scale,
+            selected, selected_lens, out, workspace, residual, v_bits, v_params), "pq_sparse_attention"):
+        return
+    import torch
+    i32 = (torch.int32,)
+    _on_current_device(q=q, codes_pool=codes_pool, params_pool=params_pool, v_pool=v_pool, bounds=bounds, bound_scales=bound_scales,
+                       block_table=block_table, seq_lens=seq_lens, selected=selected, selected_lens=selected_lens, out=out, workspace=workspace,
+                       residual=residual, v_params=v_params)
+    if q.dim() != 3 or q.shape[2] != layout.head_dim or out.shape != q.shape:
+        raise PolarQuantError("q must be [n_seqs, n_q_heads, head_dim], out of its shape")
+    if (bounds is None) != (bound_scales is None):
+        raise PolarQuantError("bounds and bound_scales must be given both, or neither")
+    n = q.shape[0]
+    n_pool_pages = _key_pool_pages(layout, codes_pool, params_pool)
+    v_ptr, vp_ptr = _value_pool(layout, v_pool, v_bits, v_params, n_pool_pages)
+    sel_ptr, len_ptr, n_selected = _selection(layout, n, selected, selected_lens)
+    b_ptr = s_ptr = table_ptr = lens_ptr = None
+    width = 0
+    if bounds is not None:
+        _one_row_each(n, block_table, seq_lens)
+        b_ptr, s_ptr = _bound_pools(layout, bounds, bound_scales, n_pool_pages)
+        table_ptr, width, lens_ptr = _dev_ptr(block_table, "block_table", i32), block_table.shape[1], _dev_ptr(seq_lens, "seq_lens", i32)
+    _check_residual(layout, residual, n)
+    st = load_library().pq_sparse_attention(
+        ctypes.byref(layout), _dev_ptr(q, "q"), _float_kind(q, "q"), n, q.shape[1], _dev_ptr(codes_pool, "codes_pool"),
+        _dev_ptr(params_pool, "params_pool"), v_ptr, v_bits, vp_ptr, b_ptr, s_ptr, n_pool_pages, table_ptr, width, lens_ptr, max_seq_len,
+        n_selected, n_first, n_last, sm_scale, sel_ptr, len_ptr, _dev_ptr(out, "out", (torch.float32,)),
+        None if residual is None else _dev_ptr(residual, "residual", (torch.float16,)),
+        _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream())
+    _check(st, "pq_sparse_attention")
+
+
+def pq_weights_workspace_bytes(layout: Layout, n_seqs: int, n_q_heads: int, max_seq_len: int) -> int:
+    return load_library().pq_weights_workspace_bytes(ctypes.byref(layout), n_seqs, n_q_heads, max_seq_len)
+
+
+def _page_weights(n: int, name: str, t):
+    import torch
+    ptr = _dev_ptr(t, name, (torch.float32,))
+    if t.dim() != 2 or t.shape[0] != n:
+        raise PolarQuantError(f"{name} must be [n_seqs, pages]")
+    return ptr
+
+
+def pq_decode_attention_weights(layout: Layout, q, codes_pool, params_pool, v_pool, block_table, seq_lens, max_seq_len: int, sm_scale: float,
+                                out, weights, workspace, weights_before=None, decay: float = 1.0, residual=None, v_bits: int = 16,
+                                v_params=None) -> None:
+    """pq_decode_attention, and each page's softmax weights summed over its tokens and all query heads; see include/polarquant.h.
+    `weights` fp32 [n_seqs, stride >= pages of max_seq_len] = decay * weights_before (None: 0; may be `weights`) + those sums;
+    `workspace` of at least pq_weights_workspace_bytes(...) bytes."""
+    if _done((_calls or _marshaller()).decode_attention_weights(
+            layout, q, codes_pool, params_pool, v_pool, block_table, seq_lens, max_seq_len, sm_scale, out, weights, workspace, weights_before,
+            decay, residual, v_bits, v_params), "pq_decode_attention_weights"):
+        return
+    import torch
+    _on_current_device(q=q, codes_pool=codes_pool, params_pool=params_pool, v_pool=v_pool, block_table=block_table, seq_lens=seq_lens, out=out,
+                       weights=weights, workspace=workspace, weights_before=weights_before, residual=residual, v_params=v_params)
+    c = _decode_common(layout, q, codes_pool, params_pool, v_pool, block_table, seq_lens, v_bits, v_params)
+    _one_row_each(c["n_seqs"], block_table, seq_lens)
+    if out.shape != q.shape:
+        raise PolarQuantError("out must have q's shape")
+    w_ptr = _page_weights(c["n_seqs"], "weights", weights)
+    before_ptr = None if weights_before is None else _page_weights(c["n_seqs"], "weights_before", weights_before)
+    if weights_before is not None and weights_before.shape != weights.shape:
+        raise PolarQuantError("weights_before must have the shape of weights")
+    _check_residual(layout, residual, c["n_seqs"])
+    st = load_library().pq_decode_attention_weights(
+        ctypes.byref(layout), c["q"], c["qk"], c["n_seqs"], c["n_q"], c["codes"], c["params"], c["v"], c["vbits"], c["vpar"],
+        c["n_pool"], c["bt"], c["width"], c["lens"], max_seq_len, sm_scale, _dev_ptr(out, "out", (torch.float32,)), before_ptr, decay, w_ptr,
+        weights.shape[1], None if residual is None else _dev_ptr(residual, "residual", (torch.float16,)),
+        _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream())
+    _check(st, "pq_decode_attention_weights")
+
+
+def pq_evict_pages(layout: Layout, block_table, seq_lens, weights, n_kept: int, n_first: int, n_last: int, table_after, lens_after,
+                   weights_after, freed, counts) -> None:
+    """Pages beyond n_kept out of the block tables, those of the smallest weights; see include/polarquant.h.  block_table and table_after
+    int32 [n_seqs, width], weights and weights_after fp32 [n_seqs, stride >= width] (each pair may be one tensor), seq_lens and
+    lens_after int32 [n_seqs] (two tensors), freed int32, counts int32 [1]."""
+    if _done((_calls or _marshaller()).evict_pages(
+            layout, block_table, seq_lens, weights, n_kept, n_first, n_last, table_after, lens_after, weights_after, freed, counts),
+            "pq_evict_pages"):
+        return
+    import torch
+    i32 = (torch.int32,)
+    _on_current_device(block_table=block_table, seq_lens=seq_lens, weights=weights, table_after=table_after, lens_after=lens_after,
+                       weights_after=weights_after, freed=freed, counts=counts)
+    n = seq_lens.numel()
+    _one_row_each(n, block_table, seq_lens)
+    if table_after.shape != block_table.shape or lens_after.numel() != n or weights_after.shape != weights.shape or counts.numel() < 1:
+        raise PolarQuantError("table_after, lens_after and weights_after must have the shapes of block_table, seq_lens and weights, counts [1]")
+    st = load_library().pq_evict_pages(
+        ctypes.byref(layout), _dev_ptr(block_table, "block_table", i32), block_table.shape[1], _dev_ptr(seq_lens, "seq_lens", i32), n,
+        _page_weights(n, "weights", weights), weights.shape[1], n_kept, n_first, n_last, _dev_ptr(table_after, "table_after", i32),
+        _dev_ptr(lens_after, "lens_after", i32), _page_weights(n, "weights_after", weights_after), _dev_ptr(freed, "freed", i32),
+        freed.numel(), _dev_ptr(counts, "counts", i32), _stream())
+    _check(st, "pq_evict_pages")
 
 
 def pq_probe_read_stream(src, sink) -> None:

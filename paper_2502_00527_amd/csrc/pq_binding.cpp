@@ -408,6 +408,179 @@ PyObject* window_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+float real(PyObject* o) {
+  if (!PyFloat_CheckExact(o)) throw Decline{};
+  return static_cast<float>(PyFloat_AS_DOUBLE(o));
+}
+// One row of the block table and one length a sequence.
+void check_sequences(const at::Tensor& table, const at::Tensor& lens, int32_t n_seqs) {
+  if (table.dim() != 2 || table.size(0) != n_seqs || lens.numel() != n_seqs) throw Decline{};
+}
+// Bounds and their scales, of at least n_pages pages.
+struct BoundPools {
+  const at::Tensor &bounds, &scales;
+  BoundPools(const pq_layout* l, PyObject* b, PyObject* s, int64_t n_pages) : bounds(contiguous_tensor(b, at::kChar)), scales(contiguous_tensor(s, at::kFloat)) {
+    if (n_pages < 0) n_pages = pages(bytes_of(bounds), pq_bounds_bytes_per_page(l));
+    if (bytes_of(bounds) < static_cast<size_t>(n_pages) * pq_bounds_bytes_per_page(l) ||
+        bytes_of(scales) < static_cast<size_t>(n_pages) * pq_bound_scales_bytes_per_page(l))
+      throw Decline{};
+  }
+};
+// A choice of pages for each KV head, and its lengths.
+struct Selection {
+  const at::Tensor &pages, &lens;
+  int32_t width;
+  Selection(const pq_layout* l, PyObject* p, PyObject* n, int32_t n_seqs) : pages(contiguous_tensor(p, at::kInt)), lens(contiguous_tensor(n, at::kInt)) {
+    if (pages.dim() != 3 || pages.size(0) != n_seqs || pages.size(1) != l->n_kv_heads || lens.numel() != static_cast<int64_t>(n_seqs) * l->n_kv_heads)
+      throw Decline{};
+    width = integer32(pages.size(2));
+  }
+};
+float* floats(const at::Tensor& t) { return static_cast<float*>(t.data_ptr()); }
+
+// (layout, codes, params, block_table, lens_before, lens_after, max_new_tokens, bounds, bound_scales)
+PyObject* bound_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 9, [&] {
+    const pq_layout layout = layout_of(a[0]), *const l = &layout;
+    const at::Tensor &codes = contiguous_tensor(a[1]), &params = contiguous_tensor(a[2]), &table = contiguous_tensor(a[3], at::kInt),
+                     &after = contiguous_tensor(a[5], at::kInt);
+    const int64_t n_pages = key_pool_pages(l, codes, params);
+    const int32_t n_seqs = integer32(after.numel()), most = integer32(integer(a[6]));
+    check_sequences(table, after, n_seqs);
+    const BoundPools b(l, a[7], a[8], n_pages);
+    const at::Tensor& before = a[4] == Py_None ? after : contiguous_tensor(a[4], at::kInt);
+    if (before.numel() != n_seqs) throw Decline{};
+    const int32_t *const bp = a[4] == Py_None ? nullptr : ints(before), *const ap = ints(after), *const tp = ints(table), width = integer32(table.size(1));
+    void *const cp = codes.data_ptr(), *const pp = params.data_ptr(), *const bounds = b.bounds.data_ptr(), *const scales = b.scales.data_ptr(),
+         *const stream = stream_of(codes, params, table, before, after, b.bounds, b.scales);
+    return without_lock([&] { return pq_bound_pages(l, cp, pp, n_pages, tp, width, bp, ap, n_seqs, most, bounds, scales, stream); });
+  });
+}
+
+// (layout, q, bounds, bound_scales, block_table, seq_lens, max_seq_len, n_first, n_last, selected, selected_lens, workspace)
+PyObject* select_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 12, [&] {
+    const pq_layout layout = layout_of(a[0]), *const l = &layout;
+    const at::Tensor& q = contiguous_tensor(a[1]);
+    check_rows(q, l, false);
+    const pq_dtype kind = float_kind(q);
+    const int32_t n_seqs = integer32(q.size(0)), n_heads = integer32(q.size(1));
+    const BoundPools b(l, a[2], a[3], -1);
+    const int64_t n_pages = pages(bytes_of(b.bounds), pq_bounds_bytes_per_page(l));
+    const at::Tensor &table = contiguous_tensor(a[4], at::kInt), &lens = contiguous_tensor(a[5], at::kInt), &workspace = contiguous_tensor(a[11]);
+    check_sequences(table, lens, n_seqs);
+    const Selection s(l, a[9], a[10], n_seqs);
+    const int32_t width = integer32(table.size(1)), max_seq_len = integer32(integer(a[6])), n_first = integer32(integer(a[7])),
+                  n_last = integer32(integer(a[8])), *const tp = ints(table), *const lp = ints(lens);
+    int32_t *const sp = ints(s.pages), *const np = ints(s.lens);
+    void *const qp = q.data_ptr(), *const bounds = b.bounds.data_ptr(), *const scales = b.scales.data_ptr(), *const ws = workspace.data_ptr(),
+         *const stream = stream_of(q, b.bounds, b.scales, table, lens, s.pages, s.lens, workspace);
+    const size_t ws_bytes = bytes_of(workspace);
+    return without_lock([&] {
+      return pq_select_pages(l, qp, kind, n_seqs, n_heads, bounds, scales, n_pages, tp, width, lp, max_seq_len, s.width, n_first, n_last, sp, np, ws, ws_bytes,
+                             stream);
+    });
+  });
+}
+
+// (layout, q, codes, params, v_pool, bounds, bound_scales, block_table, seq_lens, max_seq_len, n_first, n_last, sm_scale, selected, selected_lens,
+//  out, workspace, residual, v_bits, v_params)
+PyObject* sparse_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 20, [&] {
+    const pq_layout layout = layout_of(a[0]), *const l = &layout;
+    const at::Tensor& q = contiguous_tensor(a[1]);
+    check_rows(q, l, false);
+    const pq_dtype kind = float_kind(q);
+    const int32_t n_seqs = integer32(q.size(0)), n_heads = integer32(q.size(1)), v_bits = integer32(integer(a[18]));
+    const at::Tensor &codes = contiguous_tensor(a[2]), &params = contiguous_tensor(a[3]), &out = contiguous_tensor(a[15], at::kFloat),
+                     &workspace = contiguous_tensor(a[16]);
+    if (out.sizes() != q.sizes()) throw Decline{};
+    const int64_t n_pages = key_pool_pages(l, codes, params);
+    const ValuePool v(l, a[4], a[19], v_bits, n_pages);
+    const Selection s(l, a[13], a[14], n_seqs);
+    const int32_t max_seq_len = integer32(integer(a[9])), n_first = integer32(integer(a[10])), n_last = integer32(integer(a[11]));
+    const float sm_scale = real(a[12]);
+    const void *bounds = nullptr, *scales = nullptr;
+    const int32_t *tp = nullptr, *lp = nullptr;
+    int32_t width = 0;
+    if (a[5] != Py_None || a[6] != Py_None) {
+      const BoundPools b(l, a[5], a[6], n_pages);
+      const at::Tensor &table = contiguous_tensor(a[7], at::kInt), &lens = contiguous_tensor(a[8], at::kInt);
+      check_sequences(table, lens, n_seqs);
+      stream_of(b.bounds, b.scales, table, lens);
+      bounds = b.bounds.data_ptr();
+      scales = b.scales.data_ptr();
+      tp = ints(table);
+      lp = ints(lens);
+      width = integer32(table.size(1));
+    }
+    void* const residual = a[17] == Py_None ? nullptr : residual_of(a[17], l, n_seqs, q);
+    void *const qp = q.data_ptr(), *const cp = codes.data_ptr(), *const pp = params.data_ptr(), *const ws = workspace.data_ptr(),
+         *const stream = stream_of(q, codes, params, v.tensor, s.pages, s.lens, out, workspace);
+    int32_t *const sp = ints(s.pages), *const np = ints(s.lens);
+    float* const op = floats(out);
+    const size_t ws_bytes = bytes_of(workspace);
+    return without_lock([&] {
+      return pq_sparse_attention(l, qp, kind, n_seqs, n_heads, cp, pp, v.pool, v_bits, v.params, bounds, scales, n_pages, tp, width, lp, max_seq_len, s.width,
+                                 n_first, n_last, sm_scale, sp, np, op, residual, ws, ws_bytes, stream);
+    });
+  });
+}
+
+// (layout, q, codes, params, v_pool, block_table, seq_lens, max_seq_len, sm_scale, out, weights, workspace, weights_before, decay, residual,
+//  v_bits, v_params)
+PyObject* decode_attention_weights(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 17, [&] {
+    const pq_layout layout = layout_of(a[0]), *const l = &layout;
+    const at::Tensor& q = contiguous_tensor(a[1]);
+    check_rows(q, l, false);
+    const pq_dtype kind = float_kind(q);
+    const int32_t n_seqs = integer32(q.size(0)), n_heads = integer32(q.size(1)), v_bits = integer32(integer(a[15]));
+    const at::Tensor &codes = contiguous_tensor(a[2]), &params = contiguous_tensor(a[3]);
+    const int64_t n_pages = key_pool_pages(l, codes, params);
+    const ValuePool v(l, a[4], a[16], v_bits, n_pages);
+    const at::Tensor &table = contiguous_tensor(a[5], at::kInt), &lens = contiguous_tensor(a[6], at::kInt), &out = contiguous_tensor(a[9], at::kFloat),
+                     &weights = contiguous_tensor(a[10], at::kFloat), &workspace = contiguous_tensor(a[11]);
+    check_sequences(table, lens, n_seqs);
+    const at::Tensor& before = a[12] == Py_None ? weights : contiguous_tensor(a[12], at::kFloat);
+    if (out.sizes() != q.sizes() || weights.dim() != 2 || weights.size(0) != n_seqs || before.sizes() != weights.sizes()) throw Decline{};
+    const int32_t width = integer32(table.size(1)), max_seq_len = integer32(integer(a[7])), *const tp = ints(table), *const lp = ints(lens);
+    const float sm_scale = real(a[8]), decay = real(a[13]);
+    void* const residual = a[14] == Py_None ? nullptr : residual_of(a[14], l, n_seqs, q);
+    void *const qp = q.data_ptr(), *const cp = codes.data_ptr(), *const pp = params.data_ptr(), *const ws = workspace.data_ptr(),
+         *const stream = stream_of(q, codes, params, v.tensor, table, lens, out, weights, before, workspace);
+    float *const op = floats(out), *const wp = floats(weights), *const bp = a[12] == Py_None ? nullptr : floats(before);
+    const int64_t stride = weights.size(1);
+    const size_t ws_bytes = bytes_of(workspace);
+    return without_lock([&] {
+      return pq_decode_attention_weights(l, qp, kind, n_seqs, n_heads, cp, pp, v.pool, v_bits, v.params, n_pages, tp, width, lp, max_seq_len, sm_scale, op, bp,
+                                         decay, wp, stride, residual, ws, ws_bytes, stream);
+    });
+  });
+}
+
+// (layout, block_table, seq_lens, weights, n_kept, n_first, n_last, table_after, lens_after, weights_after, freed, counts)
+PyObject* evict_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 12, [&] {
+    const pq_layout layout = layout_of(a[0]), *const l = &layout;
+    const at::Tensor &table = contiguous_tensor(a[1], at::kInt), &lens = contiguous_tensor(a[2], at::kInt), &weights = contiguous_tensor(a[3], at::kFloat),
+                     &table_after = contiguous_tensor(a[7], at::kInt), &lens_after = contiguous_tensor(a[8], at::kInt),
+                     &weights_after = contiguous_tensor(a[9], at::kFloat), &freed = contiguous_tensor(a[10], at::kInt), &counts = contiguous_tensor(a[11], at::kInt);
+    const int32_t n_seqs = integer32(lens.numel()), n_kept = integer32(integer(a[4])), n_first = integer32(integer(a[5])), n_last = integer32(integer(a[6]));
+    check_sequences(table, lens, n_seqs);
+    if (weights.dim() != 2 || weights.size(0) != n_seqs || table_after.sizes() != table.sizes() || lens_after.numel() != n_seqs ||
+        weights_after.sizes() != weights.sizes() || counts.numel() < 1)
+      throw Decline{};
+    const int32_t width = integer32(table.size(1)), n_freed = integer32(freed.numel()), *const tp = ints(table), *const lp = ints(lens);
+    const float* const wp = floats(weights);
+    const int64_t stride = weights.size(1);
+    int32_t *const ta = ints(table_after), *const la = ints(lens_after), *const fp = ints(freed), *const cp = ints(counts);
+    float* const wa = floats(weights_after);
+    void* const stream = stream_of(table, lens, weights, table_after, lens_after, weights_after, freed, counts);
+    return without_lock([&] { return pq_evict_pages(l, tp, width, lp, n_seqs, wp, stride, n_kept, n_first, n_last, ta, la, wa, fp, n_freed, cp, stream); });
+  });
+}
+
 PyObject* set_layout_type(PyObject*, PyObject* type) {
   Py_INCREF(type);
   Py_XSETREF(layout_type, type);
@@ -417,6 +590,8 @@ PyObject* set_layout_type(PyObject*, PyObject* type) {
 #define PQ_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {PQ_METHOD(decode_attention), PQ_METHOD(score_keys), PQ_METHOD(encode_keys), PQ_METHOD(encode_values),
                          PQ_METHOD(append_keys), PQ_METHOD(plan_pages), PQ_METHOD(append_chunk), PQ_METHOD(chunk_attention), PQ_METHOD(window_attention),
+                         PQ_METHOD(bound_pages), PQ_METHOD(select_pages), PQ_METHOD(sparse_attention), PQ_METHOD(decode_attention_weights),
+                         PQ_METHOD(evict_pages),
                          {"set_layout_type", set_layout_type, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Argument marshalling for libpolarquant.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 

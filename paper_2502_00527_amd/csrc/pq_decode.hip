@@ -22,12 +22,12 @@ namespace {
 constexpr int kMergeThreads = 256;
 constexpr int kMergeSlices = kMergeThreads / 32;
 
-// kWindow: the lengths are what a sliding window leaves of them.
-template <bool kWindow>
+// kWindow: the lengths are what a sliding window leaves of them.  kWeights: the heads' maxima and sums are left in `totals`.
+template <bool kWindow, bool kWeights = false>
 __global__ __launch_bounds__(kMergeThreads) void pq_decode_merge_kernel(
     const float* __restrict__ ws_acc, const float* __restrict__ ws_ml,
     const int32_t* __restrict__ seq_lens, float* __restrict__ out, int32_t n_q_heads,
-    int32_t max_seq_len, int32_t pages_per_chunk, int32_t n_chunks, int32_t n_big, int32_t pages_small, int32_t window, int32_t n_sinks) {
+    int32_t max_seq_len, int32_t pages_per_chunk, int32_t n_chunks, int32_t n_big, int32_t pages_small, int32_t window, int32_t n_sinks, float2* totals) {
   __shared__ float4 part_o[kMergeSlices][32];
   __shared__ float part_l[kMergeSlices];
   __shared__ float wave_max[kMergeThreads / 64];
@@ -82,6 +82,9 @@ __global__ __launch_bounds__(kMergeThreads) void pq_decode_merge_kernel(
     }
     const float inv = lt > 0.f ? 1.f / lt : 0.f;
     reinterpret_cast<float4*>(out + oh * kHeadDim)[quad] = make_float4(r.x * inv, r.y * inv, r.z * inv, r.w * inv);
+    if constexpr (kWeights) {
+      if (quad == 0) totals[oh] = make_float2(M, lt);
+    }
   }
 }
 
@@ -290,6 +293,8 @@ int launch_scores(const pq_layout* layout, DecodeArgs a, hipStream_t stream) {
   return e == hipSuccess ? PQ_OK : record_hip_error(e);
 }
 
+}  // namespace
+
 // Checks of the arguments that attention over the whole cache and through a window have in common.
 int check_attention(const pq_layout* layout, const void* q, pq_dtype q_dtype, int32_t n_seqs, int32_t n_q_heads,
                     const void* codes_pool, const void* params_pool, const void* v_pool, int32_t v_bits,
@@ -315,6 +320,8 @@ int check_attention(const pq_layout* layout, const void* q, pq_dtype q_dtype, in
     return PQ_ERR_INVALID_ARG;
   return PQ_OK;
 }
+
+namespace {
 
 // What their kernels are given alike.
 DecodeArgs attention_args(const pq_layout* layout, const void* q, pq_dtype q_dtype, int32_t n_seqs, int32_t n_q_heads,
@@ -412,7 +419,7 @@ int decode_launch(const pq_layout* layout, const void* q, pq_dtype q_dtype, int3
   if (out != nullptr && !merged) {
     hipLaunchKernelGGL(pq_decode_merge_kernel<false>, dim3(n_q_heads, n_seqs), dim3(kMergeThreads), 0, stream, ws.acc,
                        ws.ml, seq_lens, out, n_q_heads, max_seq_len, plan.pages_per_chunk, plan.n_chunks, plan.n_big,
-                       plan.pages_small, 0, 0);
+                       plan.pages_small, 0, 0, nullptr);
     e = hipGetLastError();
     if (e != hipSuccess) return record_hip_error(e);
   }
@@ -463,7 +470,7 @@ extern "C" int pq_decode_merge(const pq_layout* layout, int32_t n_seqs, int32_t 
   hipLaunchKernelGGL(pq_decode_merge_kernel<false>, dim3(n_q_heads, n_seqs), dim3(kMergeThreads), 0,
                      static_cast<hipStream_t>(hip_stream), ws.acc, ws.ml, seq_lens, out, n_q_heads,
                      max_seq_len, plan.pages_per_chunk, plan.n_chunks, plan.n_big,
-                       plan.pages_small, 0, 0);
+                       plan.pages_small, 0, 0, nullptr);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return record_hip_error(e);
   return PQ_OK;
@@ -568,7 +575,116 @@ extern "C" int pq_window_attention(const pq_layout* layout, const void* q, pq_dt
   }
   if (e == hipSuccess && !merged) {
     hipLaunchKernelGGL(pq_decode_merge_kernel<true>, dim3(n_q_heads, n_seqs), dim3(kMergeThreads), 0, stream, ws.acc, ws.ml, seq_lens, out, n_q_heads,
-                       max_seq_len, plan.pages_per_chunk, plan.n_chunks, plan.n_big, plan.pages_small, a.window, a.n_sinks);
+                       max_seq_len, plan.pages_per_chunk, plan.n_chunks, plan.n_big, plan.pages_small, a.window, a.n_sinks, nullptr);
+    e = hipGetLastError();
+  }
+  return e == hipSuccess ? PQ_OK : record_hip_error(e);
+}
+
+namespace pq {
+namespace {
+
+// weights[seq][page] = decay * before[seq][page] + the sum over the query heads of l 2^(m - M) / L, (m, l) being the page's maximum and sum, (M, L)
+// the head's.  Thread = (page, slice of the heads); a slice takes every kWeightSlices-th head.
+constexpr int kWeightPages = 64, kWeightSlices = 4;
+__global__ __launch_bounds__(kWeightPages* kWeightSlices) void pq_page_weights_kernel(
+    const float2* __restrict__ page_ml, const float2* __restrict__ totals, const int32_t* __restrict__ seq_lens, const float* before, float* weights,
+    int64_t weights_stride, int32_t page_stride, int32_t n_q_heads, int32_t max_seq_len, float decay) {
+  __shared__ float part[kWeightSlices][kWeightPages];
+  const int at = threadIdx.x % kWeightPages, slice = threadIdx.x / kWeightPages, seq = blockIdx.y, page = blockIdx.x * kWeightPages + at;
+  const int L = min(seq_lens[seq], max_seq_len), n_pages = L > 0 ? (L + kGroup - 1) / kGroup : 0;
+  if (static_cast<int>(blockIdx.x) * kWeightPages >= n_pages) return;
+  float w = 0.f;
+  if (page < n_pages) {
+#pragma unroll 8
+    for (int h = slice; h < n_q_heads; h += kWeightSlices) {
+      const int64_t row = static_cast<int64_t>(seq) * n_q_heads + h;
+      const float2 all = totals[row], one = page_ml[row * page_stride + page];
+      if (one.y > 0.f) w += one.y * __builtin_amdgcn_exp2f(one.x - all.x) / all.y;
+    }
+  }
+  part[slice][at] = w;
+  __syncthreads();
+  if (slice != 0 || page >= n_pages) return;
+  w = (part[0][at] + part[1][at]) + (part[2][at] + part[3][at]);
+  const int64_t i = seq * weights_stride + page;
+  if (before && decay != 0.f) w += decay * before[i];
+  weights[i] = w;
+}
+
+struct WeightsWorkspace {
+  Workspace decode;
+  float2 *page_ml, *totals;
+  size_t bytes;
+};
+WeightsWorkspace carve_weights_workspace(void* base, const pq_layout* l, int32_t n_seqs, int32_t n_q_heads, int32_t max_seq_len) {
+  WeightsWorkspace w;
+  w.decode = carve_workspace(base, l, n_seqs, n_q_heads, max_seq_len);
+  const size_t rows = static_cast<size_t>(n_seqs) * n_q_heads, pages = (static_cast<size_t>(max_seq_len) + kGroup - 1) / kGroup;
+  const size_t total_bytes = round256(rows * sizeof(float2));
+  uint8_t* const at = static_cast<uint8_t*>(base) + w.decode.bytes;
+  w.totals = reinterpret_cast<float2*>(at);
+  w.page_ml = reinterpret_cast<float2*>(at + total_bytes);
+  w.bytes = w.decode.bytes + total_bytes + round256(rows * pages * sizeof(float2));
+  return w;
+}
+
+}  // namespace
+}  // namespace pq
+
+extern "C" size_t pq_weights_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_t n_q_heads, int32_t max_seq_len) {
+  if (check_decode_shape(layout, n_seqs, n_q_heads, max_seq_len) != PQ_OK) return 0;
+  return carve_weights_workspace(nullptr, layout, n_seqs, n_q_heads, max_seq_len).bytes;
+}
+
+extern "C" int pq_decode_attention_weights(const pq_layout* layout, const void* q, pq_dtype q_dtype, int32_t n_seqs, int32_t n_q_heads,
+                                           const void* codes_pool, const void* params_pool, const void* v_pool, int32_t v_bits,
+                                           const void* v_params_pool, int64_t n_pool_pages, const int32_t* block_table, int32_t max_pages_per_seq,
+                                           const int32_t* seq_lens, int32_t max_seq_len, float sm_scale, float* out, const float* weights_before,
+                                           float decay, float* weights, int64_t weights_stride, const void* residual_keys, void* workspace,
+                                           size_t workspace_bytes, void* hip_stream) {
+  if (!out || (reinterpret_cast<uintptr_t>(out) & 15u)) return PQ_ERR_INVALID_ARG;
+  const int st = check_attention(layout, q, q_dtype, n_seqs, n_q_heads, codes_pool, params_pool, v_pool, v_bits, v_params_pool, n_pool_pages, block_table,
+                                 max_pages_per_seq, seq_lens, max_seq_len, sm_scale, residual_keys);
+  if (st != PQ_OK) return st;
+  const int64_t max_pages = (static_cast<int64_t>(max_seq_len) + kGroup - 1) / kGroup;
+  if (!weights || ((reinterpret_cast<uintptr_t>(weights) | reinterpret_cast<uintptr_t>(weights_before)) & 3u) || weights_stride < max_pages || !isfinite(decay))
+    return PQ_ERR_INVALID_ARG;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return PQ_ERR_WORKSPACE;
+  const WeightsWorkspace ws = carve_weights_workspace(workspace, layout, n_seqs, n_q_heads, max_seq_len);
+  if (workspace_bytes < ws.bytes) return PQ_ERR_WORKSPACE;
+  const ChunkPlan plan = plan_attention(layout, v_bits, n_seqs, n_q_heads, max_seq_len);
+  const DeviceCut cut = device_cut(layout, plan, v_bits, n_seqs, n_q_heads, max_seq_len);
+  DecodeArgs a = attention_args(layout, q, q_dtype, n_seqs, n_q_heads, codes_pool, params_pool, v_pool, v_params_pool, n_pool_pages, block_table,
+                                max_pages_per_seq, seq_lens, max_seq_len, sm_scale, out, residual_keys, ws.decode, plan);
+  const bool merged = merges_in_kernel(layout, plan, cut, n_seqs, n_q_heads, max_seq_len);
+  a.merge_in_kernel = merged ? 1 : 0;
+  a.cut_places = cut.places;
+  a.spare_chunks = cut.spare_chunks;
+  a.fit_chunks = cut.fit_chunks;
+  a.wide_groups = wide_groups(layout, plan, n_seqs, max_seq_len) ? 1 : 0;
+  a.page_ml = ws.page_ml;
+  a.totals = ws.totals;
+  a.page_stride = static_cast<int32_t>(max_pages);
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  const dim3 grid = a.cut_places > 0 ? dim3(layout->n_kv_heads, a.cut_places) : dim3(layout->n_kv_heads, n_seqs, plan.n_chunks);
+  hipError_t e = hipSuccess;
+  for (a.head0 = 0; a.head0 < a.group_total && e == hipSuccess; a.head0 += a.n_heads) {
+    a.n_heads = std::min(a.group_total - a.head0, kMaxHeads);
+    if (v_bits == 16) launch_weights_v16(layout, a, grid, stream);
+    else if (v_bits == 4) launch_weights_v4(layout, a, grid, stream);
+    else launch_weights_v2(layout, a, grid, stream);
+    e = hipGetLastError();
+  }
+  if (e == hipSuccess && !merged) {
+    hipLaunchKernelGGL((pq_decode_merge_kernel<false, true>), dim3(n_q_heads, n_seqs), dim3(kMergeThreads), 0, stream, ws.decode.acc, ws.decode.ml, seq_lens,
+                       out, n_q_heads, max_seq_len, plan.pages_per_chunk, plan.n_chunks, plan.n_big, plan.pages_small, 0, 0, ws.totals);
+    e = hipGetLastError();
+  }
+  if (e == hipSuccess) {
+    hipLaunchKernelGGL(pq_page_weights_kernel, dim3(static_cast<uint32_t>((max_pages + kWeightPages - 1) / kWeightPages), n_seqs),
+                       dim3(kWeightPages * kWeightSlices), 0, stream, ws.page_ml, ws.totals, seq_lens, weights_before, weights, weights_stride, a.page_stride,
+                       n_q_heads, max_seq_len, decay);
     e = hipGetLastError();
   }
   return e == hipSuccess ? PQ_OK : record_hip_error(e);

@@ -63,6 +63,10 @@ bool launch_scores_grouped(int rt, const DecodeArgs& a, dim3 grid, hipStream_t s
 bool launch_window_v16(const pq_layout* l, const DecodeArgs& a, dim3 grid, hipStream_t st);
 bool launch_window_v4(const pq_layout* l, const DecodeArgs& a, dim3 grid, hipStream_t st);
 bool launch_window_v2(const pq_layout* l, const DecodeArgs& a, dim3 grid, hipStream_t st);
+// With each page's maximum and sum, of either quantizer (pq_decode_weights.hip, one per value width).
+bool launch_weights_v16(const pq_layout* l, const DecodeArgs& a, dim3 grid, hipStream_t st);
+bool launch_weights_v4(const pq_layout* l, const DecodeArgs& a, dim3 grid, hipStream_t st);
+bool launch_weights_v2(const pq_layout* l, const DecodeArgs& a, dim3 grid, hipStream_t st);
 
 namespace {
 
@@ -1042,7 +1046,8 @@ __device__ __forceinline__ void grouped_scores_body(const DecodeArgs& a) {
 // kCut: the chunks are cut on the device (a.cut_places > 0).  kMatWaves: wavefronts of the work-group, 4 or 8.
 // kGroupedRadius: 0 on the uniform grid; with the grouped angle quantizer the radius bits (queries of either type are
 // taken as fp32 there, so that Q32 is true).  kWindow: through a sliding window with sinks (WindowView; the launch is cut on the host).
-template <int W, int VB, int NH, bool Q32, bool kCut, int kMatWaves, int kGroupedRadius = 0, bool kWindow = false>
+// kWeights: each page's sum of exponentials and the maximum it was taken against go to a.page_ml, those of all pages to a.totals.
+template <int W, int VB, int NH, bool Q32, bool kCut, int kMatWaves, int kGroupedRadius = 0, bool kWindow = false, bool kWeights = false>
 __device__ __forceinline__ void attention_body(const DecodeArgs& a) {
   constexpr int UB = 2 * W;
   constexpr int kMatThreads = kMatWaves * 64;
@@ -1358,11 +1363,13 @@ __device__ __forceinline__ void attention_body(const DecodeArgs& a) {
     const float off = dead ? 0.f : -m_run;
     const f32x2 part = split_part<kUp>(lane_now() & 8);
     uint32_t p_op[8][2];                                               // batch t: fp16 pairs of tokens 4 row + (0, 1), (2, 3)
+    [[maybe_unused]] float l_page = 0.f;
 #pragma unroll
     for (int t = 0; t < kOwn; ++t) {
       float p[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(w.s[t][i], mult, off));
+      if constexpr (kWeights) l_page += (p[0] + p[1]) + (p[2] + p[3]);
       if constexpr (kQuantV) {
         // V~ = code * s + z (Section 2): fold s (times 2^s_exp) into the probability, collect p * z (low-part columns; p in the others)
         const u32x4 vp = *(const PQ_LDS u32x4*)static_cast<uintptr_t>(vpar_get + batch_token<kOrder>(t, 0) * 4);
@@ -1388,6 +1395,13 @@ __device__ __forceinline__ void attention_body(const DecodeArgs& a) {
           p_op[4 + t][e] = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(own, own, 0x12c, 0xf, 0x5, false));
         }
       }
+    }
+
+    if constexpr (kWeights) {
+      l_page = sum_rows(l_page);
+      if constexpr (NH == 4) l_page += dpp_of<0x12c>(l_page);          // the other half's batches
+      const int h = lane_now();
+      if (h < a.n_heads) a.page_ml[(first_head + h) * a.page_stride + pi] = make_float2(m_run, l_page);
     }
 
     // ---- values: acc += P^T V, 32 tokens (batches 2g, 2g + 1) per instruction ----
@@ -1509,7 +1523,7 @@ __device__ __forceinline__ void attention_body(const DecodeArgs& a) {
     __syncthreads();
   }
 
-  finish_chunk<NH>(a, seq, kvh, chunk, n_chunks, row0, stride, wave * 64 + lane_id(), [&](int h, int quad, float& M, float& l) {
+  finish_chunk<NH, kWeights>(a, seq, kvh, chunk, n_chunks, row0, stride, wave * 64 + lane_id(), [&](int h, int quad, float& M, float& l) {
     M = top_of(h);
     auto part = [&](int v) { return *reinterpret_cast<const f32x4*>(&sh.red[v][h][quad * 4]); };
     f32x4 o = (part(0) + part(2)) + (part(1) + part(3));

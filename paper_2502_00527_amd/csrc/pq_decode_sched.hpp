@@ -85,7 +85,8 @@ constexpr int kFinishLdsFloats = kFinishThreads * 5;
 // arrival is registered -- not by fences, which write back and invalidate whole caches (measured:
 // with fences in every work-group the launch takes twice as long).
 // The unit's partials: head h (from a.head0 on), chunk c in row row0 + h * stride + c.
-template <int NH, typename Partial>
+// kWeights: a unit that is finished here leaves its heads' maxima and sums in a.totals.
+template <int NH, bool kWeights = false, typename Partial>
 __device__ __forceinline__ void finish_chunk(const DecodeArgs& a, int seq, int kvh, int chunk, int n_chunks_seq, int64_t row0,
                                              int stride, int tid, Partial partial, float* lent, int* stage) {
   const int h = tid >> 5, quad = tid & 31;             // 256 threads: 8 heads x 32 quads
@@ -99,6 +100,9 @@ __device__ __forceinline__ void finish_chunk(const DecodeArgs& a, int seq, int k
     if (mine) {
       const float inv = l > 0.f ? 1.f / l : 0.f;
       reinterpret_cast<float4*>(out_rows)[tid] = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+      if constexpr (kWeights) {
+        if (quad == 0) a.totals[head_row + h] = make_float2(M, l);
+      }
     }
     return;
   }
@@ -164,6 +168,7 @@ __device__ __forceinline__ void finish_chunk(const DecodeArgs& a, int seq, int k
     float* const part_l = lent + kFinishThreads * 4;
     const float top = fmaxf(m, __shfl_xor(m, 32));
     const float wgt = top > kNegInf ? __builtin_amdgcn_exp2f(m - top) : 0.f;
+    if constexpr (kWeights) m = top;
     if (tid < kFinishThreads) {
       part_o[tid] = r * wgt;
       part_l[tid] = lt * wgt;
@@ -177,6 +182,9 @@ __device__ __forceinline__ void finish_chunk(const DecodeArgs& a, int seq, int k
   if (slice == 0 && ch < a.n_heads) {
     const float inv = lt > 0.f ? 1.f / lt : 0.f;
     reinterpret_cast<float4*>(out_rows)[ch * 32 + quad] = make_float4(r.x * inv, r.y * inv, r.z * inv, r.w * inv);
+    if constexpr (kWeights) {
+      if (quad == 0) a.totals[head_row + ch] = make_float2(m, lt);
+    }
   }
   if (tid == 0) reset_arrivals(word);
 }

@@ -1,0 +1,141 @@
+// pq_evict_pages: the pages of the smallest weights leave a block table, the others move together, weights with them.
+//
+// How many pages a sequence gives up follows from its length alone, so that each work-group finds its place in the list of freed
+// pages by summing over the sequences before it: one launch, nobody waits for anybody.  Which ones is a choice of the k largest keys
+// (pq_rank.hpp), the keys being the weights' upside down.
+//
+// One work-group a sequence.  Bound: a launch's own time; 16 bytes a page are read and written.
+#include <hip/hip_runtime.h>
+
+#include "pq_internal.hpp"
+#include "pq_rank.hpp"
+
+namespace pq {
+namespace {
+
+constexpr int kMostKeys = 4096;                              // pages whose keys stay in LDS
+
+struct EvictArgs {
+  const int32_t* block_table;
+  const int32_t* seq_lens;
+  const float* weights;
+  int32_t* table_after;
+  int32_t* lens_after;
+  float* weights_after;
+  int32_t* freed;
+  int32_t* counts;
+  int64_t weights_stride;
+  int32_t n_seqs, max_pages_per_seq, n_kept, n_first, n_last, n_freed;
+};
+
+struct Kept {
+  int pages, last, gone;                                     // of the sequence; kept at its end; given up
+};
+__device__ __forceinline__ Kept kept_of(const EvictArgs& a, int seq) {
+  const int len = max(0, a.seq_lens[seq]);
+  Kept k;
+  k.pages = len / kGroup + (len % kGroup != 0);
+  if (k.pages > a.max_pages_per_seq) return {a.max_pages_per_seq, 0, 0};          // no such sequence: left as it is
+  k.last = max(a.n_last, len % kGroup != 0 ? 1 : 0);
+  const int sure = static_cast<int>(min(static_cast<int64_t>(k.pages), static_cast<int64_t>(a.n_first) + k.last));
+  k.gone = max(0, k.pages - max(a.n_kept, sure));
+  return k;
+}
+
+template <int kThreads>
+__global__ __launch_bounds__(kThreads) void pq_evict_kernel(const EvictArgs a) {
+  __shared__ RankShared<kThreads> rank;
+  __shared__ uint32_t keys[kMostKeys];
+  __shared__ uint32_t sums[kThreads / 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, seq = blockIdx.x;
+  uint32_t before = 0;
+  for (int s = tid; s < min(seq, a.n_seqs); s += kThreads) before += kept_of(a, s).gone;
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) before += __shfl_xor(before, d);
+  if (lane == 0) sums[wave] = before;
+  const Kept k = seq < a.n_seqs ? kept_of(a, seq) : Kept{0, 0, 0};
+  const int64_t table_row = static_cast<int64_t>(seq) * a.max_pages_per_seq, weight_row = seq * a.weights_stride;
+  const int begin = a.n_first, end = k.pages - k.last;
+  // the smallest weight has the largest key; a NaN counts as the largest weight
+  auto key_at = [&](int p) {
+    const float w = a.weights[weight_row + p];
+    return ~(w == w ? key_of(w) : 0xffffffffu);
+  };
+  const bool in_lds = k.pages <= kMostKeys;
+  if (in_lds && k.gone > 0)
+    for (int p = begin + tid; p < end; p += kThreads) keys[p] = key_at(p);
+  __syncthreads();
+  before = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) before += sums[w];
+  if (seq >= a.n_seqs - 1 && tid == 0) a.counts[0] = static_cast<int32_t>(before + k.gone);
+  if (seq >= a.n_seqs) return;
+  if (tid == 0) a.lens_after[seq] = max(0, a.seq_lens[seq]) - k.gone * kGroup;
+  if (k.gone == 0 && a.table_after == a.block_table && a.weights_after == a.weights) return;
+  auto key = [&](int p) { return in_lds ? keys[p] : key_at(p); };
+  const Threshold t = k.gone > 0 ? find_threshold<kThreads>(rank, begin, end, static_cast<uint32_t>(k.gone), key, tid) : Threshold{0xffffffffu, 0};
+  Places places;
+  for (int base = 0; base < k.pages; base += kThreads) {
+    const int p = base + tid;
+    const bool there = p < k.pages, in = p >= begin && p < end && k.gone > 0;
+    const int32_t id = there ? a.block_table[table_row + p] : 0;
+    const float weight = there ? a.weights[weight_row + p] : 0.f;
+    bool chosen;
+    // (the wait in it: everybody has read before anybody writes, to where others have read before)
+    const uint32_t at = place<kThreads>(rank, places, t, in, in ? key(p) : 0, tid, chosen);
+    if (chosen) {
+      if (before + at < static_cast<uint32_t>(a.n_freed)) a.freed[before + at] = id;
+    } else if (there) {
+      a.table_after[table_row + p - at] = id;
+      a.weights_after[weight_row + p - at] = weight;
+    }
+  }
+  for (int p = k.pages - k.gone + tid; p < k.pages; p += kThreads) {
+    a.table_after[table_row + p] = -1;
+    a.weights_after[weight_row + p] = 0.f;
+  }
+}
+
+}  // namespace
+}  // namespace pq
+
+using namespace pq;
+
+extern "C" int pq_evict_pages(const pq_layout* layout, const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* seq_lens, int32_t n_seqs,
+                              const float* weights, int64_t weights_stride, int32_t n_kept, int32_t n_first, int32_t n_last, int32_t* table_after,
+                              int32_t* lens_after, float* weights_after, int32_t* freed, int32_t n_freed, int32_t* counts, void* hip_stream) {
+  if (!layout) return PQ_ERR_INVALID_ARG;
+  if (!layout_supported(layout)) return PQ_ERR_UNSUPPORTED;
+  if (n_seqs < 0 || max_pages_per_seq <= 0 || weights_stride < max_pages_per_seq || n_kept < 0 || n_first < 0 || n_last < 0 || n_freed < 0)
+    return PQ_ERR_INVALID_ARG;
+  if (!counts || (n_seqs > 0 && (!block_table || !seq_lens || !weights || !table_after || !lens_after || !weights_after)) || (n_freed > 0 && !freed))
+    return PQ_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(block_table) | reinterpret_cast<uintptr_t>(seq_lens) | reinterpret_cast<uintptr_t>(weights) |
+       reinterpret_cast<uintptr_t>(table_after) | reinterpret_cast<uintptr_t>(lens_after) | reinterpret_cast<uintptr_t>(weights_after) |
+       reinterpret_cast<uintptr_t>(freed) | reinterpret_cast<uintptr_t>(counts)) & 3u)
+    return PQ_ERR_INVALID_ARG;
+  if (n_seqs > 0 && lens_after == seq_lens) return PQ_ERR_INVALID_ARG;        // (other work-groups still read what one would write)
+  if (n_seqs > 65535) return PQ_ERR_UNSUPPORTED;
+  EvictArgs a;
+  a.block_table = block_table;
+  a.seq_lens = seq_lens;
+  a.weights = weights;
+  a.table_after = table_after;
+  a.lens_after = lens_after;
+  a.weights_after = weights_after;
+  a.freed = freed;
+  a.counts = counts;
+  a.weights_stride = weights_stride;
+  a.n_seqs = n_seqs;
+  a.max_pages_per_seq = max_pages_per_seq;
+  a.n_kept = n_kept;
+  a.n_first = n_first;
+  a.n_last = n_last;
+  a.n_freed = n_freed;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  const dim3 grid(static_cast<uint32_t>(std::max(n_seqs, 1)));
+  if (max_pages_per_seq > 256) hipLaunchKernelGGL(pq_evict_kernel<1024>, grid, dim3(1024), 0, st, a);
+  else hipLaunchKernelGGL(pq_evict_kernel<256>, grid, dim3(256), 0, st, a);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? PQ_OK : record_hip_error(e);
+}

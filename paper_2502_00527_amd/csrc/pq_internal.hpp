@@ -15,6 +15,12 @@ int record_hip_error(hipError_t e);
 // True when this build has kernels for the layout.
 bool layout_supported(const pq_layout* l);
 
+// Checks of the arguments that the calls of single-token attention have in common.
+int check_attention(const pq_layout* layout, const void* q, pq_dtype q_dtype, int32_t n_seqs, int32_t n_q_heads, const void* codes_pool,
+                    const void* params_pool, const void* v_pool, int32_t v_bits, const void* v_params_pool, int64_t n_pool_pages,
+                    const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* seq_lens, int32_t max_seq_len, float sm_scale,
+                    const void* residual_keys);
+
 // An encoder's work-groups (256 threads) are one a (token group, KV head) in a one-dimensional grid, which HIP limits to
 // 2^32 - 1 threads: launch(first group, groups) is called for as many ranges of token groups as that takes.
 template <typename F>
