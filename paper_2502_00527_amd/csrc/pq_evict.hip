@@ -7,6 +7,7 @@
 // One work-group a sequence.  Bound: a launch's own time; 16 bytes a page are read and written.
 #include <hip/hip_runtime.h>
 
+#include "pq_decode_sched.hpp"
 #include "pq_internal.hpp"
 #include "pq_rank.hpp"
 
@@ -42,55 +43,83 @@ __device__ __forceinline__ Kept kept_of(const EvictArgs& a, int seq) {
   return k;
 }
 
-template <int kThreads>
-__global__ __launch_bounds__(kThreads) void pq_evict_kernel(const EvictArgs a) {
-  __shared__ RankShared<kThreads> rank;
+__global__ __launch_bounds__(kRankThreads) void pq_evict_kernel(const EvictArgs a) {
+  __shared__ RankShared rank;
   __shared__ uint32_t keys[kMostKeys];
-  __shared__ uint32_t sums[kThreads / 64];
+  __shared__ uint32_t sums[kRankWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, seq = blockIdx.x;
-  uint32_t before = 0;
-  for (int s = tid; s < min(seq, a.n_seqs); s += kThreads) before += kept_of(a, s).gone;
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) before += __shfl_xor(before, d);
-  if (lane == 0) sums[wave] = before;
-  const Kept k = seq < a.n_seqs ? kept_of(a, seq) : Kept{0, 0, 0};
   const int64_t table_row = static_cast<int64_t>(seq) * a.max_pages_per_seq, weight_row = seq * a.weights_stride;
+  // a first round of the rows, which exist whatever the sequence's length, is asked for before the lengths
+  int32_t id[kKeysPerThread];
+  float weight[kKeysPerThread];
+  auto load_round = [&](int p0, int most) {
+#pragma unroll
+    for (int j = 0; j < kKeysPerThread; ++j) {
+      const bool there = p0 + j < most && seq < a.n_seqs;
+      id[j] = there ? a.block_table[table_row + p0 + j] : 0;
+      weight[j] = there ? a.weights[weight_row + p0 + j] : 0.f;
+    }
+  };
+  load_round(tid * kKeysPerThread, a.max_pages_per_seq);
+  uint32_t before = 0;
+  for (int s = tid; s < min(seq, a.n_seqs); s += kRankThreads) before += kept_of(a, s).gone;
+  const Kept k = seq < a.n_seqs ? kept_of(a, seq) : Kept{0, 0, 0};
+  before = wave_sum(before);
+  if (lane == 0) sums[wave] = before;
   const int begin = a.n_first, end = k.pages - k.last;
   // the smallest weight has the largest key; a NaN counts as the largest weight
-  auto key_at = [&](int p) {
-    const float w = a.weights[weight_row + p];
-    return ~(w == w ? key_of(w) : 0xffffffffu);
-  };
+  auto key_of_weight = [](float w) { return ~(w == w ? key_of(w) : 0xffffffffu); };
   const bool in_lds = k.pages <= kMostKeys;
-  if (in_lds && k.gone > 0)
-    for (int p = begin + tid; p < end; p += kThreads) keys[p] = key_at(p);
-  __syncthreads();
-  before = 0;
+  uint32_t low = 0xffffffffu, high = 0;
+  if (k.gone > 0) {
+    for (int base = 0; base < k.pages; base += kRankRound) {
+      const int p0 = base + tid * kKeysPerThread;
 #pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) before += sums[w];
+      for (int j = 0; j < kKeysPerThread; ++j) {
+        if (p0 + j >= k.pages) continue;
+        const uint32_t v = key_of_weight(base == 0 ? weight[j] : a.weights[weight_row + p0 + j]);
+        if (in_lds) keys[p0 + j] = v;
+        if (p0 + j >= begin && p0 + j < end) {
+          low = min(low, v);
+          high = max(high, v);
+        }
+      }
+    }
+  }
+  auto key = [&](int p) { return in_lds ? keys[p] : key_of_weight(a.weights[weight_row + p]); };
+  const Threshold t = find_threshold(rank, begin, end, static_cast<uint32_t>(k.gone), low, high, key, tid);
+  before = (sums[0] + sums[1]) + (sums[2] + sums[3]);
   if (seq >= a.n_seqs - 1 && tid == 0) a.counts[0] = static_cast<int32_t>(before + k.gone);
   if (seq >= a.n_seqs) return;
   if (tid == 0) a.lens_after[seq] = max(0, a.seq_lens[seq]) - k.gone * kGroup;
   if (k.gone == 0 && a.table_after == a.block_table && a.weights_after == a.weights) return;
-  auto key = [&](int p) { return in_lds ? keys[p] : key_at(p); };
-  const Threshold t = k.gone > 0 ? find_threshold<kThreads>(rank, begin, end, static_cast<uint32_t>(k.gone), key, tid) : Threshold{0xffffffffu, 0};
   Places places;
-  for (int base = 0; base < k.pages; base += kThreads) {
-    const int p = base + tid;
-    const bool there = p < k.pages, in = p >= begin && p < end && k.gone > 0;
-    const int32_t id = there ? a.block_table[table_row + p] : 0;
-    const float weight = there ? a.weights[weight_row + p] : 0.f;
-    bool chosen;
-    // (the wait in it: everybody has read before anybody writes, to where others have read before)
-    const uint32_t at = place<kThreads>(rank, places, t, in, in ? key(p) : 0, tid, chosen);
-    if (chosen) {
-      if (before + at < static_cast<uint32_t>(a.n_freed)) a.freed[before + at] = id;
-    } else if (there) {
-      a.table_after[table_row + p - at] = id;
-      a.weights_after[weight_row + p - at] = weight;
+  for (int base = 0; base < k.pages; base += kRankRound) {
+    const int p0 = base + tid * kKeysPerThread;
+    if (base > 0) load_round(p0, k.pages);
+    bool in[kKeysPerThread], chosen[kKeysPerThread];
+    uint32_t v[kKeysPerThread], at[kKeysPerThread];
+#pragma unroll
+    for (int j = 0; j < kKeysPerThread; ++j) {
+      in[j] = p0 + j >= begin && p0 + j < end && k.gone > 0;
+      v[j] = in[j] ? key_of_weight(weight[j]) : 0;
+    }
+    // everybody has read before anybody writes, to where others have read before: what was asked for has come, and all wait for one another in
+    // place_keys()
+    stores_done();
+    place_keys(rank, places, t, in, v, tid, chosen, at);
+#pragma unroll
+    for (int j = 0; j < kKeysPerThread; ++j) {
+      const int p = p0 + j;
+      if (chosen[j]) {
+        if (before + at[j] < static_cast<uint32_t>(a.n_freed)) a.freed[before + at[j]] = id[j];
+      } else if (p < k.pages) {
+        a.table_after[table_row + p - at[j]] = id[j];
+        a.weights_after[weight_row + p - at[j]] = weight[j];
+      }
     }
   }
-  for (int p = k.pages - k.gone + tid; p < k.pages; p += kThreads) {
+  for (int p = k.pages - k.gone + tid; p < k.pages; p += kRankThreads) {
     a.table_after[table_row + p] = -1;
     a.weights_after[weight_row + p] = 0.f;
   }
@@ -134,8 +163,7 @@ extern "C" int pq_evict_pages(const pq_layout* layout, const int32_t* block_tabl
   a.n_freed = n_freed;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   const dim3 grid(static_cast<uint32_t>(std::max(n_seqs, 1)));
-  if (max_pages_per_seq > 256) hipLaunchKernelGGL(pq_evict_kernel<1024>, grid, dim3(1024), 0, st, a);
-  else hipLaunchKernelGGL(pq_evict_kernel<256>, grid, dim3(256), 0, st, a);
+  hipLaunchKernelGGL(pq_evict_kernel, grid, dim3(kRankThreads), 0, st, a);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? PQ_OK : record_hip_error(e);
 }

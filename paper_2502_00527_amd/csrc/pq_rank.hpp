@@ -1,9 +1,11 @@
 // The k largest of a list of 32-bit keys, ties to the first ones, by one work-group: where the choice lies, and each key's place in it.
 //
 // A threshold T and a number n of ties say it: key i is chosen if it is above T, or is T and fewer than n keys before it are.  T is found
-// by counting keys in 256 bins of equal width between the smallest and the largest key, then within the bin where
-// the count crosses k, and so on: scores of one call share their high bits, so that bins by bits would hold nearly all keys at first
-// (and their counters would be one word of LDS).
+// by counting keys in 1024 bins of equal width between the smallest and the largest key, and where the count crosses k, each of that bin's keys against
+// each, or, if they are more than 64, in 1024 bins again.  (Scores of one call share their high bits: bins by bits would hold nearly all of them at
+// first, and their counters would be one word of LDS.  Weights spread over 30 powers of two put 80 of 900 keys into one of 256 bins: a second
+// count.)  A wait of the work-group costs as much as all its arithmetic on a thousand keys:
+// there are three, and one more for the places.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -12,7 +14,11 @@
 namespace pq {
 namespace {
 
-constexpr int kBins = 256;
+constexpr int kRankThreads = 256;
+constexpr int kRankWaves = kRankThreads / 64;
+constexpr int kBins = 1024;
+constexpr int kKeysPerThread = 4;                            // of a round of place_keys()
+constexpr int kRankRound = kRankThreads * kKeysPerThread;
 
 // A float as a key that grows with it; -0 is 0.
 __device__ __forceinline__ uint32_t key_of(float x) {
@@ -20,117 +26,182 @@ __device__ __forceinline__ uint32_t key_of(float x) {
   return u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
 }
 
-template <int kThreads>
+// op over the wavefront, in every lane: rotations within the rows of 16 lanes, then rows with rows.
+template <int CTRL>
+__device__ __forceinline__ uint32_t moved(uint32_t x) {
+  return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), CTRL, 0xf, 0xf, true));
+}
+template <typename Op>
+__device__ __forceinline__ uint32_t over_rows(uint32_t x, Op op) {
+  auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = op(r[0], r[1]);
+  r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return op(r[0], r[1]);
+}
+template <typename Op>
+__device__ __forceinline__ uint32_t over_wave(uint32_t x, Op op) {
+  x = op(x, moved<0x128>(x));                                // row_ror 8, 4, 2, 1
+  x = op(x, moved<0x124>(x));
+  x = op(x, moved<0x122>(x));
+  x = op(x, moved<0x121>(x));
+  return over_rows(x, op);
+}
+__device__ __forceinline__ uint32_t wave_min(uint32_t x) { return over_wave(x, [](uint32_t a, uint32_t b) { return min(a, b); }); }
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) { return over_wave(x, [](uint32_t a, uint32_t b) { return max(a, b); }); }
+__device__ __forceinline__ uint32_t wave_sum(uint32_t x) { return over_wave(x, [](uint32_t a, uint32_t b) { return a + b; }); }
+// Sum over this lane and those above it.
+__device__ __forceinline__ uint32_t sum_from(uint32_t x, int lane) {
+  x += moved<0x101>(x);                                      // row_shl 1, 2, 4, 8: zeros come in
+  x += moved<0x102>(x);
+  x += moved<0x104>(x);
+  x += moved<0x108>(x);
+  const uint32_t r1 = __builtin_amdgcn_readlane(x, 16), r2 = __builtin_amdgcn_readlane(x, 32), r3 = __builtin_amdgcn_readlane(x, 48);
+  return x + (lane < 16 ? r1 : 0) + (lane < 32 ? r2 : 0) + (lane < 48 ? r3 : 0);
+}
+
+// A wait of the work-group for what it has written to LDS.  (__syncthreads() also waits for every load from memory that is under way.)
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 struct RankShared {
-  uint32_t hist[kBins];
-  uint32_t low[kThreads / 64], high[kThreads / 64];
-  uint32_t bin, above, inside;
-  uint32_t counts[2][kThreads / 64][2];       // chosen surely, ties: of a wavefront's keys
+  __attribute__((aligned(16))) uint32_t hist[kBins];
+  __attribute__((aligned(16))) uint32_t low[kRankWaves], high[kRankWaves];
+  uint32_t listed;
+  uint32_t list[64];
+  __attribute__((aligned(16))) uint2 counts[2][kRankWaves];  // chosen surely, ties: of a wavefront's keys
 };
+static_assert(kBins == 4 * kRankThreads && kRankWaves == 4, "four words together");
 
 struct Threshold {
   uint32_t key, ties;
 };
 
-// key(i), i in [begin, end), is read several times; 0 <= k <= end - begin.  All threads of the work-group call it and get the result.
-template <int kThreads, typename Key>
-__device__ __forceinline__ Threshold find_threshold(RankShared<kThreads>& sh, int begin, int end, uint32_t k, Key key, int tid) {
-  if (k == 0) return {0xffffffffu, 0};
-  if (k >= static_cast<uint32_t>(end - begin)) return {0, 0xffffffffu};
+// key(i), i in [begin, end), is read several times; 0 <= k <= end - begin.  low, high: the smallest and the largest of some of the keys, those of all
+// threads together being all (0xffffffff, 0: of none).  All threads of the work-group call it and get the result; what they have stored is there for
+// everybody after the wait that it begins with.
+template <typename Key>
+__device__ __forceinline__ Threshold find_threshold(RankShared& sh, int begin, int end, uint32_t k, uint32_t low, uint32_t high, Key key, int tid) {
   const int lane = tid & 63, wave = tid >> 6;
-  uint32_t low = 0xffffffffu, high = 0;
-  for (int i = begin + tid; i < end; i += kThreads) {
-    const uint32_t v = key(i);
-    low = min(low, v);
-    high = max(high, v);
-  }
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) {
-    low = min(low, __shfl_xor(low, d));
-    high = max(high, __shfl_xor(high, d));
-  }
+  low = wave_min(low);
+  high = wave_max(high);
   if (lane == 0) {
     sh.low[wave] = low;
     sh.high[wave] = high;
   }
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) {
-    low = min(low, sh.low[w]);
-    high = max(high, sh.high[w]);
-  }
+  reinterpret_cast<uint4*>(sh.hist)[tid] = make_uint4(0, 0, 0, 0);
+  if (tid == 0) sh.listed = 0;
+  lds_barrier();
+  if (k == 0) return {0xffffffffu, 0};
+  if (k >= static_cast<uint32_t>(end - begin)) return {0, 0xffffffffu};
+  low = min(min(sh.low[0], sh.low[1]), min(sh.low[2], sh.low[3]));
+  high = max(max(sh.high[0], sh.high[1]), max(sh.high[2], sh.high[3]));
   uint32_t base = low, limit = high - low;                   // keys base .. base + limit are in question
   while (limit > 0) {
-    const int shift = max(0, 24 - __builtin_clz(limit));
-    for (int i = tid; i < kBins; i += kThreads) sh.hist[i] = 0;
-    __syncthreads();
-    for (int i = begin + tid; i < end; i += kThreads) {
+    const int shift = max(0, 22 - __builtin_clz(limit));
+    for (int i = begin + tid; i < end; i += kRankThreads) {
       const uint32_t v = key(i), off = v - base;
       if (v >= base && off <= limit) atomicAdd(&sh.hist[off >> shift], 1u);
     }
-    __syncthreads();
-    if (wave == 0) {
-      uint32_t h[kBins / 64], sum = 0;
+    lds_barrier();
+    // every wavefront for itself: the bin where the count from above crosses k
+    constexpr int kOwn = kBins / 64;
+    uint32_t h[kOwn], sum = 0;
 #pragma unroll
-      for (int j = 0; j < kBins / 64; ++j) {
-        h[j] = sh.hist[lane * (kBins / 64) + j];
-        sum += h[j];
-      }
-      uint32_t from = sum;                                   // keys of this lane's bins and all above
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t other = __shfl_down(from, d);
-        from += lane + d < 64 ? other : 0;
-      }
-      uint32_t above = from - sum;
-      if (above < k && from >= k) {                          // in one lane
-#pragma unroll
-        for (int j = kBins / 64 - 1; j >= 0; --j) {
-          if (above < k && above + h[j] >= k) {
-            sh.bin = lane * (kBins / 64) + j;
-            sh.above = above;
-            sh.inside = h[j];
-          }
-          above += h[j];
-        }
-      }
+    for (int j = 0; j < kOwn; j += 4) {
+      const uint4 h4 = *reinterpret_cast<const uint4*>(&sh.hist[lane * kOwn + j]);
+      h[j] = h4.x;
+      h[j + 1] = h4.y;
+      h[j + 2] = h4.z;
+      h[j + 3] = h4.w;
+      sum += (h4.x + h4.y) + (h4.z + h4.w);
     }
-    __syncthreads();
-    k -= sh.above;
-    base += sh.bin << shift;
-    if (sh.inside == k) return {base, 0xffffffffu};          // all of the bin: those above its first key, and that one
+    const uint32_t from = sum_from(sum, lane);
+    const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(from - sum < k && from >= k));
+    uint32_t above = from - sum, bin = 0, taken = 0, inside = 0;
+#pragma unroll
+    for (int j = kOwn - 1; j >= 0; --j) {
+      if (above < k && above + h[j] >= k) {
+        bin = lane * kOwn + j;
+        taken = above;
+        inside = h[j];
+      }
+      above += h[j];
+    }
+    inside = __builtin_amdgcn_readlane(inside, at);
+    k -= __builtin_amdgcn_readlane(taken, at);
+    base += __builtin_amdgcn_readlane(bin, at) << shift;
+    if (inside == k) return {base, 0xffffffffu};             // all of the bin: those above its first key, and that one
     limit = (1u << shift) - 1;
+    if (limit == 0) break;
+    if (inside <= 64) {                                      // few: each against each, in every wavefront
+      for (int i = begin + tid; i < end; i += kRankThreads) {
+        const uint32_t v = key(i);
+        if (v >= base && v - base <= limit) sh.list[atomicAdd(&sh.listed, 1u)] = v;
+      }
+      lds_barrier();
+      const uint32_t mine = static_cast<uint32_t>(lane) < inside ? sh.list[lane] : 0;
+      uint32_t larger = 0, equal = 0;
+      for (uint32_t j = 0; j < inside; ++j) {
+        const uint32_t v = __builtin_amdgcn_readlane(mine, j);
+        larger += v > mine;
+        equal += v == mine;
+      }
+      const int here = __builtin_ctzll(__builtin_amdgcn_ballot_w64(static_cast<uint32_t>(lane) < inside && larger < k && larger + equal >= k));
+      return {static_cast<uint32_t>(__builtin_amdgcn_readlane(mine, here)), k - __builtin_amdgcn_readlane(larger, here)};
+    }
+    lds_barrier();                                           // everybody has read the bins
+    reinterpret_cast<uint4*>(sh.hist)[tid] = make_uint4(0, 0, 0, 0);
+    lds_barrier();
   }
   return {base, k};
 }
 
-// How many keys before this thread's are chosen, and whether its own is; keys come kThreads at a time in order, thread after thread.
+// Rounds of kRankRound keys in order, thread t's being 4 t .. 4 t + 3 of a round: which are chosen, and how many keys before each are.
 struct Places {
   uint32_t sure = 0, ties = 0;
   int turn = 0;
 };
-template <int kThreads>
-__device__ __forceinline__ uint32_t place(RankShared<kThreads>& sh, Places& p, const Threshold& t, bool in, uint32_t key, int tid, bool& chosen) {
+__device__ __forceinline__ void place_keys(RankShared& sh, Places& p, const Threshold& t, const bool (&in)[kKeysPerThread], const uint32_t (&key)[kKeysPerThread],
+                                           int tid, bool (&chosen)[kKeysPerThread], uint32_t (&at)[kKeysPerThread]) {
   const int lane = tid & 63, wave = tid >> 6;
-  const bool above = in && key > t.key, tie = in && key == t.key;
-  const uint64_t a = __builtin_amdgcn_ballot_w64(above), b = __builtin_amdgcn_ballot_w64(tie), before = (uint64_t{1} << lane) - 1;
-  if (lane == 0) {
-    sh.counts[p.turn][wave][0] = __builtin_popcountll(a);
-    sh.counts[p.turn][wave][1] = __builtin_popcountll(b);
-  }
-  __syncthreads();
-  uint32_t sure = p.sure + __builtin_popcountll(a & before), ties = p.ties + __builtin_popcountll(b & before);
+  bool above[kKeysPerThread], tie[kKeysPerThread];
+  uint32_t sure = 0, ties = 0, all_sure = 0, all_ties = 0;   // before this thread's first key, and of the wavefront
+  auto below = [](uint64_t mask, uint32_t add) {             // of the lanes below this one
+    return __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(mask >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(mask), add));
+  };
 #pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) {
-    const uint32_t s = sh.counts[p.turn][w][0], n = sh.counts[p.turn][w][1];
-    sure += w < wave ? s : 0;
-    ties += w < wave ? n : 0;
-    p.sure += s;
-    p.ties += n;
+  for (int j = 0; j < kKeysPerThread; ++j) {
+    above[j] = in[j] && key[j] > t.key;
+    tie[j] = in[j] && key[j] == t.key;
+    const uint64_t a = __builtin_amdgcn_ballot_w64(above[j]), b = __builtin_amdgcn_ballot_w64(tie[j]);
+    sure = below(a, sure);
+    ties = below(b, ties);
+    all_sure += __builtin_popcountll(a);
+    all_ties += __builtin_popcountll(b);
+  }
+  if (lane == 0) sh.counts[p.turn][wave] = make_uint2(all_sure, all_ties);
+  lds_barrier();
+  sure += p.sure;
+  ties += p.ties;
+#pragma unroll
+  for (int w = 0; w < kRankWaves; ++w) {
+    const uint2 c = sh.counts[p.turn][w];
+    sure += w < wave ? c.x : 0;
+    ties += w < wave ? c.y : 0;
+    p.sure += c.x;
+    p.ties += c.y;
   }
   p.turn ^= 1;
-  chosen = above || (tie && ties < t.ties);
-  return sure + min(ties, t.ties);
+#pragma unroll
+  for (int j = 0; j < kKeysPerThread; ++j) {
+    chosen[j] = above[j] || (tie[j] && ties < t.ties);
+    at[j] = sure + min(ties, t.ties);
+    sure += above[j];
+    ties += tie[j];
+  }
 }
 
 }  // namespace

@@ -5,10 +5,15 @@
 // per 16 pages and 16 query heads, {c, w} of a block being 64 bytes in the order the instruction reads them -- times the block's
 // scales in fp32; whole numbers below 2^24 and fp32 operations that are rounded one by one make it the same for whoever computes it.
 //
+// Few (sequence, KV head) units with many pages share a unit's pages among work-groups: one compute unit has about 60 lines of 128 bytes
+// under way, and 1024 pages of 272 bytes took one 9.5 us.  The keys go to the workspace past the caches, and whoever registers last at the unit's
+// arrival word makes the choice (pq_decode_sched.hpp): one launch, nobody waits for anybody.
+//
 // A choice is a row of a block table: page and KV head are one index into the pools taken head by head, so that attention over the
 // chosen pages is decode attention of n_seqs * n_kv_heads sequences with one KV head each.
 #include <hip/hip_runtime.h>
 
+#include "pq_decode_sched.hpp"
 #include "pq_internal.hpp"
 #include "pq_rank.hpp"
 
@@ -33,10 +38,12 @@ struct SelectArgs {
   const int32_t* seq_lens;
   int32_t* selected;
   int32_t* selected_lens;
-  uint32_t* keys;                                            // [sequence][KV head][max_pages], if they do not stay in LDS
-  int64_t n_pool_pages;
+  uint64_t* arrivals;                                        // one word a unit; of units shared among work-groups
+  uint32_t* keys;                                            // [unit][max_pages], of the same
+  int32_t n_pool_pages;
   int32_t n_kv_heads, group, max_pages_per_seq, max_seq_len, max_pages;
   int32_t n_selected, n_first, n_last;
+  int32_t part_pages;                                        // pages of a work-group; max_pages at least: of all
   int32_t q_is_f32;
 };
 
@@ -49,22 +56,41 @@ struct QueryOperand {
   i32x4 code[kBlocks][64];
   float largest[kBlocks];
 };
-__device__ __forceinline__ void make_operand(QueryOperand& o, const SelectArgs& a, int64_t head0, int b, int lane) {
-  const int64_t at = (head0 + min(lane & 15, a.group - 1)) * kHeadDim + ((lane >> 4) & 1) * kPairs + b * 16;
-  float v[16];
-  if (a.q_is_f32) {
-    __builtin_memcpy(v, static_cast<const float*>(a.q) + at, sizeof(v));
-  } else {
-    _Float16 h[16];
-    __builtin_memcpy(h, static_cast<const _Float16*>(a.q) + at, sizeof(h));
+// What a lane of block b's operand is made of, as it lies in memory.
+struct QueryFetch {
+  uint4 w[4];
+  __device__ __forceinline__ QueryFetch(const SelectArgs& a, int64_t head0, int b, int lane) {
+    const int64_t at = (head0 + min(lane & 15, a.group - 1)) * kHeadDim + ((lane >> 4) & 1) * kPairs + b * 16;
+    if (a.q_is_f32) {
+      const uint4* const src = reinterpret_cast<const uint4*>(static_cast<const float*>(a.q) + at);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = static_cast<float>(h[i]);
+      for (int i = 0; i < 4; ++i) w[i] = src[i];
+    } else {
+      const uint4* const src = reinterpret_cast<const uint4*>(static_cast<const _Float16*>(a.q) + at);
+      w[0] = src[0];
+      w[1] = src[1];
+    }
+  }
+  __device__ __forceinline__ float value(bool f32, int i) const {
+    const uint32_t wide[4] = {w[i / 4].x, w[i / 4].y, w[i / 4].z, w[i / 4].w};
+    if (f32) return __builtin_bit_cast(float, wide[i % 4]);
+    const uint32_t two[4] = {w[i / 8].x, w[i / 8].y, w[i / 8].z, w[i / 8].w};
+    return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(two[i / 2 % 4] >> (16 * (i & 1)))));
+  }
+};
+__device__ __forceinline__ void store_operand(QueryOperand& o, const QueryFetch& f, bool f32, int b, int lane) {
+  float v[16];
+  if (f32) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = f.value(true, i);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = f.value(false, i);
   }
   float m = 0.f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(v[i]));
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+  m = __builtin_bit_cast(float, wave_max(__builtin_bit_cast(uint32_t, m)));                  // (not negative: in the order of its bits)
   const float up = m >= kTiny ? 127.0f / m : 0.f;
   i32x4 code;
 #pragma unroll
@@ -81,101 +107,158 @@ __device__ __forceinline__ void make_operand(QueryOperand& o, const SelectArgs& 
   if (lane == 0) o.largest[b] = m;
 }
 
-// Keys of the scores of pages first .. first + 15, page l % 16 in every lane.
-__device__ __forceinline__ uint32_t tile_keys(const QueryOperand& o, const SelectArgs& a, const int32_t* row, int kvh, int first, int pages, int lane) {
-  const int p = first + (lane & 15);
-  const int64_t page = p < pages ? row[p] : -1;
-  const bool there = page >= 0 && page < a.n_pool_pages;
-  const int64_t ph = there ? page * a.n_kv_heads + kvh : 0;
-  const int8_t* const bound = a.bounds + ph * kBoundBytes + (lane >> 4) * 16;
-  i32x4 b[kBlocks];
+// Pages first .. first + 15 of a sequence, page first + l % 16 in every lane: block-table entry, bounds, scales, and what comes of them.
+struct Tile {
+  int32_t id;
+  i32x4 bound[kBlocks];
+  float4 scale;
+  __device__ __forceinline__ bool there(const SelectArgs& a) const { return id >= 0 && id < a.n_pool_pages; }
+  // (p < a.max_pages is in the row whatever the sequence's length)
+  __device__ __forceinline__ void load_id(const SelectArgs& a, const int32_t* row, int p) { id = p < a.max_pages ? row[p] : -1; }
+  __device__ __forceinline__ void load(const SelectArgs& a, int kvh, int lane) {
+    const int64_t ph = there(a) ? id * a.n_kv_heads + kvh : 0;                     // (below 2^31: checked on the host)
+    const int8_t* const from = a.bounds + ph * kBoundBytes + (lane >> 4) * 16;
 #pragma unroll
-  for (int i = 0; i < kBlocks; ++i) b[i] = *reinterpret_cast<const i32x4*>(bound + i * kBlockBytes);
-  const float4 scale = *reinterpret_cast<const float4*>(a.scales + ph * kBlocks);
-  const float u[kBlocks] = {o.largest[0] * scale.x, o.largest[1] * scale.y, o.largest[2] * scale.z, o.largest[3] * scale.w};
-  i32x4 n[kBlocks];
-#pragma unroll
-  for (int i = 0; i < kBlocks; ++i) n[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(o.code[i][lane], b[i], i32x4{0, 0, 0, 0}, 0, 0, 0);
-  float best = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {                              // heads 4 (l / 16) + i
-    float t[kBlocks];
-#pragma unroll
-    for (int j = 0; j < kBlocks; ++j) t[j] = static_cast<float>(n[j][i]) * u[j];
-    best = fmaxf(best, (t[0] + t[1]) + (t[2] + t[3]));
+    for (int i = 0; i < kBlocks; ++i) bound[i] = *reinterpret_cast<const i32x4*>(from + i * kBlockBytes);
+    scale = *reinterpret_cast<const float4*>(a.scales + ph * kBlocks);
   }
-  best = fmaxf(best, __shfl_xor(best, 16));
-  best = fmaxf(best, __shfl_xor(best, 32));
-  return key_of(there ? best : -INFINITY);
-}
-
-// Scores alone, of long sequences: one work-group 64 tiles of a (sequence, KV head).
-constexpr int kScoreThreads = 256;
-constexpr int kScorePages = 64 * kTilePages;
-__global__ __launch_bounds__(kScoreThreads) void pq_page_scores_kernel(const SelectArgs a) {
-  __shared__ __attribute__((aligned(16))) QueryOperand o;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, kvh = blockIdx.y, seq = blockIdx.z;
-  const int pages = pages_up(clamped(a, seq)), first = blockIdx.x * kScorePages;
-  if (first >= pages || pages <= a.n_selected) return;
-  make_operand(o, a, (static_cast<int64_t>(seq) * a.n_kv_heads + kvh) * a.group, wave, lane);
-  __syncthreads();
-  const int32_t* const row = a.block_table + static_cast<int64_t>(seq) * a.max_pages_per_seq;
-  uint32_t* const keys = a.keys + (static_cast<int64_t>(seq) * a.n_kv_heads + kvh) * a.max_pages;
-  for (int p = first + wave * kTilePages; p < min(pages, first + kScorePages); p += kScoreThreads / 64 * kTilePages) {
-    const uint32_t key = tile_keys(o, a, row, kvh, p, pages, lane);
-    if (lane < kTilePages && p + lane < pages) keys[p + lane] = key;
+  __device__ __forceinline__ uint32_t key(const SelectArgs& a, const QueryOperand& o, int lane) const {
+    const float u[kBlocks] = {o.largest[0] * scale.x, o.largest[1] * scale.y, o.largest[2] * scale.z, o.largest[3] * scale.w};
+    i32x4 n[kBlocks];
+#pragma unroll
+    for (int i = 0; i < kBlocks; ++i) n[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(o.code[i][lane], bound[i], i32x4{0, 0, 0, 0}, 0, 0, 0);
+    float best = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {                            // heads 4 (l / 16) + i
+      float t[kBlocks];
+#pragma unroll
+      for (int j = 0; j < kBlocks; ++j) t[j] = static_cast<float>(n[j][i]) * u[j];
+      best = fmaxf(best, (t[0] + t[1]) + (t[2] + t[3]));
+    }
+    // (no other order of floats than fmaxf's: the largest key would not be the same where a score is no number)
+    best = __builtin_bit_cast(float, over_rows(__builtin_bit_cast(uint32_t, best), [](uint32_t x, uint32_t y) {
+      return __builtin_bit_cast(uint32_t, fmaxf(__builtin_bit_cast(float, x), __builtin_bit_cast(float, y)));
+    }));
+    return key_of(there(a) ? best : -INFINITY);
   }
-}
+};
+// Tiles of a wavefront whose loads are under way together: a block-table entry and then the bounds are two waits for memory, for all of them.
+constexpr int kTilesAtOnce = 4;
+constexpr int kRoundPages = kRankWaves * kTilePages;         // a tile each
+constexpr int kBatchPages = kTilesAtOnce * kRoundPages;
 
-// kScored: pq_page_scores_kernel has left the keys in memory.
-template <int kThreads, bool kScored>
-__global__ __launch_bounds__(kThreads) void pq_select_kernel(const SelectArgs a) {
-  __shared__ RankShared<kThreads> rank;
+// kTiles: of a wavefront at once; 4 but for parts of fewer.
+template <int kTiles>
+__global__ __launch_bounds__(kRankThreads) void pq_select_kernel(const SelectArgs a) {
+  __shared__ RankShared rank;
   __shared__ __attribute__((aligned(16))) QueryOperand o;
-  __shared__ uint32_t in_lds[kScored ? 1 : kMostKeys];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, kvh = blockIdx.x, seq = blockIdx.y;
-  const int len = clamped(a, seq), pages = pages_up(len);
+  __shared__ __attribute__((aligned(16))) uint32_t in_lds[kMostKeys];
+  __shared__ int stage;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, kvh = blockIdx.x, seq = blockIdx.y, part = blockIdx.z;
   const int64_t unit = static_cast<int64_t>(seq) * a.n_kv_heads + kvh;
   const int32_t* const row = a.block_table + static_cast<int64_t>(seq) * a.max_pages_per_seq;
   int32_t* const out = a.selected + unit * a.n_selected;
-  auto name = [&](int p) {                                   // the page's row in the pools taken head by head
-    const int64_t page = row[p];
-    return page >= 0 && page < a.n_pool_pages ? static_cast<int32_t>(page * a.n_kv_heads + kvh) : -1;
-  };
+  // the page's row in the pools taken head by head
+  auto name = [&](int32_t page) { return page >= 0 && page < a.n_pool_pages ? page * a.n_kv_heads + kvh : -1; };
+  Tile tile[kTiles];
+  const int part0 = part * a.part_pages, first = part0 + wave * kTilePages + (lane & 15);   // (tiles in turn: all wavefronts have some)
+#pragma unroll
+  for (int j = 0; j < kTiles; ++j) tile[j].load_id(a, row, first + j * kRoundPages);
+  const QueryFetch f(a, unit * a.group, wave, lane);
+  const int len = clamped(a, seq), pages = pages_up(len);
   if (pages <= a.n_selected) {
-    for (int p = tid; p < a.n_selected; p += kThreads) out[p] = p < pages ? name(p) : -1;
+    if (part != 0) return;
+    for (int p = tid; p < a.n_selected; p += kRankThreads) out[p] = p < pages ? name(row[p]) : -1;
     if (tid == 0) a.selected_lens[unit] = len;
     return;
   }
-  const uint32_t* const stored = kScored ? a.keys + unit * a.max_pages : nullptr;
-  auto key = [&](int p) { return kScored ? stored[p] : in_lds[p]; };
-  const int begin = a.n_first, end = pages - a.n_last, n_free = a.n_selected - a.n_first - a.n_last;
-  if constexpr (!kScored) {
-    if (wave < kBlocks) make_operand(o, a, unit * a.group, wave, lane);
-    __syncthreads();
-    for (int p = wave * kTilePages; p < pages; p += kThreads / 64 * kTilePages) {
-      const uint32_t k = tile_keys(o, a, row, kvh, p, pages, lane);
-      if (lane < kTilePages && p + lane < pages) in_lds[p + lane] = k;
+  if (part0 >= pages) return;
+  const int parts = (pages + a.part_pages - 1) / a.part_pages, part_end = min(pages, part0 + a.part_pages);
+  const int begin = a.n_first, end = pages - a.n_last;       // pages there is a choice of
+  const bool shared = parts > 1, in_memory = shared && pages > kMostKeys;
+  const __amdgpu_buffer_rsrc_t r_keys = make_rsrc(a.keys + (shared ? unit * a.max_pages : 0), shared ? static_cast<uint32_t>(pages) * 4u : 0u);
+  uint32_t low = 0xffffffffu, high = 0;
+  for (int done = 0; part0 + done < part_end; done += kTiles * kRoundPages) {
+    if (done > 0) {
+#pragma unroll
+      for (int j = 0; j < kTiles; ++j) tile[j].load_id(a, row, done + first + j * kRoundPages);
     }
+#pragma unroll
+    for (int j = 0; j < kTiles; ++j) tile[j].load(a, kvh, lane);
+    if (done == 0) {
+      store_operand(o, f, a.q_is_f32 != 0, wave, lane);
+      __syncthreads();
+    }
+#pragma unroll
+    for (int j = 0; j < kTiles; ++j) {
+      const int p = done + first + j * kRoundPages;
+      const uint32_t k = tile[j].key(a, o, lane);
+      if (lane < kTilePages && p < part_end) {
+        if (shared) __builtin_amdgcn_raw_buffer_store_b32(k, r_keys, p * 4, 0, kAuxDevice);
+        else in_lds[p] = k;
+      }
+      if (p >= begin && p < end) {
+        low = min(low, k);
+        high = max(high, k);
+      }
+    }
+  }
+  if (shared) {
+    stores_done();
     __syncthreads();
+    if (tid == 0) stage = arrive(a.arrivals + unit, parts) ? 1 : 0;
+    __syncthreads();
+    if (stage == 0) return;
+    low = 0xffffffffu;
+    high = 0;
+    for (int p = tid; p < pages; p += kRankThreads) {
+      const uint32_t k = __builtin_amdgcn_raw_buffer_load_b32(r_keys, p * 4, 0, kAuxDevice);
+      if (!in_memory) in_lds[p] = k;
+      if (p >= begin && p < end) {
+        low = min(low, k);
+        high = max(high, k);
+      }
+    }
+    if (tid == 0) reset_arrivals(a.arrivals + unit);
   }
-  const Threshold t = find_threshold<kThreads>(rank, begin, end, static_cast<uint32_t>(n_free), key, tid);
+  auto key = [&](int p) { return in_memory ? __builtin_amdgcn_raw_buffer_load_b32(r_keys, p * 4, 0, kAuxDevice) : in_lds[p]; };
+  int32_t id[kKeysPerThread];
+#pragma unroll
+  for (int j = 0; j < kKeysPerThread; ++j) id[j] = tid * kKeysPerThread + j < pages ? row[tid * kKeysPerThread + j] : -1;
+  const Threshold t = find_threshold(rank, begin, end, static_cast<uint32_t>(a.n_selected - a.n_first - a.n_last), low, high, key, tid);
   Places places;
-  for (int base = begin; base < end; base += kThreads) {
-    const int p = base + tid;
-    bool chosen;
-    const uint32_t at = place<kThreads>(rank, places, t, p < end, p < end ? key(p) : 0, tid, chosen);
-    if (chosen) out[a.n_first + at] = name(p);
+  for (int base = 0; base < pages; base += kRankRound) {
+    const int p0 = base + tid * kKeysPerThread;
+    bool in[kKeysPerThread], chosen[kKeysPerThread];
+    uint32_t k[kKeysPerThread], at[kKeysPerThread];
+#pragma unroll
+    for (int j = 0; j < kKeysPerThread; ++j) {
+      in[j] = p0 + j >= begin && p0 + j < end;
+      k[j] = in[j] ? key(p0 + j) : 0;
+      if (base > 0) id[j] = p0 + j < pages ? row[p0 + j] : -1;
+    }
+    place_keys(rank, places, t, in, k, tid, chosen, at);
+#pragma unroll
+    for (int j = 0; j < kKeysPerThread; ++j) {
+      const int p = p0 + j, to = chosen[j] ? a.n_first + static_cast<int>(at[j]) : (p < begin ? p : (p >= end ? a.n_selected - pages + p : -1));
+      if (to >= 0 && p < pages) out[to] = name(id[j]);
+    }
   }
-  for (int p = tid; p < a.n_first; p += kThreads) out[p] = name(p);
-  for (int p = tid; p < a.n_last; p += kThreads) out[a.n_selected - a.n_last + p] = name(end + p);
   if (tid == 0) a.selected_lens[unit] = len - (pages - a.n_selected) * kGroup;
 }
 
 int64_t most_pages(int32_t max_seq_len) { return (static_cast<int64_t>(max_seq_len) + kGroup - 1) / kGroup; }
 
-// Whether the scores take a launch of their own.
-bool scores_apart(int32_t max_seq_len) { return most_pages(max_seq_len) > kMostKeys; }
+// Pages of a work-group: all of a unit's, if that is one batch of loads a wavefront or the units fill the compute units; otherwise as few as make
+// no more than two work-groups a compute unit.
+int32_t pages_of_part(const pq_layout* l, int32_t n_seqs, int32_t max_seq_len) {
+  const int64_t pages = most_pages(max_seq_len), units = static_cast<int64_t>(n_seqs) * l->n_kv_heads;
+  if (pages <= kBatchPages || (units >= kComputeUnits && pages <= kMostKeys)) return static_cast<int32_t>(std::min<int64_t>(pages, kMostKeys));
+  for (int tiles = 1; tiles < kTilesAtOnce; tiles *= 2)
+    if (units * ((pages + tiles * kRoundPages - 1) / (tiles * kRoundPages)) <= kResidentGroups) return tiles * kRoundPages;
+  return kBatchPages;
+}
+bool shares_units(const pq_layout* l, int32_t n_seqs, int32_t max_seq_len) { return pages_of_part(l, n_seqs, max_seq_len) < most_pages(max_seq_len); }
 
 int check_selection(const pq_layout* l, int32_t n_seqs, int32_t n_q_heads, int32_t max_seq_len, int32_t n_selected, int32_t n_first, int32_t n_last) {
   if (!l || n_seqs <= 0 || n_q_heads <= 0 || max_seq_len <= 0) return PQ_ERR_INVALID_ARG;
@@ -183,12 +266,16 @@ int check_selection(const pq_layout* l, int32_t n_seqs, int32_t n_q_heads, int32
   if (n_first < 0 || n_last < 1 || static_cast<int64_t>(n_first) + n_last > n_selected) return PQ_ERR_INVALID_ARG;
   if (!layout_supported(l)) return PQ_ERR_UNSUPPORTED;
   if (n_q_heads / l->n_kv_heads > 16 || static_cast<int64_t>(n_seqs) * l->n_kv_heads > 65535) return PQ_ERR_UNSUPPORTED;
+  if (most_pages(max_seq_len) > 65535 * int64_t{kBatchPages}) return PQ_ERR_UNSUPPORTED;      // grid.z, and a count of 16 bits at an arrival word
   return PQ_OK;
 }
 
+size_t round256(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
+size_t arrival_bytes(const pq_layout* l, int32_t n_seqs) { return round256(static_cast<size_t>(n_seqs) * l->n_kv_heads * sizeof(uint64_t)); }
+// The arrival words, then the keys.
 size_t select_bytes(const pq_layout* l, int32_t n_seqs, int32_t max_seq_len) {
-  const size_t keys = scores_apart(max_seq_len) ? static_cast<size_t>(n_seqs) * l->n_kv_heads * most_pages(max_seq_len) * sizeof(uint32_t) : 0;
-  return std::max<size_t>(256, (keys + 255) & ~static_cast<size_t>(255));
+  if (!shares_units(l, n_seqs, max_seq_len)) return 256;
+  return arrival_bytes(l, n_seqs) + round256(static_cast<size_t>(n_seqs) * l->n_kv_heads * most_pages(max_seq_len) * sizeof(uint32_t));
 }
 
 // The arguments that the selection reads or writes, beyond check_selection().
@@ -217,8 +304,9 @@ int launch_selection(const pq_layout* l, const void* q, pq_dtype q_dtype, int32_
   a.seq_lens = seq_lens;
   a.selected = selected;
   a.selected_lens = selected_lens;
-  a.keys = static_cast<uint32_t*>(workspace);
-  a.n_pool_pages = n_pool_pages;
+  a.arrivals = static_cast<uint64_t*>(workspace);
+  a.keys = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(workspace) + (shares_units(l, n_seqs, max_seq_len) ? arrival_bytes(l, n_seqs) : 0));
+  a.n_pool_pages = static_cast<int32_t>(n_pool_pages);
   a.n_kv_heads = l->n_kv_heads;
   a.group = n_q_heads / l->n_kv_heads;
   a.max_pages_per_seq = max_pages_per_seq;
@@ -228,17 +316,11 @@ int launch_selection(const pq_layout* l, const void* q, pq_dtype q_dtype, int32_
   a.n_first = n_first;
   a.n_last = n_last;
   a.q_is_f32 = q_dtype == PQ_F32 ? 1 : 0;
-  const dim3 grid(l->n_kv_heads, n_seqs);
-  if (scores_apart(max_seq_len)) {
-    hipLaunchKernelGGL(pq_page_scores_kernel, dim3((a.max_pages + kScorePages - 1) / kScorePages, l->n_kv_heads, n_seqs), dim3(kScoreThreads), 0, st, a);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return record_hip_error(e);
-    hipLaunchKernelGGL((pq_select_kernel<1024, true>), grid, dim3(1024), 0, st, a);
-  } else if (a.max_pages > 256) {
-    hipLaunchKernelGGL((pq_select_kernel<1024, false>), grid, dim3(1024), 0, st, a);
-  } else {
-    hipLaunchKernelGGL((pq_select_kernel<256, false>), grid, dim3(256), 0, st, a);
-  }
+  a.part_pages = pages_of_part(l, n_seqs, max_seq_len);
+  const dim3 grid(l->n_kv_heads, n_seqs, (a.max_pages + a.part_pages - 1) / a.part_pages);
+  if (a.part_pages <= kRoundPages) hipLaunchKernelGGL(pq_select_kernel<1>, grid, dim3(kRankThreads), 0, st, a);
+  else if (a.part_pages <= 2 * kRoundPages) hipLaunchKernelGGL(pq_select_kernel<2>, grid, dim3(kRankThreads), 0, st, a);
+  else hipLaunchKernelGGL(pq_select_kernel<kTilesAtOnce>, grid, dim3(kRankThreads), 0, st, a);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? PQ_OK : record_hip_error(e);
 }
