@@ -22,12 +22,12 @@ namespace {
 constexpr int kMergeThreads = 256;
 constexpr int kMergeSlices = kMergeThreads / 32;
 
-// kWindow: the lengths are what a sliding window leaves of them.  kWeights: the heads' maxima and sums are left in `totals`.
-template <bool kWindow, bool kWeights = false>
-__global__ __launch_bounds__(kMergeThreads) void pq_decode_merge_kernel(
+// kWindow: the lengths are what a sliding window leaves of them.
+template <bool kWindow>
+__device__ __forceinline__ void merge_chunks(
     const float* __restrict__ ws_acc, const float* __restrict__ ws_ml,
     const int32_t* __restrict__ seq_lens, float* __restrict__ out, int32_t n_q_heads,
-    int32_t max_seq_len, int32_t pages_per_chunk, int32_t n_chunks, int32_t n_big, int32_t pages_small, int32_t window, int32_t n_sinks, float2* totals) {
+    int32_t max_seq_len, int32_t pages_per_chunk, int32_t n_chunks, int32_t n_big, int32_t pages_small, int32_t window, int32_t n_sinks) {
   __shared__ float4 part_o[kMergeSlices][32];
   __shared__ float part_l[kMergeSlices];
   __shared__ float wave_max[kMergeThreads / 64];
@@ -82,10 +82,14 @@ __global__ __launch_bounds__(kMergeThreads) void pq_decode_merge_kernel(
     }
     const float inv = lt > 0.f ? 1.f / lt : 0.f;
     reinterpret_cast<float4*>(out + oh * kHeadDim)[quad] = make_float4(r.x * inv, r.y * inv, r.z * inv, r.w * inv);
-    if constexpr (kWeights) {
-      if (quad == 0) totals[oh] = make_float2(M, lt);
-    }
   }
+}
+template <bool kWindow>
+__global__ __launch_bounds__(kMergeThreads) void pq_decode_merge_kernel(
+    const float* __restrict__ ws_acc, const float* __restrict__ ws_ml,
+    const int32_t* __restrict__ seq_lens, float* __restrict__ out, int32_t n_q_heads,
+    int32_t max_seq_len, int32_t pages_per_chunk, int32_t n_chunks, int32_t n_big, int32_t pages_small, int32_t window, int32_t n_sinks) {
+  merge_chunks<kWindow>(ws_acc, ws_ml, seq_lens, out, n_q_heads, max_seq_len, pages_per_chunk, n_chunks, n_big, pages_small, window, n_sinks);
 }
 
 // Score-only kernels on the vector unit: the kernel whose lanes are tokens on the uniform grid; the grouped quantizer
@@ -419,7 +423,7 @@ int decode_launch(const pq_layout* layout, const void* q, pq_dtype q_dtype, int3
   if (out != nullptr && !merged) {
     hipLaunchKernelGGL(pq_decode_merge_kernel<false>, dim3(n_q_heads, n_seqs), dim3(kMergeThreads), 0, stream, ws.acc,
                        ws.ml, seq_lens, out, n_q_heads, max_seq_len, plan.pages_per_chunk, plan.n_chunks, plan.n_big,
-                       plan.pages_small, 0, 0, nullptr);
+                       plan.pages_small, 0, 0);
     e = hipGetLastError();
     if (e != hipSuccess) return record_hip_error(e);
   }
@@ -470,7 +474,7 @@ extern "C" int pq_decode_merge(const pq_layout* layout, int32_t n_seqs, int32_t 
   hipLaunchKernelGGL(pq_decode_merge_kernel<false>, dim3(n_q_heads, n_seqs), dim3(kMergeThreads), 0,
                      static_cast<hipStream_t>(hip_stream), ws.acc, ws.ml, seq_lens, out, n_q_heads,
                      max_seq_len, plan.pages_per_chunk, plan.n_chunks, plan.n_big,
-                       plan.pages_small, 0, 0, nullptr);
+                       plan.pages_small, 0, 0);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return record_hip_error(e);
   return PQ_OK;
@@ -575,7 +579,49 @@ extern "C" int pq_window_attention(const pq_layout* layout, const void* q, pq_dt
   }
   if (e == hipSuccess && !merged) {
     hipLaunchKernelGGL(pq_decode_merge_kernel<true>, dim3(n_q_heads, n_seqs), dim3(kMergeThreads), 0, stream, ws.acc, ws.ml, seq_lens, out, n_q_heads,
-                       max_seq_len, plan.pages_per_chunk, plan.n_chunks, plan.n_big, plan.pages_small, a.window, a.n_sinks, nullptr);
+                       max_seq_len, plan.pages_per_chunk, plan.n_chunks, plan.n_big, plan.pages_small, a.window, a.n_sinks);
+    e = hipGetLastError();
+  }
+  return e == hipSuccess ? PQ_OK : record_hip_error(e);
+}
+
+// Chunks as for a window: sequences are alike, as many chunks as start at once (the general plan makes chunks of 8 or 16 pages: 128 units of 48 pages are
+// then 384 work-groups, 46.8 us; in fours of 12 pages 512, 44.3).
+size_t pq::alike_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_t n_q_heads, int32_t max_seq_len) {
+  const size_t general = pq_decode_workspace_bytes(layout, n_seqs, n_q_heads, max_seq_len);
+  const ChunkPlan plan = plan_window(layout, n_seqs, max_seq_len);
+  if (general == 0 || plan.n_chunks > 65535) return 0;                         // grid.z
+  return std::max(general, carve_window_workspace(nullptr, layout, n_seqs, n_q_heads, plan).bytes);
+}
+
+int pq::attend_alike(const pq_layout* layout, const void* q, pq_dtype q_dtype, int32_t n_seqs, int32_t n_q_heads, const void* codes_pool,
+                     const void* params_pool, const void* v_pool, int32_t v_bits, const void* v_params_pool, int64_t n_pool_pages,
+                     const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* seq_lens, int32_t max_seq_len, float sm_scale, float* out,
+                     const void* residual_keys, void* workspace, hipStream_t stream) {
+  const bool grouped = layout->angle_quantizer == PQ_ANGLE_GROUPED;
+  if (grouped && !grouped_on_matrix(layout, n_q_heads / layout->n_kv_heads))  // (whose chunks are whole rounds)
+    return pq_decode_attention(layout, q, q_dtype, n_seqs, n_q_heads, codes_pool, params_pool, v_pool, v_bits, v_params_pool, n_pool_pages, block_table,
+                               max_pages_per_seq, seq_lens, max_seq_len, sm_scale, out, nullptr, 0, residual_keys, workspace,
+                               pq_decode_workspace_bytes(layout, n_seqs, n_q_heads, max_seq_len), stream);
+  const ChunkPlan plan = plan_window(layout, n_seqs, max_seq_len);
+  const Workspace ws = carve_window_workspace(workspace, layout, n_seqs, n_q_heads, plan);
+  DecodeArgs a = attention_args(layout, q, q_dtype, n_seqs, n_q_heads, codes_pool, params_pool, v_pool, v_params_pool, n_pool_pages, block_table,
+                                max_pages_per_seq, seq_lens, max_seq_len, sm_scale, out, residual_keys, ws, plan);
+  // (few units, too: 8 of 32 pages 22.5 us with a merge launch, 22.0 so)
+  const bool merged = plan.n_chunks <= kMergeFan;
+  a.merge_in_kernel = merged ? 1 : 0;
+  a.wide_groups = wide_groups(layout, plan, n_seqs, max_seq_len) ? 1 : 0;
+  const dim3 grid(layout->n_kv_heads, n_seqs, plan.n_chunks);
+  hipError_t e = hipSuccess;
+  for (a.head0 = 0; a.head0 < a.group_total && e == hipSuccess; a.head0 += a.n_heads) {
+    a.n_heads = std::min(a.group_total - a.head0, kMaxHeads);
+    if (grouped) launch_grouped(layout->r_bits * 10 + layout->t_bits, v_bits, a, grid, stream);
+    else launch_attention(layout->r_bits + layout->t_bits, v_bits, false, a, grid, stream);
+    e = hipGetLastError();
+  }
+  if (e == hipSuccess && !merged) {
+    hipLaunchKernelGGL(pq_decode_merge_kernel<false>, dim3(n_q_heads, n_seqs), dim3(kMergeThreads), 0, stream, ws.acc, ws.ml, seq_lens, out, n_q_heads,
+                       max_seq_len, plan.pages_per_chunk, plan.n_chunks, plan.n_big, plan.pages_small, 0, 0);
     e = hipGetLastError();
   }
   return e == hipSuccess ? PQ_OK : record_hip_error(e);
@@ -586,30 +632,77 @@ namespace {
 
 // weights[seq][page] = decay * before[seq][page] + the sum over the query heads of l 2^(m - M) / L, (m, l) being the page's maximum and sum, (M, L)
 // the head's.  Thread = (page, slice of the heads); a slice takes every kWeightSlices-th head.
-constexpr int kWeightPages = 64, kWeightSlices = 4;
-__global__ __launch_bounds__(kWeightPages* kWeightSlices) void pq_page_weights_kernel(
-    const float2* __restrict__ page_ml, const float2* __restrict__ totals, const int32_t* __restrict__ seq_lens, const float* before, float* weights,
-    int64_t weights_stride, int32_t page_stride, int32_t n_q_heads, int32_t max_seq_len, float decay) {
+// kMerge: the chunks' partials are still to be combined.  The first n_q_heads work-groups of a sequence do that, as pq_decode_merge_kernel does, and
+// the others find (M, L) of their heads from the chunks' by themselves: one launch instead of two (one sequence of 3000 tokens 19.5 -> 16.5 us).
+constexpr int kWeightPages = 16, kWeightSlices = kMergeThreads / kWeightPages;
+static_assert(kWeightPages == 16, "a slice is a row of 16 lanes");
+struct WeightsArgs {
+  const float2* page_ml;
+  const float2* totals;
+  const int32_t* seq_lens;
+  const float* before;
+  float* weights;
+  const float* ws_acc;                                       // kMerge: the chunks' partials
+  const float* ws_ml;
+  float* out;
+  int64_t weights_stride;
+  ChunkPlan plan;
+  int32_t page_stride, n_q_heads, max_seq_len;
+  float decay;
+};
+template <bool kMerge>
+__global__ __launch_bounds__(kMergeThreads) void pq_page_weights_kernel(const WeightsArgs a) {
   __shared__ float part[kWeightSlices][kWeightPages];
-  const int at = threadIdx.x % kWeightPages, slice = threadIdx.x / kWeightPages, seq = blockIdx.y, page = blockIdx.x * kWeightPages + at;
-  const int L = min(seq_lens[seq], max_seq_len), n_pages = L > 0 ? (L + kGroup - 1) / kGroup : 0;
-  if (static_cast<int>(blockIdx.x) * kWeightPages >= n_pages) return;
+  if (kMerge && static_cast<int>(blockIdx.x) < a.n_q_heads) {
+    merge_chunks<false>(a.ws_acc, a.ws_ml, a.seq_lens, a.out, a.n_q_heads, a.max_seq_len, a.plan.pages_per_chunk, a.plan.n_chunks, a.plan.n_big,
+                        a.plan.pages_small, 0, 0);
+    return;
+  }
+  const int at = threadIdx.x % kWeightPages, slice = threadIdx.x / kWeightPages, seq = blockIdx.y;
+  const int first = (static_cast<int>(blockIdx.x) - (kMerge ? a.n_q_heads : 0)) * kWeightPages, page = first + at;
+  const int L = min(a.seq_lens[seq], a.max_seq_len), n_pages = L > 0 ? (L + kGroup - 1) / kGroup : 0;
+  if (first >= n_pages) return;
+  const int chunks = kMerge ? chunks_of_pages(n_pages, a.plan.pages_per_chunk, a.plan.n_big, a.plan.pages_small) : 0;
   float w = 0.f;
-  if (page < n_pages) {
-#pragma unroll 8
-    for (int h = slice; h < n_q_heads; h += kWeightSlices) {
-      const int64_t row = static_cast<int64_t>(seq) * n_q_heads + h;
-      const float2 all = totals[row], one = page_ml[row * page_stride + page];
-      if (one.y > 0.f) w += one.y * __builtin_amdgcn_exp2f(one.x - all.x) / all.y;
+#pragma unroll kMerge ? 1 : 4
+  for (int h = slice; h < a.n_q_heads; h += kWeightSlices) {
+    const int64_t row = static_cast<int64_t>(seq) * a.n_q_heads + h;
+    const float2 one = page < n_pages ? a.page_ml[row * a.page_stride + page] : make_float2(0.f, 0.f);
+    float2 all;
+    if constexpr (kMerge) {
+      const float2* const ml = reinterpret_cast<const float2*>(a.ws_ml) + row * a.plan.n_chunks;
+      all = make_float2(kNegInf, 0.f);
+      for (int c = at; c < chunks; c += kWeightPages) {
+        const float2 of = ml[c];
+        const float top = fmaxf(all.x, of.x);
+        if (top > kNegInf) all.y = all.y * __builtin_amdgcn_exp2f(all.x - top) + of.y * __builtin_amdgcn_exp2f(of.x - top);
+        all.x = top;
+      }
+      float top = all.x;
+      top = fmaxf(top, dpp_of<0x128>(top));
+      top = fmaxf(top, dpp_of<0x124>(top));
+      top = fmaxf(top, dpp_of<0x122>(top));
+      top = fmaxf(top, dpp_of<0x121>(top));
+      float sum = top > kNegInf ? all.y * __builtin_amdgcn_exp2f(all.x - top) : 0.f;
+      sum += dpp_of<0x128>(sum);
+      sum += dpp_of<0x124>(sum);
+      sum += dpp_of<0x122>(sum);
+      sum += dpp_of<0x121>(sum);
+      all = make_float2(top, sum);
+    } else {
+      all = a.totals[row];
     }
+    if (one.y > 0.f) w += one.y * __builtin_amdgcn_exp2f(one.x - all.x) / all.y;
   }
   part[slice][at] = w;
   __syncthreads();
   if (slice != 0 || page >= n_pages) return;
-  w = (part[0][at] + part[1][at]) + (part[2][at] + part[3][at]);
-  const int64_t i = seq * weights_stride + page;
-  if (before && decay != 0.f) w += decay * before[i];
-  weights[i] = w;
+  w = 0.f;
+#pragma unroll
+  for (int i = 0; i < kWeightSlices; ++i) w += part[i][at];
+  const int64_t i = seq * a.weights_stride + page;
+  if (a.before && a.decay != 0.f) w += a.decay * a.before[i];
+  a.weights[i] = w;
 }
 
 struct WeightsWorkspace {
@@ -676,15 +769,25 @@ extern "C" int pq_decode_attention_weights(const pq_layout* layout, const void* 
     else launch_weights_v2(layout, a, grid, stream);
     e = hipGetLastError();
   }
-  if (e == hipSuccess && !merged) {
-    hipLaunchKernelGGL((pq_decode_merge_kernel<false, true>), dim3(n_q_heads, n_seqs), dim3(kMergeThreads), 0, stream, ws.decode.acc, ws.decode.ml, seq_lens,
-                       out, n_q_heads, max_seq_len, plan.pages_per_chunk, plan.n_chunks, plan.n_big, plan.pages_small, 0, 0, ws.totals);
-    e = hipGetLastError();
-  }
   if (e == hipSuccess) {
-    hipLaunchKernelGGL(pq_page_weights_kernel, dim3(static_cast<uint32_t>((max_pages + kWeightPages - 1) / kWeightPages), n_seqs),
-                       dim3(kWeightPages * kWeightSlices), 0, stream, ws.page_ml, ws.totals, seq_lens, weights_before, weights, weights_stride, a.page_stride,
-                       n_q_heads, max_seq_len, decay);
+    WeightsArgs w;
+    w.page_ml = ws.page_ml;
+    w.totals = ws.totals;
+    w.seq_lens = seq_lens;
+    w.before = weights_before;
+    w.weights = weights;
+    w.ws_acc = ws.decode.acc;
+    w.ws_ml = ws.decode.ml;
+    w.out = out;
+    w.weights_stride = weights_stride;
+    w.plan = plan;
+    w.page_stride = a.page_stride;
+    w.n_q_heads = n_q_heads;
+    w.max_seq_len = max_seq_len;
+    w.decay = decay;
+    const uint32_t tiles = static_cast<uint32_t>((max_pages + kWeightPages - 1) / kWeightPages);
+    if (merged) hipLaunchKernelGGL(pq_page_weights_kernel<false>, dim3(tiles, n_seqs), dim3(kMergeThreads), 0, stream, w);
+    else hipLaunchKernelGGL(pq_page_weights_kernel<true>, dim3(n_q_heads + tiles, n_seqs), dim3(kMergeThreads), 0, stream, w);
     e = hipGetLastError();
   }
   return e == hipSuccess ? PQ_OK : record_hip_error(e);

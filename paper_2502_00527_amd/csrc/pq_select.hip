@@ -362,7 +362,7 @@ extern "C" int pq_select_pages(const pq_layout* layout, const void* q, pq_dtype 
 extern "C" size_t pq_sparse_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_t n_q_heads, int32_t max_seq_len, int32_t n_selected) {
   if (check_selection(layout, n_seqs, n_q_heads, max_seq_len, n_selected, 0, 1) != PQ_OK) return 0;
   const pq_layout one = one_head(layout);
-  const size_t attention = pq_decode_workspace_bytes(&one, n_seqs * layout->n_kv_heads, n_q_heads / layout->n_kv_heads, chosen_tokens(max_seq_len, n_selected));
+  const size_t attention = alike_workspace_bytes(&one, n_seqs * layout->n_kv_heads, n_q_heads / layout->n_kv_heads, chosen_tokens(max_seq_len, n_selected));
   return attention == 0 ? 0 : select_bytes(layout, n_seqs, max_seq_len) + attention;
 }
 
@@ -385,15 +385,14 @@ extern "C" int pq_sparse_attention(const pq_layout* layout, const void* q, pq_dt
   st = check_attention(&one, q, q_dtype, rows, heads, codes_pool, params_pool, v_pool, v_bits, v_params_pool, row_pages, selected, n_selected, selected_lens,
                        tokens, sm_scale, residual_keys);
   if (st != PQ_OK) return st;
-  const size_t before = select_bytes(layout, n_seqs, max_seq_len);
-  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < before + pq_decode_workspace_bytes(&one, rows, heads, tokens))
-    return PQ_ERR_WORKSPACE;
+  const size_t before = select_bytes(layout, n_seqs, max_seq_len), attention = alike_workspace_bytes(&one, rows, heads, tokens);
+  if (attention == 0) return PQ_ERR_UNSUPPORTED;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < before + attention) return PQ_ERR_WORKSPACE;
   if (!given) {
     st = launch_selection(layout, q, q_dtype, n_seqs, n_q_heads, bounds, bound_scales, n_pool_pages, block_table, max_pages_per_seq, seq_lens, max_seq_len,
                           n_selected, n_first, n_last, selected, selected_lens, workspace, static_cast<hipStream_t>(hip_stream));
     if (st != PQ_OK) return st;
   }
-  return pq_decode_attention(&one, q, q_dtype, rows, heads, codes_pool, params_pool, v_pool, v_bits, v_params_pool, row_pages, selected, n_selected,
-                             selected_lens, tokens, sm_scale, out, nullptr, 0, residual_keys, static_cast<uint8_t*>(workspace) + before,
-                             workspace_bytes - before, hip_stream);
+  return attend_alike(&one, q, q_dtype, rows, heads, codes_pool, params_pool, v_pool, v_bits, v_params_pool, row_pages, selected, n_selected, selected_lens,
+                      tokens, sm_scale, out, residual_keys, static_cast<uint8_t*>(workspace) + before, static_cast<hipStream_t>(hip_stream));
 }

@@ -334,7 +334,9 @@ def test_sparse_of_many_sequences():
 
 
 def test_all_pages_chosen_is_decode_attention():
-    """n_selected as large as the sequences: the bits of decode attention over the same pages, each head a sequence."""
+    """n_selected as large as the sequences: decode attention over the same pages, each head a sequence, but for the order in which the chunks'
+    partials are added.  They are 12 at most, with exact weights: each order's sum and denominator are off by 12 * 2^-24 of the terms' sizes, whose sum is at most the
+    denominator times the largest value, and the quotient's two roundings add 2^-23 of it each time."""
     c = Cache([1500, 700, 0, 129], 2)
     q = _queries(4, 8, 5)
     out, selected, lens = _sparse(c, q, _bound(c), 12)
@@ -343,7 +345,10 @@ def test_all_pages_chosen_is_decode_attention():
     want = torch.empty_like(out)
     c.pq.pq_decode_attention(one, q.view(8, 4, D), c.codes, c.params, c.v_pool, selected.view(8, 12), lens.view(8), c.max_seq_len, float(c.sm_scale),
                              want.view(8, 4, D), torch.empty(size, dtype=torch.uint8, device=DEV), None, c.residual)
-    assert torch.equal(out, want)
+    largest = max(float(v.abs().max()) for v in c.v64 if len(v))
+    assert float((out - want).abs().max()) <= 2 * (2 * 12 * 2.0 ** -24 + 2 * 2.0 ** -23) * largest
+    short = lens.view(8) <= 512                              # one chunk: the same bits
+    assert bool(short.any()) and torch.equal(out.view(8, 4, D)[short], want.view(8, 4, D)[short])
 
 
 def test_a_choice_that_is_given():
