@@ -8,13 +8,14 @@
 // A bit is set by an OR in LDS (lane = pair: its words lie in its own bank).  An instruction brings address and data of 64 lanes to LDS in
 // about 8 cycles, whatever the SIMD, a byte's reading in 4: with the symbols read from LDS one by one that path was busy for 83 % of 50 us
 // (8 x 20K .. 32K tokens x 8 heads).  So a wavefront loads a token's unit of 16 symbols a lane and transposes bytes between the 16 lanes of a
-// block of pairs in registers: 20 instructions for 16 symbols.
+// block of pairs in registers: 20 instructions for 16 symbols.  What bounds it then is vector issue.
 //
 // One work-group one or four KV heads of a page, the next head's codes on their way while one is worked on; wavefront = 32 tokens.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
 
+#include "pq_decode_kernels.hpp"
 #include "pq_internal.hpp"
 #include "pq_rank.hpp"
 
@@ -93,7 +94,7 @@ __device__ __forceinline__ void transpose_bytes(uint32_t (&d)[4], uint32_t selec
 }
 // A unit as it lies in memory, and as one symbol a byte (6-bit symbols: with two bits of the next one above them).
 template <int W>
-struct Unit {
+struct TokenUnit {
   uint32_t w[W / 2];
   __device__ __forceinline__ void load(const uint8_t* from) {
     if constexpr (W == 8) {
@@ -118,6 +119,17 @@ struct Unit {
     }
   }
 };
+
+// 1 << (byte `kByte` of x, its low five bits)
+template <int kByte>
+__device__ __forceinline__ uint32_t bit_of_byte(uint32_t x, uint32_t one) {
+  if constexpr (kByte == 0) return one << (x & 31);
+  uint32_t r;
+  if constexpr (kByte == 1) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1 src1_sel:DWORD" : "=v"(r) : "v"(x), "v"(one));
+  if constexpr (kByte == 2) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2 src1_sel:DWORD" : "=v"(r) : "v"(x), "v"(one));
+  if constexpr (kByte == 3) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3 src1_sel:DWORD" : "=v"(r) : "v"(x), "v"(one));
+  return r;
+}
 
 // cos and sin of |theta| < 4, good to a few units of 2^-53: Cody and Waite's reduction by quarter turns with pi / 2 in two parts, then the Taylor
 // series on [-pi / 4, pi / 4], whose first omitted terms are below 2^-54.
@@ -152,8 +164,13 @@ template <int RB, int TB, bool kGroupedAngles>
 __global__ __launch_bounds__(kBoundThreads, kGroupedAngles ? 5 : 8) void pq_bound_pages_kernel(const BoundArgs a, const BinTable bins) {
   constexpr int W = RB + TB, UB = 2 * W;
   constexpr int kWords = (1 << W) / 32, kOfWord = 32 >> RB;                       // of a pair's bits; angle codes of a word
-  __shared__ __attribute__((aligned(16))) uint32_t seen[kWords][kPairs];
-  __shared__ __attribute__((aligned(16))) float part[kBoundThreads / 64][kPairs][4];
+  static_assert(kPairs * 4 == 256, "a word's number is the second byte of an address, the lane its first");
+  __shared__ struct {
+    __attribute__((aligned(16))) uint32_t seen[kWords][kPairs];
+    __attribute__((aligned(16))) float part[kBoundThreads / 64][kPairs][4];
+  } sh;
+  auto& seen = sh.seen;
+  auto& part = sh.part;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int per_page = (a.n_kv_heads + a.heads_of_group - 1) / a.heads_of_group;
   const int nth = blockIdx.x / per_page, head0 = blockIdx.x % per_page * a.heads_of_group, seq = blockIdx.y;
@@ -167,7 +184,10 @@ __global__ __launch_bounds__(kBoundThreads, kGroupedAngles ? 5 : 8) void pq_boun
   // bytes {0, 1} of the own word and of the other lane's in the lane below, {2, 3} in the one above; then the even ones and the odd ones
   const uint32_t select2 = lane & 2 ? 0x03020706u : 0x05040100u, select1 = lane & 1 ? 0x03070105u : 0x06020400u;
 
-  Unit<W> raw[2];
+  const uint32_t lane4 = lane * 4, seen_at = lds_addr(&seen[0][0]);
+  uint32_t one = 1;
+  asm("" : "+v"(one));
+  TokenUnit<W> raw[2];
   uint32_t radius_par = 0, angle_par = 0;
   auto load = [&](int64_t ph) {
     const uint8_t* const from = a.codes + ph * (kBlocks * kGroup * UB) + (block * kGroup + wave * 32 + k) * UB;
@@ -191,9 +211,15 @@ __global__ __launch_bounds__(kBoundThreads, kGroupedAngles ? 5 : 8) void pq_boun
     for (int u = 0; u < 2; ++u) {
       transpose_bytes(d[u], select2, select1);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const uint32_t symbol = d[u][i / 4] >> (8 * (i % 4));                     // (bits above the symbol's are another's)
-        __hip_atomic_fetch_or(&seen[(symbol >> 5) & (kWords - 1)][lane], 1u << (symbol & 31), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t four = d[u][i], words = (four >> 5) & (0x01010101u * (kWords - 1));       // (bits above a symbol's are another's)
+        auto set = [&](uint32_t at, uint32_t bit) {
+          __hip_atomic_fetch_or((PQ_LDS uint32_t*)static_cast<uintptr_t>(seen_at + at), bit, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        };
+        set(__builtin_amdgcn_perm(words, lane4, 0x0c0c0400u), bit_of_byte<0>(four, one));
+        set(__builtin_amdgcn_perm(words, lane4, 0x0c0c0500u), bit_of_byte<1>(four, one));
+        set(__builtin_amdgcn_perm(words, lane4, 0x0c0c0600u), bit_of_byte<2>(four, one));
+        set(__builtin_amdgcn_perm(words, lane4, 0x0c0c0700u), bit_of_byte<3>(four, one));
       }
     }
     lds_barrier();
@@ -211,7 +237,7 @@ __global__ __launch_bounds__(kBoundThreads, kGroupedAngles ? 5 : 8) void pq_boun
         sn = bins.sn[state];
       }
       // (c + 1/2) s is exact, so that one rounding is what its sum with z has.  A state that nobody has is no number, which minima and maxima pass over
-      float near = fmaf(__builtin_ctz(radii) + 0.5f, rs, rz), far = fmaf(31 - __builtin_clz(radii) + 0.5f, rs, rz);
+      float near = fmaf(__builtin_ctz(radii) + 0.5f, rs, rz), far = fmaf(31.5f - __builtin_clz(radii), rs, rz);
       near = radii == 0 ? NAN : near;
       far = radii == 0 ? NAN : far;
       low_x = min3(low_x, near * cs, far * cs);
