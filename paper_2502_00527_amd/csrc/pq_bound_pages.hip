@@ -171,7 +171,7 @@ __global__ __launch_bounds__(kBoundThreads, kGroupedAngles ? 5 : 8) void pq_boun
   } sh;
   auto& seen = sh.seen;
   auto& part = sh.part;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int per_page = (a.n_kv_heads + a.heads_of_group - 1) / a.heads_of_group;
   const int nth = blockIdx.x / per_page, head0 = blockIdx.x % per_page * a.heads_of_group, seq = blockIdx.y;
   const int first = a.lens_before ? max(0, a.lens_before[seq]) / kGroup : 0, last = max(0, a.lens_after[seq]) / kGroup;
@@ -228,7 +228,7 @@ __global__ __launch_bounds__(kBoundThreads, kGroupedAngles ? 5 : 8) void pq_boun
 #pragma unroll kGroupedAngles ? 1 : (1 << TB) / 4
     for (int i = 0; i < (1 << TB) / 4; ++i) {
       const int state = 4 * i + wave;                        // angle code
-      const uint32_t radii = (seen[state / kOfWord][lane] >> ((state % kOfWord) << RB)) & (RB == 5 ? 0xffffffffu : (1u << (1 << RB)) - 1);
+      const uint32_t radii = (seen[state / kOfWord][lane] >> ((state % kOfWord) << RB)) & static_cast<uint32_t>((uint64_t{1} << (1 << RB)) - 1);
       float cs, sn;
       if constexpr (kGroupedAngles) {
         cos_sin((state + 0.5) * static_cast<double>(ts) + static_cast<double>(tz), cs, sn);

@@ -47,7 +47,7 @@ __global__ __launch_bounds__(kRankThreads) void pq_evict_kernel(const EvictArgs 
   __shared__ RankShared rank;
   __shared__ uint32_t keys[kMostKeys];
   __shared__ uint32_t sums[kRankWaves];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, seq = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), seq = blockIdx.x;
   const int64_t table_row = static_cast<int64_t>(seq) * a.max_pages_per_seq, weight_row = seq * a.weights_stride;
   // a first round of the rows, which exist whatever the sequence's length, is asked for before the lengths
   int32_t id[kKeysPerThread];

@@ -154,7 +154,7 @@ __global__ __launch_bounds__(kRankThreads) void pq_select_kernel(const SelectArg
   __shared__ __attribute__((aligned(16))) QueryOperand o;
   __shared__ __attribute__((aligned(16))) uint32_t in_lds[kMostKeys];
   __shared__ int stage;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, kvh = blockIdx.x, seq = blockIdx.y, part = blockIdx.z;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kvh = blockIdx.x, seq = blockIdx.y, part = blockIdx.z;
   const int64_t unit = static_cast<int64_t>(seq) * a.n_kv_heads + kvh;
   const int32_t* const row = a.block_table + static_cast<int64_t>(seq) * a.max_pages_per_seq;
   int32_t* const out = a.selected + unit * a.n_selected;
