@@ -14,7 +14,8 @@
 namespace pq {
 namespace {
 
-constexpr int kMostKeys = 4096;                              // pages whose keys stay in LDS
+constexpr int kKeysPerThread = 4;
+constexpr int kRankRound = kRankThreads * kKeysPerThread;    // pages whose weights stay in registers; of others they are read again
 
 struct EvictArgs {
   const int32_t* block_table;
@@ -45,7 +46,6 @@ __device__ __forceinline__ Kept kept_of(const EvictArgs& a, int seq) {
 
 __global__ __launch_bounds__(kRankThreads) void pq_evict_kernel(const EvictArgs a) {
   __shared__ RankShared rank;
-  __shared__ uint32_t keys[kMostKeys];
   __shared__ uint32_t sums[kRankWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), seq = blockIdx.x;
   const int64_t table_row = static_cast<int64_t>(seq) * a.max_pages_per_seq, weight_row = seq * a.weights_stride;
@@ -69,25 +69,18 @@ __global__ __launch_bounds__(kRankThreads) void pq_evict_kernel(const EvictArgs 
   const int begin = a.n_first, end = k.pages - k.last;
   // the smallest weight has the largest key; a NaN counts as the largest weight
   auto key_of_weight = [](float w) { return ~(w == w ? key_of(w) : 0xffffffffu); };
-  const bool in_lds = k.pages <= kMostKeys;
-  uint32_t low = 0xffffffffu, high = 0;
-  if (k.gone > 0) {
-    for (int base = 0; base < k.pages; base += kRankRound) {
-      const int p0 = base + tid * kKeysPerThread;
+  uint32_t first_key[kKeysPerThread];
 #pragma unroll
-      for (int j = 0; j < kKeysPerThread; ++j) {
-        if (p0 + j >= k.pages) continue;
-        const uint32_t v = key_of_weight(base == 0 ? weight[j] : a.weights[weight_row + p0 + j]);
-        if (in_lds) keys[p0 + j] = v;
-        if (p0 + j >= begin && p0 + j < end) {
-          low = min(low, v);
-          high = max(high, v);
-        }
-      }
+  for (int j = 0; j < kKeysPerThread; ++j) first_key[j] = key_of_weight(weight[j]);
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int j = 0; j < kKeysPerThread; ++j) {
+      const int p = tid * kKeysPerThread + j;
+      if (p >= begin && p < end) f(first_key[j]);
     }
-  }
-  auto key = [&](int p) { return in_lds ? keys[p] : key_of_weight(a.weights[weight_row + p]); };
-  const Threshold t = find_threshold(rank, begin, end, static_cast<uint32_t>(k.gone), low, high, key, tid);
+    for (int p = max(begin, kRankRound) + tid; p < end; p += kRankThreads) f(key_of_weight(a.weights[weight_row + p]));
+  };
+  const Threshold t = find_threshold(rank, end - begin, static_cast<uint32_t>(k.gone), each, tid);
   before = (sums[0] + sums[1]) + (sums[2] + sums[3]);
   if (seq >= a.n_seqs - 1 && tid == 0) a.counts[0] = static_cast<int32_t>(before + k.gone);
   if (seq >= a.n_seqs) return;
@@ -107,7 +100,7 @@ __global__ __launch_bounds__(kRankThreads) void pq_evict_kernel(const EvictArgs 
     // everybody has read before anybody writes, to where others have read before: what was asked for has come, and all wait for one another in
     // place_keys()
     stores_done();
-    place_keys(rank, places, t, in, v, tid, chosen, at);
+    place_keys<kKeysPerThread>(rank, places, t, in, v, tid, chosen, at);
 #pragma unroll
     for (int j = 0; j < kKeysPerThread; ++j) {
       const int p = p0 + j;

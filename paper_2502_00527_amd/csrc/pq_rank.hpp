@@ -17,8 +17,6 @@ namespace {
 constexpr int kRankThreads = 256;
 constexpr int kRankWaves = kRankThreads / 64;
 constexpr int kBins = 1024;
-constexpr int kKeysPerThread = 4;                            // of a round of place_keys()
-constexpr int kRankRound = kRankThreads * kKeysPerThread;
 
 // A float as a key that grows with it; -0 is 0.
 __device__ __forceinline__ uint32_t key_of(float x) {
@@ -79,12 +77,16 @@ struct Threshold {
   uint32_t key, ties;
 };
 
-// key(i), i in [begin, end), is read several times; 0 <= k <= end - begin.  low, high: the smallest and the largest of some of the keys, those of all
-// threads together being all (0xffffffff, 0: of none).  All threads of the work-group call it and get the result; what they have stored is there for
-// everybody after the wait that it begins with.
-template <typename Key>
-__device__ __forceinline__ Threshold find_threshold(RankShared& sh, int begin, int end, uint32_t k, uint32_t low, uint32_t high, Key key, int tid) {
-  const int lane = tid & 63, wave = tid >> 6;
+// each(f): f(key) for this thread's share of the `count` keys; called several times.  0 <= k <= count.  All threads of the work-group call it and get the
+// result; what they have stored in LDS is there for everybody after the wait that it begins with.
+template <typename Each>
+__device__ __forceinline__ Threshold find_threshold(RankShared& sh, int count, uint32_t k, Each each, int tid) {
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  uint32_t low = 0xffffffffu, high = 0;
+  each([&](uint32_t v) {
+    low = min(low, v);
+    high = max(high, v);
+  });
   low = wave_min(low);
   high = wave_max(high);
   if (lane == 0) {
@@ -95,16 +97,16 @@ __device__ __forceinline__ Threshold find_threshold(RankShared& sh, int begin, i
   if (tid == 0) sh.listed = 0;
   lds_barrier();
   if (k == 0) return {0xffffffffu, 0};
-  if (k >= static_cast<uint32_t>(end - begin)) return {0, 0xffffffffu};
-  low = min(min(sh.low[0], sh.low[1]), min(sh.low[2], sh.low[3]));
-  high = max(max(sh.high[0], sh.high[1]), max(sh.high[2], sh.high[3]));
-  uint32_t base = low, limit = high - low;                   // keys base .. base + limit are in question
+  if (k >= static_cast<uint32_t>(count)) return {0, 0xffffffffu};
+  const uint4 lows = *reinterpret_cast<const uint4*>(sh.low), highs = *reinterpret_cast<const uint4*>(sh.high);
+  uint32_t base = __builtin_amdgcn_readfirstlane(min(min(lows.x, lows.y), min(lows.z, lows.w)));
+  uint32_t limit = __builtin_amdgcn_readfirstlane(max(max(highs.x, highs.y), max(highs.z, highs.w))) - base;   // keys base .. base + limit are in question
   while (limit > 0) {
     const int shift = max(0, 22 - __builtin_clz(limit));
-    for (int i = begin + tid; i < end; i += kRankThreads) {
-      const uint32_t v = key(i), off = v - base;
+    each([&](uint32_t v) {
+      const uint32_t off = v - base;
       if (v >= base && off <= limit) atomicAdd(&sh.hist[off >> shift], 1u);
-    }
+    });
     lds_barrier();
     // every wavefront for itself: the bin where the count from above crosses k
     constexpr int kOwn = kBins / 64;
@@ -120,27 +122,28 @@ __device__ __forceinline__ Threshold find_threshold(RankShared& sh, int begin, i
     }
     const uint32_t from = sum_from(sum, lane);
     const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(from - sum < k && from >= k));
-    uint32_t above = from - sum, bin = 0, taken = 0, inside = 0;
+    // in that lane: how many of its bins are wholly above, which the last bin with k or more from it on tells
+    uint32_t above = from - sum, bin = 0, taken = above, inside = 0;
 #pragma unroll
     for (int j = kOwn - 1; j >= 0; --j) {
-      if (above < k && above + h[j] >= k) {
-        bin = lane * kOwn + j;
-        taken = above;
-        inside = h[j];
-      }
+      const bool crossed = above + h[j] >= k;
+      bin = max(bin, crossed ? j : 0u);
+      inside = crossed ? inside : h[j];
       above += h[j];
+      taken = crossed ? taken : above;
     }
-    inside = __builtin_amdgcn_readlane(inside, at);
+    bin = __builtin_amdgcn_readlane(bin, at);
     k -= __builtin_amdgcn_readlane(taken, at);
-    base += __builtin_amdgcn_readlane(bin, at) << shift;
+    inside = sh.hist[at * kOwn + bin];
+    inside = __builtin_amdgcn_readfirstlane(inside);
+    base += (at * kOwn + bin) << shift;
     if (inside == k) return {base, 0xffffffffu};             // all of the bin: those above its first key, and that one
     limit = (1u << shift) - 1;
     if (limit == 0) break;
     if (inside <= 64) {                                      // few: each against each, in every wavefront
-      for (int i = begin + tid; i < end; i += kRankThreads) {
-        const uint32_t v = key(i);
+      each([&](uint32_t v) {
         if (v >= base && v - base <= limit) sh.list[atomicAdd(&sh.listed, 1u)] = v;
-      }
+      });
       lds_barrier();
       const uint32_t mine = static_cast<uint32_t>(lane) < inside ? sh.list[lane] : 0;
       uint32_t larger = 0, equal = 0;
@@ -159,21 +162,22 @@ __device__ __forceinline__ Threshold find_threshold(RankShared& sh, int begin, i
   return {base, k};
 }
 
-// Rounds of kRankRound keys in order, thread t's being 4 t .. 4 t + 3 of a round: which are chosen, and how many keys before each are.
+// Rounds of kRankThreads * kKeys keys in order, thread t's being kKeys t .. of a round: which are chosen, and how many chosen ones are before each.
 struct Places {
   uint32_t sure = 0, ties = 0;
   int turn = 0;
 };
-__device__ __forceinline__ void place_keys(RankShared& sh, Places& p, const Threshold& t, const bool (&in)[kKeysPerThread], const uint32_t (&key)[kKeysPerThread],
-                                           int tid, bool (&chosen)[kKeysPerThread], uint32_t (&at)[kKeysPerThread]) {
-  const int lane = tid & 63, wave = tid >> 6;
-  bool above[kKeysPerThread], tie[kKeysPerThread];
+template <int kKeys>
+__device__ __forceinline__ void place_keys(RankShared& sh, Places& p, const Threshold& t, const bool (&in)[kKeys], const uint32_t (&key)[kKeys], int tid,
+                                           bool (&chosen)[kKeys], uint32_t (&at)[kKeys]) {
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  bool above[kKeys], tie[kKeys];
   uint32_t sure = 0, ties = 0, all_sure = 0, all_ties = 0;   // before this thread's first key, and of the wavefront
   auto below = [](uint64_t mask, uint32_t add) {             // of the lanes below this one
     return __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(mask >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(mask), add));
   };
 #pragma unroll
-  for (int j = 0; j < kKeysPerThread; ++j) {
+  for (int j = 0; j < kKeys; ++j) {
     above[j] = in[j] && key[j] > t.key;
     tie[j] = in[j] && key[j] == t.key;
     const uint64_t a = __builtin_amdgcn_ballot_w64(above[j]), b = __builtin_amdgcn_ballot_w64(tie[j]);
@@ -196,7 +200,7 @@ __device__ __forceinline__ void place_keys(RankShared& sh, Places& p, const Thre
   }
   p.turn ^= 1;
 #pragma unroll
-  for (int j = 0; j < kKeysPerThread; ++j) {
+  for (int j = 0; j < kKeys; ++j) {
     chosen[j] = above[j] || (tie[j] && ties < t.ties);
     at[j] = sure + min(ties, t.ties);
     sure += above[j];

@@ -1,9 +1,12 @@
 // Choice of pages by a cheap score of the queries against the pages' bounds (pq_select_pages), and attention over the chosen
 // ones (pq_sparse_attention).
 //
-// The score of a page is, block of 32 channels by block, q8 . c + |q8| . w in whole numbers -- one matrix instruction of 64 products
-// per 16 pages and 16 query heads, {c, w} of a block being 64 bytes in the order the instruction reads them -- times the block's
+// The score of a page is, block of 32 channels by block, q8 . c + |q8| . w in whole numbers -- {c, w} of a block being 64 bytes, the
+// depth of one matrix instruction, in the order it reads them -- times the block's
 // scales in fp32; whole numbers below 2^24 and fp32 operations that are rounded one by one make it the same for whoever computes it.
+// The instruction takes 16 pages and 16 rows: four heads of block 0, of block 1, ..., with zeros in the rows of other blocks, so that one accumulator has
+// the four blocks' sums of four heads, a block in each row of lanes.  Adding blocks up is then two swaps of rows, which serve four tiles of 16
+// pages at once and leave each lane the score of one page: 80 instructions for 64 pages and four heads, where an accumulator a block took 300.
 //
 // Few (sequence, KV head) units with many pages share a unit's pages among work-groups: one compute unit has about 60 lines of 128 bytes
 // under way, and 1024 pages of 272 bytes took one 9.5 us.  The keys go to the workspace past the caches, and whoever registers last at the unit's
@@ -50,68 +53,72 @@ struct SelectArgs {
 __device__ __forceinline__ int clamped(const SelectArgs& a, int seq) { return max(0, min(a.seq_lens[seq], a.max_seq_len)); }
 __device__ __forceinline__ int pages_up(int tokens) { return (tokens + kGroup - 1) / kGroup; }
 
-// The queries of a KV head as the matrix instruction's operand: lane (head l % 16, part l / 16) has 16 bytes a block, parts x, y, |x|, |y|
-// of the block's 16 pairs.  Heads past the last are that one again.
-struct QueryOperand {
-  i32x4 code[kBlocks][64];
-  float largest[kBlocks];
-};
-// What a lane of block b's operand is made of, as it lies in memory.
-struct QueryFetch {
-  uint4 w[4];
-  __device__ __forceinline__ QueryFetch(const SelectArgs& a, int64_t head0, int b, int lane) {
-    const int64_t at = (head0 + min(lane & 15, a.group - 1)) * kHeadDim + ((lane >> 4) & 1) * kPairs + b * 16;
-    if (a.q_is_f32) {
-      const uint4* const src = reinterpret_cast<const uint4*>(static_cast<const float*>(a.q) + at);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = src[i];
-    } else {
-      const uint4* const src = reinterpret_cast<const uint4*>(static_cast<const _Float16*>(a.q) + at);
-      w[0] = src[0];
-      w[1] = src[1];
-    }
-  }
-  __device__ __forceinline__ float value(bool f32, int i) const {
-    const uint32_t wide[4] = {w[i / 4].x, w[i / 4].y, w[i / 4].z, w[i / 4].w};
-    if (f32) return __builtin_bit_cast(float, wide[i % 4]);
-    const uint32_t two[4] = {w[i / 8].x, w[i / 8].y, w[i / 8].z, w[i / 8].w};
-    return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(two[i / 2 % 4] >> (16 * (i & 1)))));
-  }
-};
-__device__ __forceinline__ void store_operand(QueryOperand& o, const QueryFetch& f, bool f32, int b, int lane) {
-  float v[16];
-  if (f32) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = f.value(true, i);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = f.value(false, i);
-  }
-  float m = 0.f;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(v[i]));
-  m = __builtin_bit_cast(float, wave_max(__builtin_bit_cast(uint32_t, m)));                  // (not negative: in the order of its bits)
-  const float up = m >= kTiny ? 127.0f / m : 0.f;
-  i32x4 code;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    uint32_t word = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float r = rintf(v[4 * w + i] * up);
-      word |= (static_cast<uint32_t>(static_cast<int>(lane < 32 ? r : fabsf(r))) & 255u) << (8 * i);
-    }
-    code[w] = static_cast<int>(word);
-  }
-  o.code[b][lane] = code;
-  if (lane == 0) o.largest[b] = m;
-}
+// The queries of a KV head as operands.  Lane l has head 4 s + l % 4 of set s, block (l / 4) % 4, and of its 16 pairs part l / 16: x, y, |x| or |y|.
+// Heads past the last are that one again.
+template <int kSets>
+struct Query {
+  i32x4 code[kSets];
+  float largest;                                             // of block l / 16, any head
 
-// Pages first .. first + 15 of a sequence, page first + l % 16 in every lane: block-table entry, bounds, scales, and what comes of them.
+  u32x4 w[kSets][4];                                         // as they lie in memory
+  __device__ __forceinline__ void fetch(const SelectArgs& a, int64_t head0, int lane) {
+    const int per_row = a.q_is_f32 ? kHeadDim * 4 : kHeadDim * 2, per_part = per_row / 8;
+#pragma unroll
+    for (int s = 0; s < kSets; ++s) {
+      const int64_t head = head0 + min(4 * s + (lane & 3), a.group - 1);
+      const u32x4* const src = reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(a.q) + head * per_row + ((lane >> 4) & 1) * (per_row / 2) + ((lane >> 2) & 3) * per_part);
+      w[s][0] = src[0];
+      w[s][1] = src[1];
+      w[s][2] = src[a.q_is_f32 ? 2 : 0];                     // (fp16: not looked at)
+      w[s][3] = src[a.q_is_f32 ? 3 : 0];
+    }
+  }
+  template <bool kF32>
+  __device__ __forceinline__ float value(int s, int i) const {
+    if constexpr (kF32) return u2f(w[s][i / 4][i % 4]);
+    else return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(w[s][i / 8][i / 2 % 4] >> (16 * (i & 1)))));
+  }
+  template <bool kF32>
+  __device__ __forceinline__ void make(int lane) {
+    float m = 0.f;
+#pragma unroll
+    for (int s = 0; s < kSets; ++s)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(value<kF32>(s, i)));
+    uint32_t bits = __builtin_bit_cast(uint32_t, m);         // (not negative: in the order of its bits)
+    bits = max(bits, moved<0xb1>(bits));                     // over the block's heads (quad_perm) and parts
+    bits = max(bits, moved<0x4e>(bits));
+    bits = over_rows(bits, [](uint32_t x, uint32_t y) { return max(x, y); });
+    m = __builtin_bit_cast(float, bits);
+    const uint32_t m0 = __builtin_amdgcn_readlane(bits, 0), m1 = __builtin_amdgcn_readlane(bits, 4), m2 = __builtin_amdgcn_readlane(bits, 8),
+                   m3 = __builtin_amdgcn_readlane(bits, 12);
+    largest = u2f(lane & 32 ? (lane & 16 ? m3 : m2) : (lane & 16 ? m1 : m0));
+    const float up = m >= kTiny ? 127.0f / m : 0.f;
+    const uint32_t sign = lane < 32 ? 0xffffffffu : 0x7fffffffu;
+#pragma unroll
+    for (int s = 0; s < kSets; ++s)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t word = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float r = rintf(value<kF32>(s, 4 * i + j) * up);
+          word |= (static_cast<uint32_t>(static_cast<int>(__builtin_bit_cast(float, __builtin_bit_cast(uint32_t, r) & sign))) & 255u) << (8 * j);
+        }
+        code[s][i] = static_cast<int>(word);
+      }
+  }
+  __device__ __forceinline__ i32x4 operand(int s, int b, int lane) const {
+    const bool here = ((lane >> 2) & 3) == b;
+    return i32x4{here ? code[s].x : 0, here ? code[s].y : 0, here ? code[s].z : 0, here ? code[s].w : 0};
+  }
+};
+
+// Pages first .. first + 15 of a sequence: lane l has page l % 16's block-table entry, part l / 16 of its bounds' blocks, and the scale of block l / 16.
 struct Tile {
   int32_t id;
   i32x4 bound[kBlocks];
-  float4 scale;
+  float scale;
   __device__ __forceinline__ bool there(const SelectArgs& a) const { return id >= 0 && id < a.n_pool_pages; }
   // (p < a.max_pages is in the row whatever the sequence's length)
   __device__ __forceinline__ void load_id(const SelectArgs& a, const int32_t* row, int p) { id = p < a.max_pages ? row[p] : -1; }
@@ -120,39 +127,56 @@ struct Tile {
     const int8_t* const from = a.bounds + ph * kBoundBytes + (lane >> 4) * 16;
 #pragma unroll
     for (int i = 0; i < kBlocks; ++i) bound[i] = *reinterpret_cast<const i32x4*>(from + i * kBlockBytes);
-    scale = *reinterpret_cast<const float4*>(a.scales + ph * kBlocks);
-  }
-  __device__ __forceinline__ uint32_t key(const SelectArgs& a, const QueryOperand& o, int lane) const {
-    const float u[kBlocks] = {o.largest[0] * scale.x, o.largest[1] * scale.y, o.largest[2] * scale.z, o.largest[3] * scale.w};
-    i32x4 n[kBlocks];
-#pragma unroll
-    for (int i = 0; i < kBlocks; ++i) n[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(o.code[i][lane], bound[i], i32x4{0, 0, 0, 0}, 0, 0, 0);
-    float best = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {                            // heads 4 (l / 16) + i
-      float t[kBlocks];
-#pragma unroll
-      for (int j = 0; j < kBlocks; ++j) t[j] = static_cast<float>(n[j][i]) * u[j];
-      best = fmaxf(best, (t[0] + t[1]) + (t[2] + t[3]));
-    }
-    // (no other order of floats than fmaxf's: the largest key would not be the same where a score is no number)
-    best = __builtin_bit_cast(float, over_rows(__builtin_bit_cast(uint32_t, best), [](uint32_t x, uint32_t y) {
-      return __builtin_bit_cast(uint32_t, fmaxf(__builtin_bit_cast(float, x), __builtin_bit_cast(float, y)));
-    }));
-    return key_of(there(a) ? best : -INFINITY);
+    scale = a.scales[ph * kBlocks + (lane >> 4)];
   }
 };
 // Tiles of a wavefront whose loads are under way together: a block-table entry and then the bounds are two waits for memory, for all of them.
 constexpr int kTilesAtOnce = 4;
-constexpr int kRoundPages = kRankWaves * kTilePages;         // a tile each
-constexpr int kBatchPages = kTilesAtOnce * kRoundPages;
+constexpr int kBatchPages = kRankWaves * kTilesAtOnce * kTilePages;                // of a work-group
 
-// kTiles: of a wavefront at once; 4 but for parts of fewer.
-template <int kTiles>
+// The key of page 16 (l / 16) + l % 16 of the tiles in lane l (l / 16 modulo kTiles).
+template <int kTiles, int kSets>
+__device__ __forceinline__ uint32_t tile_keys(const Tile (&tile)[kTiles], const Query<kSets>& q, const SelectArgs& a, int lane) {
+  const int row = lane >> 4;
+  float best = -INFINITY;
+#pragma unroll
+  for (int s = 0; s < kSets; ++s) {
+    float t[kTiles][4];                                      // [tile][head 4 s + i], of block `row` and page l % 16
+    i32x4 n[kTiles];
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+      const i32x4 x = q.operand(s, b, lane);
+#pragma unroll
+      for (int j = 0; j < kTiles; ++j) n[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, tile[j].bound[b], b == 0 ? i32x4{0, 0, 0, 0} : n[j], 0, 0, 0);
+    }
+#pragma unroll
+    for (int j = 0; j < kTiles; ++j) {
+      const float u = q.largest * tile[j].scale;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) t[j][i] = static_cast<float>(n[j][i]) * u;
+    }
+    // blocks 0 + 1 and 2 + 3, then those: row r keeps tile r's
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float first = tsum16(t[0][i], t[1 % kTiles][i]), second = kTiles == 4 ? tsum16(t[2 % kTiles][i], t[3 % kTiles][i]) : first;
+      best = fmaxf(best, tsum32(first, second));
+    }
+  }
+  bool there = tile[0].there(a);
+  if constexpr (kTiles == 2) there = row & 1 ? tile[1].there(a) : there;
+  if constexpr (kTiles == 4) there = row < 2 ? (row == 0 ? there : tile[1].there(a)) : (row == 2 ? tile[2].there(a) : tile[3].there(a));
+  return key_of(there ? best : -INFINITY);
+}
+
+// kTiles: of a wavefront at once.  kSets: of four query heads.  kKeys: keys of a thread when the choice is made: 1, where a batch is all there is -- every
+// thread has scored one page -- or 4.
+template <int kTiles, int kSets, int kKeys>
 __global__ __launch_bounds__(kRankThreads) void pq_select_kernel(const SelectArgs a) {
+  constexpr int kPartPages = kRankWaves * kTiles * kTilePages, kRound = kRankThreads * kKeys;
+  static_assert(kKeys == 1 || kKeys == 4, "one page a thread, or a 128-bit read");
+  static_assert(kKeys != 1 || kTiles == kTilesAtOnce, "a page a thread");
   __shared__ RankShared rank;
-  __shared__ __attribute__((aligned(16))) QueryOperand o;
-  __shared__ __attribute__((aligned(16))) uint32_t in_lds[kMostKeys];
+  __shared__ __attribute__((aligned(16))) uint32_t in_lds[kKeys == 1 ? 4 : kMostKeys];
   __shared__ int stage;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kvh = blockIdx.x, seq = blockIdx.y, part = blockIdx.z;
   const int64_t unit = static_cast<int64_t>(seq) * a.n_kv_heads + kvh;
@@ -161,10 +185,11 @@ __global__ __launch_bounds__(kRankThreads) void pq_select_kernel(const SelectArg
   // the page's row in the pools taken head by head
   auto name = [&](int32_t page) { return page >= 0 && page < a.n_pool_pages ? page * a.n_kv_heads + kvh : -1; };
   Tile tile[kTiles];
-  const int part0 = part * a.part_pages, first = part0 + wave * kTilePages + (lane & 15);   // (tiles in turn: all wavefronts have some)
+  const int part0 = part * a.part_pages, first = part0 + wave * (kTiles * kTilePages);
 #pragma unroll
-  for (int j = 0; j < kTiles; ++j) tile[j].load_id(a, row, first + j * kRoundPages);
-  const QueryFetch f(a, unit * a.group, wave, lane);
+  for (int j = 0; j < kTiles; ++j) tile[j].load_id(a, row, first + j * kTilePages + (lane & 15));
+  Query<kSets> q;
+  q.fetch(a, unit * a.group, lane);
   const int len = clamped(a, seq), pages = pages_up(len);
   if (pages <= a.n_selected) {
     if (part != 0) return;
@@ -175,76 +200,78 @@ __global__ __launch_bounds__(kRankThreads) void pq_select_kernel(const SelectArg
   if (part0 >= pages) return;
   const int parts = (pages + a.part_pages - 1) / a.part_pages, part_end = min(pages, part0 + a.part_pages);
   const int begin = a.n_first, end = pages - a.n_last;       // pages there is a choice of
-  const bool shared = parts > 1, in_memory = shared && pages > kMostKeys;
+  const bool shared = kKeys != 1 && parts > 1, in_memory = shared && pages > kMostKeys;
   const __amdgpu_buffer_rsrc_t r_keys = make_rsrc(a.keys + (shared ? unit * a.max_pages : 0), shared ? static_cast<uint32_t>(pages) * 4u : 0u);
-  uint32_t low = 0xffffffffu, high = 0;
-  for (int done = 0; part0 + done < part_end; done += kTiles * kRoundPages) {
+  uint32_t own = 0;                                          // kKeys == 1: page tid's
+  for (int done = 0; part0 + done < part_end; done += kPartPages) {
     if (done > 0) {
 #pragma unroll
-      for (int j = 0; j < kTiles; ++j) tile[j].load_id(a, row, done + first + j * kRoundPages);
+      for (int j = 0; j < kTiles; ++j) tile[j].load_id(a, row, done + first + j * kTilePages + (lane & 15));
     }
 #pragma unroll
     for (int j = 0; j < kTiles; ++j) tile[j].load(a, kvh, lane);
     if (done == 0) {
-      store_operand(o, f, a.q_is_f32 != 0, wave, lane);
-      __syncthreads();
+      if (a.q_is_f32) q.template make<true>(lane);
+      else q.template make<false>(lane);
     }
-#pragma unroll
-    for (int j = 0; j < kTiles; ++j) {
-      const int p = done + first + j * kRoundPages;
-      const uint32_t k = tile[j].key(a, o, lane);
-      if (lane < kTilePages && p < part_end) {
-        if (shared) __builtin_amdgcn_raw_buffer_store_b32(k, r_keys, p * 4, 0, kAuxDevice);
-        else in_lds[p] = k;
-      }
-      if (p >= begin && p < end) {
-        low = min(low, k);
-        high = max(high, k);
-      }
+    const uint32_t k = tile_keys<kTiles, kSets>(tile, q, a, lane);
+    const int p = done + first + lane;
+    if constexpr (kKeys == 1) {
+      own = k;
+    } else if (lane < kTiles * kTilePages && p < part_end) {
+      if (shared) __builtin_amdgcn_raw_buffer_store_b32(k, r_keys, p * 4, 0, kAuxDevice);
+      else in_lds[p] = k;
     }
   }
   if (shared) {
     stores_done();
-    __syncthreads();
+    lds_barrier();
     if (tid == 0) stage = arrive(a.arrivals + unit, parts) ? 1 : 0;
-    __syncthreads();
+    lds_barrier();
     if (stage == 0) return;
-    low = 0xffffffffu;
-    high = 0;
-    for (int p = tid; p < pages; p += kRankThreads) {
-      const uint32_t k = __builtin_amdgcn_raw_buffer_load_b32(r_keys, p * 4, 0, kAuxDevice);
-      if (!in_memory) in_lds[p] = k;
-      if (p >= begin && p < end) {
-        low = min(low, k);
-        high = max(high, k);
-      }
-    }
     if (tid == 0) reset_arrivals(a.arrivals + unit);
+    if (!in_memory)
+      for (int p = tid; p < pages; p += kRankThreads) in_lds[p] = __builtin_amdgcn_raw_buffer_load_b32(r_keys, p * 4, 0, kAuxDevice);
   }
+  int32_t id[kKeys];
+#pragma unroll
+  for (int j = 0; j < kKeys; ++j) id[j] = tid * kKeys + j < pages ? row[tid * kKeys + j] : -1;
+  if constexpr (kKeys != 1) lds_barrier();
   auto key = [&](int p) { return in_memory ? __builtin_amdgcn_raw_buffer_load_b32(r_keys, p * 4, 0, kAuxDevice) : in_lds[p]; };
-  int32_t id[kKeysPerThread];
-#pragma unroll
-  for (int j = 0; j < kKeysPerThread; ++j) id[j] = tid * kKeysPerThread + j < pages ? row[tid * kKeysPerThread + j] : -1;
-  const Threshold t = find_threshold(rank, begin, end, static_cast<uint32_t>(a.n_selected - a.n_first - a.n_last), low, high, key, tid);
+  auto each = [&](auto f) {
+    if constexpr (kKeys == 1) {
+      if (tid >= begin && tid < end) f(own);
+    } else {
+      for (int p = begin + tid; p < end; p += kRankThreads) f(key(p));
+    }
+  };
+  const Threshold t = find_threshold(rank, end - begin, static_cast<uint32_t>(a.n_selected - a.n_first - a.n_last), each, tid);
   Places places;
-  for (int base = 0; base < pages; base += kRankRound) {
-    const int p0 = base + tid * kKeysPerThread;
-    bool in[kKeysPerThread], chosen[kKeysPerThread];
-    uint32_t k[kKeysPerThread], at[kKeysPerThread];
+  for (int base = 0; base < pages; base += kRound) {
+    const int p0 = base + tid * kKeys;
+    bool in[kKeys], chosen[kKeys];
+    uint32_t k[kKeys], at[kKeys];
 #pragma unroll
-    for (int j = 0; j < kKeysPerThread; ++j) {
+    for (int j = 0; j < kKeys; ++j) {
       in[j] = p0 + j >= begin && p0 + j < end;
-      k[j] = in[j] ? key(p0 + j) : 0;
+      k[j] = kKeys == 1 ? own : (in[j] ? key(p0 + j) : 0);
       if (base > 0) id[j] = p0 + j < pages ? row[p0 + j] : -1;
     }
-    place_keys(rank, places, t, in, k, tid, chosen, at);
+    place_keys<kKeys>(rank, places, t, in, k, tid, chosen, at);
 #pragma unroll
-    for (int j = 0; j < kKeysPerThread; ++j) {
+    for (int j = 0; j < kKeys; ++j) {
       const int p = p0 + j, to = chosen[j] ? a.n_first + static_cast<int>(at[j]) : (p < begin ? p : (p >= end ? a.n_selected - pages + p : -1));
       if (to >= 0 && p < pages) out[to] = name(id[j]);
     }
   }
   if (tid == 0) a.selected_lens[unit] = len - (pages - a.n_selected) * kGroup;
+}
+
+template <int kTiles, int kKeys>
+void launch_select(const SelectArgs& a, dim3 grid, hipStream_t st) {
+  if (a.group <= 4) hipLaunchKernelGGL((pq_select_kernel<kTiles, 1, kKeys>), grid, dim3(kRankThreads), 0, st, a);
+  else if (a.group <= 8) hipLaunchKernelGGL((pq_select_kernel<kTiles, 2, kKeys>), grid, dim3(kRankThreads), 0, st, a);
+  else hipLaunchKernelGGL((pq_select_kernel<kTiles, 4, kKeys>), grid, dim3(kRankThreads), 0, st, a);
 }
 
 int64_t most_pages(int32_t max_seq_len) { return (static_cast<int64_t>(max_seq_len) + kGroup - 1) / kGroup; }
@@ -254,8 +281,10 @@ int64_t most_pages(int32_t max_seq_len) { return (static_cast<int64_t>(max_seq_l
 int32_t pages_of_part(const pq_layout* l, int32_t n_seqs, int32_t max_seq_len) {
   const int64_t pages = most_pages(max_seq_len), units = static_cast<int64_t>(n_seqs) * l->n_kv_heads;
   if (pages <= kBatchPages || (units >= kComputeUnits && pages <= kMostKeys)) return static_cast<int32_t>(std::min<int64_t>(pages, kMostKeys));
-  for (int tiles = 1; tiles < kTilesAtOnce; tiles *= 2)
-    if (units * ((pages + tiles * kRoundPages - 1) / (tiles * kRoundPages)) <= kResidentGroups) return tiles * kRoundPages;
+  for (int tiles = 1; tiles < kTilesAtOnce; tiles *= 2) {
+    const int part = kRankWaves * tiles * kTilePages;
+    if (units * ((pages + part - 1) / part) <= kResidentGroups) return part;
+  }
   return kBatchPages;
 }
 bool shares_units(const pq_layout* l, int32_t n_seqs, int32_t max_seq_len) { return pages_of_part(l, n_seqs, max_seq_len) < most_pages(max_seq_len); }
@@ -318,9 +347,10 @@ int launch_selection(const pq_layout* l, const void* q, pq_dtype q_dtype, int32_
   a.q_is_f32 = q_dtype == PQ_F32 ? 1 : 0;
   a.part_pages = pages_of_part(l, n_seqs, max_seq_len);
   const dim3 grid(l->n_kv_heads, n_seqs, (a.max_pages + a.part_pages - 1) / a.part_pages);
-  if (a.part_pages <= kRoundPages) hipLaunchKernelGGL(pq_select_kernel<1>, grid, dim3(kRankThreads), 0, st, a);
-  else if (a.part_pages <= 2 * kRoundPages) hipLaunchKernelGGL(pq_select_kernel<2>, grid, dim3(kRankThreads), 0, st, a);
-  else hipLaunchKernelGGL(pq_select_kernel<kTilesAtOnce>, grid, dim3(kRankThreads), 0, st, a);
+  if (a.max_pages <= kBatchPages) launch_select<kTilesAtOnce, 1>(a, grid, st);
+  else if (a.part_pages == kBatchPages / 4) launch_select<1, 4>(a, grid, st);
+  else if (a.part_pages == kBatchPages / 2) launch_select<2, 4>(a, grid, st);
+  else launch_select<kTilesAtOnce, 4>(a, grid, st);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? PQ_OK : record_hip_error(e);
 }

@@ -213,6 +213,15 @@ def test_choice_of_long_sequences_and_ties(pages, distinct):
     _check_choice(c, _queries(3, 8, pages), _random_pools(50, 2, pages, distinct), min(pages - 1, 100), 1, 2)
 
 
+@pytest.mark.parametrize("group", [1, 6, 16])
+@pytest.mark.parametrize("seqs,heads,pages", [(1, 1, 300), (1, 4, 1500), (40, 2, 700), (3, 1, 5000), (70, 2, 500), (1, 32, 1030), (130, 2, 260)])
+def test_choice_of_every_way_to_share_units(seqs, heads, pages, group):
+    """Units of one work-group, and of several with one, two and four tiles a wavefront; each with one, two and four sets of heads."""
+    rng = np.random.default_rng(pages)
+    c = _Plain([pages * G] + [int(n) for n in rng.integers(1, pages * G, seqs - 1)], heads, 90)
+    _check_choice(c, _queries(seqs, heads * group, 3, torch.float32 if group == 6 else torch.float16), _random_pools(90, heads, 7), 40, 1, 2)
+
+
 @pytest.mark.parametrize("lens", [[5000 * G], [200, 130000]])
 def test_a_bound_above_the_lengths(lens):
     c = _Plain(lens, 1, 50)
