@@ -30,7 +30,7 @@ typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 constexpr int kBoundBytes = 4 * kPairs;                      // of a page and head
 constexpr int kBlockBytes = kBoundBytes / kBlocks;
 constexpr float kTiny = 0x1p-100f;
-constexpr int kMostKeys = 4096;                              // pages whose keys stay in LDS
+constexpr int kMostKeys = 8192;                              // pages whose keys stay in LDS
 constexpr int kTilePages = 16;                               // of a matrix instruction
 
 struct SelectArgs {
@@ -42,10 +42,11 @@ struct SelectArgs {
   int32_t* selected;
   int32_t* selected_lens;
   uint64_t* arrivals;                                        // one word a unit; of units shared among work-groups
-  uint32_t* keys;                                            // [unit][max_pages], of the same
+  uint32_t* keys;                                            // [unit][key_stride], of the same
   int32_t n_pool_pages;
   int32_t n_kv_heads, group, max_pages_per_seq, max_seq_len, max_pages;
   int32_t n_selected, n_first, n_last;
+  int32_t key_stride;                                        // a multiple of 4
   int32_t part_pages;                                        // pages of a work-group; max_pages at least: of all
   int32_t q_is_f32;
 };
@@ -173,6 +174,7 @@ __device__ __forceinline__ uint32_t tile_keys(const Tile (&tile)[kTiles], const 
 template <int kTiles, int kSets, int kKeys>
 __global__ __launch_bounds__(kRankThreads) void pq_select_kernel(const SelectArgs a) {
   constexpr int kPartPages = kRankWaves * kTiles * kTilePages, kRound = kRankThreads * kKeys;
+  constexpr int kAtOnce = 4;                                 // reads of four keys that are under way together
   static_assert(kKeys == 1 || kKeys == 4, "one page a thread, or a 128-bit read");
   static_assert(kKeys != 1 || kTiles == kTilesAtOnce, "a page a thread");
   __shared__ RankShared rank;
@@ -201,7 +203,8 @@ __global__ __launch_bounds__(kRankThreads) void pq_select_kernel(const SelectArg
   const int parts = (pages + a.part_pages - 1) / a.part_pages, part_end = min(pages, part0 + a.part_pages);
   const int begin = a.n_first, end = pages - a.n_last;       // pages there is a choice of
   const bool shared = kKeys != 1 && parts > 1, in_memory = shared && pages > kMostKeys;
-  const __amdgpu_buffer_rsrc_t r_keys = make_rsrc(a.keys + (shared ? unit * a.max_pages : 0), shared ? static_cast<uint32_t>(pages) * 4u : 0u);
+  const __amdgpu_buffer_rsrc_t r_keys = make_rsrc(a.keys + (shared ? unit * a.key_stride : 0), shared ? static_cast<uint32_t>(pages) * 4u : 0u);
+  auto stored = [&](int p0) { return __builtin_amdgcn_raw_buffer_load_b128(r_keys, p0 * 4, 0, kAuxDevice); };
   uint32_t own = 0;                                          // kKeys == 1: page tid's
   for (int done = 0; part0 + done < part_end; done += kPartPages) {
     if (done > 0) {
@@ -230,19 +233,37 @@ __global__ __launch_bounds__(kRankThreads) void pq_select_kernel(const SelectArg
     lds_barrier();
     if (stage == 0) return;
     if (tid == 0) reset_arrivals(a.arrivals + unit);
-    if (!in_memory)
-      for (int p = tid; p < pages; p += kRankThreads) in_lds[p] = __builtin_amdgcn_raw_buffer_load_b32(r_keys, p * 4, 0, kAuxDevice);
+    if (!in_memory) {
+      for (int p0 = tid * 4; p0 < pages; p0 += kAtOnce * kRound) {                 // (zeros behind the last)
+        u32x4 k[kAtOnce];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) k[j] = stored(p0 + j * kRound);
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j)
+          if (p0 + j * kRound < pages) *reinterpret_cast<u32x4*>(&in_lds[p0 + j * kRound]) = k[j];
+      }
+    }
   }
   int32_t id[kKeys];
 #pragma unroll
   for (int j = 0; j < kKeys; ++j) id[j] = tid * kKeys + j < pages ? row[tid * kKeys + j] : -1;
   if constexpr (kKeys != 1) lds_barrier();
-  auto key = [&](int p) { return in_memory ? __builtin_amdgcn_raw_buffer_load_b32(r_keys, p * 4, 0, kAuxDevice) : in_lds[p]; };
+  auto four = [&](int p0) { return in_memory ? stored(p0) : *reinterpret_cast<const u32x4*>(&in_lds[p0]); };
   auto each = [&](auto f) {
     if constexpr (kKeys == 1) {
       if (tid >= begin && tid < end) f(own);
     } else {
-      for (int p = begin + tid; p < end; p += kRankThreads) f(key(p));
+      for (int p0 = tid * 4; p0 < end; p0 += kAtOnce * kRound) {
+        u32x4 k[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+          if (p0 + i * kRound < end) k[i] = four(p0 + i * kRound);
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (p0 + i * kRound + j >= begin && p0 + i * kRound + j < end) f(k[i][j]);
+      }
     }
   };
   const Threshold t = find_threshold(rank, end - begin, static_cast<uint32_t>(a.n_selected - a.n_first - a.n_last), each, tid);
@@ -251,10 +272,14 @@ __global__ __launch_bounds__(kRankThreads) void pq_select_kernel(const SelectArg
     const int p0 = base + tid * kKeys;
     bool in[kKeys], chosen[kKeys];
     uint32_t k[kKeys], at[kKeys];
+    u32x4 now = {0, 0, 0, 0};
+    if constexpr (kKeys != 1) {
+      if (p0 < pages) now = four(p0);
+    }
 #pragma unroll
     for (int j = 0; j < kKeys; ++j) {
       in[j] = p0 + j >= begin && p0 + j < end;
-      k[j] = kKeys == 1 ? own : (in[j] ? key(p0 + j) : 0);
+      k[j] = kKeys == 1 ? own : now[j];
       if (base > 0) id[j] = p0 + j < pages ? row[p0 + j] : -1;
     }
     place_keys<kKeys>(rank, places, t, in, k, tid, chosen, at);
@@ -277,13 +302,14 @@ void launch_select(const SelectArgs& a, dim3 grid, hipStream_t st) {
 int64_t most_pages(int32_t max_seq_len) { return (static_cast<int64_t>(max_seq_len) + kGroup - 1) / kGroup; }
 
 // Pages of a work-group: all of a unit's, if that is one batch of loads a wavefront or the units fill the compute units; otherwise as few as make
-// no more than two work-groups a compute unit.
+// no more than a work-group a compute unit, or a batch.  (8 units of 1024 pages 8.2 us, a work-group each 15.6; 128 of 512 10.5 and 11.5; 256 of 512 14.3 and 13.6.
+// With twice as many work-groups 32 units of 1024 pages 10.7 instead of 9.3.)
 int32_t pages_of_part(const pq_layout* l, int32_t n_seqs, int32_t max_seq_len) {
   const int64_t pages = most_pages(max_seq_len), units = static_cast<int64_t>(n_seqs) * l->n_kv_heads;
   if (pages <= kBatchPages || (units >= kComputeUnits && pages <= kMostKeys)) return static_cast<int32_t>(std::min<int64_t>(pages, kMostKeys));
   for (int tiles = 1; tiles < kTilesAtOnce; tiles *= 2) {
     const int part = kRankWaves * tiles * kTilePages;
-    if (units * ((pages + part - 1) / part) <= kResidentGroups) return part;
+    if (units * ((pages + part - 1) / part) <= kComputeUnits) return part;
   }
   return kBatchPages;
 }
@@ -299,12 +325,13 @@ int check_selection(const pq_layout* l, int32_t n_seqs, int32_t n_q_heads, int32
   return PQ_OK;
 }
 
+int64_t key_stride(int32_t max_seq_len) { return (most_pages(max_seq_len) + 3) & ~int64_t{3}; }
 size_t round256(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
 size_t arrival_bytes(const pq_layout* l, int32_t n_seqs) { return round256(static_cast<size_t>(n_seqs) * l->n_kv_heads * sizeof(uint64_t)); }
 // The arrival words, then the keys.
 size_t select_bytes(const pq_layout* l, int32_t n_seqs, int32_t max_seq_len) {
   if (!shares_units(l, n_seqs, max_seq_len)) return 256;
-  return arrival_bytes(l, n_seqs) + round256(static_cast<size_t>(n_seqs) * l->n_kv_heads * most_pages(max_seq_len) * sizeof(uint32_t));
+  return arrival_bytes(l, n_seqs) + round256(static_cast<size_t>(n_seqs) * l->n_kv_heads * key_stride(max_seq_len) * sizeof(uint32_t));
 }
 
 // The arguments that the selection reads or writes, beyond check_selection().
@@ -345,6 +372,7 @@ int launch_selection(const pq_layout* l, const void* q, pq_dtype q_dtype, int32_
   a.n_first = n_first;
   a.n_last = n_last;
   a.q_is_f32 = q_dtype == PQ_F32 ? 1 : 0;
+  a.key_stride = static_cast<int32_t>(key_stride(max_seq_len));
   a.part_pages = pages_of_part(l, n_seqs, max_seq_len);
   const dim3 grid(l->n_kv_heads, n_seqs, (a.max_pages + a.part_pages - 1) / a.part_pages);
   if (a.max_pages <= kBatchPages) launch_select<kTilesAtOnce, 1>(a, grid, st);
