@@ -72,7 +72,7 @@ __global__ __launch_bounds__(kRankThreads) void pq_evict_kernel(const EvictArgs 
   uint32_t first_key[kKeysPerThread];
 #pragma unroll
   for (int j = 0; j < kKeysPerThread; ++j) first_key[j] = key_of_weight(weight[j]);
-  auto each = [&](auto f) {
+  auto each = [&](auto f) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < kKeysPerThread; ++j) {
       const int p = tid * kKeysPerThread + j;

@@ -249,20 +249,16 @@ __global__ __launch_bounds__(kRankThreads) void pq_select_kernel(const SelectArg
   for (int j = 0; j < kKeys; ++j) id[j] = tid * kKeys + j < pages ? row[tid * kKeys + j] : -1;
   if constexpr (kKeys != 1) lds_barrier();
   auto four = [&](int p0) { return in_memory ? stored(p0) : *reinterpret_cast<const u32x4*>(&in_lds[p0]); };
-  auto each = [&](auto f) {
+  auto each = [&](auto f) __attribute__((always_inline)) {
     if constexpr (kKeys == 1) {
       if (tid >= begin && tid < end) f(own);
     } else {
-      for (int p0 = tid * 4; p0 < end; p0 += kAtOnce * kRound) {
-        u32x4 k[kAtOnce];
+#pragma unroll 2
+      for (int p0 = tid * 4; p0 < end; p0 += kRound) {
+        const u32x4 k = four(p0);
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i)
-          if (p0 + i * kRound < end) k[i] = four(p0 + i * kRound);
-#pragma unroll
-        for (int i = 0; i < kAtOnce; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (p0 + i * kRound + j >= begin && p0 + i * kRound + j < end) f(k[i][j]);
+        for (int j = 0; j < 4; ++j)
+          if (p0 + j >= begin && p0 + j < end) f(k[j]);
       }
     }
   };
