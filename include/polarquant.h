@@ -555,7 +555,7 @@ int pq_decode_attention_weights(const pq_layout* layout, const void* q, pq_dtype
  *                   had: those that are left, then -1 and weights of 0
  *   lens_after      device int32 [n_seqs], written: tokens that are left; not seq_lens
  *   freed           device int32 [n_freed], written: block-table entries of the pages given up, sequence by sequence and in each from its
- *                   beginning, as they were (-1 where a page was missing); as far as n_freed.  free_pages of a later pq_plan_pages
+ *                   beginning, as they were (-1 where a page was missing; a page that two rows hold as often as they give it up); as far as n_freed.  free_pages of a later pq_plan_pages
  *   counts          device int32 [1], written: pages given up
  * n_seqs <= 65535.  No workspace; calls that overlap share nothing but their outputs.
  */

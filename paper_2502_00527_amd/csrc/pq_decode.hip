@@ -660,7 +660,7 @@ __global__ __launch_bounds__(kMergeThreads) void pq_page_weights_kernel(const We
   }
   const int at = threadIdx.x % kWeightPages, slice = threadIdx.x / kWeightPages, seq = blockIdx.y;
   const int first = (static_cast<int>(blockIdx.x) - (kMerge ? a.n_q_heads : 0)) * kWeightPages, page = first + at;
-  const int L = min(a.seq_lens[seq], a.max_seq_len), n_pages = L > 0 ? (L + kGroup - 1) / kGroup : 0;
+  const int L = max(0, min(a.seq_lens[seq], a.max_seq_len)), n_pages = L / kGroup + (L % kGroup != 0);
   if (first >= n_pages) return;
   const int chunks = kMerge ? chunks_of_pages(n_pages, a.plan.pages_per_chunk, a.plan.n_big, a.plan.pages_small) : 0;
   float w = 0.f;

@@ -66,7 +66,7 @@ __global__ __launch_bounds__(kRankThreads) void pq_evict_kernel(const EvictArgs 
   const Kept k = seq < a.n_seqs ? kept_of(a, seq) : Kept{0, 0, 0};
   before = wave_sum(before);
   if (lane == 0) sums[wave] = before;
-  const int begin = a.n_first, end = k.pages - k.last;
+  const int begin = min(a.n_first, k.pages), end = max(begin, k.pages - k.last);  // pages there is a choice of
   // the smallest weight has the largest key; a NaN counts as the largest weight
   auto key_of_weight = [](float w) { return ~(w == w ? key_of(w) : 0xffffffffu); };
   uint32_t first_key[kKeysPerThread];

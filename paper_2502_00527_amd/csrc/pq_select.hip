@@ -52,7 +52,7 @@ struct SelectArgs {
 };
 
 __device__ __forceinline__ int clamped(const SelectArgs& a, int seq) { return max(0, min(a.seq_lens[seq], a.max_seq_len)); }
-__device__ __forceinline__ int pages_up(int tokens) { return (tokens + kGroup - 1) / kGroup; }
+__device__ __forceinline__ int pages_up(int tokens) { return tokens / kGroup + (tokens % kGroup != 0); }
 
 // The queries of a KV head as operands.  Lane l has head 4 s + l % 4 of set s, block (l / 4) % 4, and of its 16 pairs part l / 16: x, y, |x| or |y|.
 // Heads past the last are that one again.

@@ -508,7 +508,8 @@ LENS = [10000, 0, 1, 127, 128, 129, 1280, 1281, 9999, 5120, -4]
 
 @pytest.mark.parametrize("in_place", [False, True])
 @pytest.mark.parametrize("ties", [False, True])
-@pytest.mark.parametrize("n_kept,n_first,n_last", [(10, 1, 2), (0, 0, 0), (1, 0, 0), (5, 4, 4), (40, 0, 1), (79, 2, 0), (1000, 1, 1), (3, 100, 2)])
+@pytest.mark.parametrize("n_kept,n_first,n_last", [(10, 1, 2), (0, 0, 0), (1, 0, 0), (5, 4, 4), (40, 0, 1), (79, 2, 0), (1000, 1, 1), (3, 100, 2),
+                                                    (2 ** 31 - 1, 0, 0), (3, 2 ** 31 - 1, 1), (3, 1, 2 ** 31 - 1), (0, 2 ** 31 - 1, 2 ** 31 - 1)])
 def test_evictions(n_kept, n_first, n_last, ties, in_place):
     _check_evict(LENS, 79, n_kept, n_first, n_last, ties=ties, in_place=in_place)
 
@@ -524,6 +525,14 @@ def test_evictions_of_long_sequences(pages, kept):
 def test_evictions_of_many_sequences():
     lens = [int(n) for n in np.random.default_rng(7).integers(0, 3000, 1500)]
     _check_evict(lens, 24, 9, 1, 2)
+
+
+def test_two_sequences_that_share_pages():
+    """A page that two rows hold is in the list of freed ones as often as it was given up, and stays where it was kept."""
+    def change(table, weights):
+        table[8, :20] = table[0, :20]
+        weights[8, :20] = weights[0, :20] + 1
+    _check_evict(LENS, 79, 10, 1, 2, change=change)
 
 
 def test_evicted_pages_beyond_the_list():
