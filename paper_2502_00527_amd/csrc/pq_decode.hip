@@ -660,49 +660,64 @@ __global__ __launch_bounds__(kMergeThreads) void pq_page_weights_kernel(const We
   }
   const int at = threadIdx.x % kWeightPages, slice = threadIdx.x / kWeightPages, seq = blockIdx.y;
   const int first = (static_cast<int>(blockIdx.x) - (kMerge ? a.n_q_heads : 0)) * kWeightPages, page = first + at;
+  const int64_t row0 = static_cast<int64_t>(seq) * a.n_q_heads, i = seq * a.weights_stride + page;
+  const bool in_row = page < a.page_stride;
+  auto page_of = [&](int h) { return in_row ? a.page_ml[(row0 + h) * a.page_stride + page] : make_float2(0.f, 0.f); };
+  // a first round of heads is asked for without waiting for the length: the rows are there whatever it is
+  constexpr int kAhead = 2;
+  float2 one[kAhead], all[kAhead];
+#pragma unroll
+  for (int j = 0; j < kAhead; ++j) {
+    const int h = slice + j * kWeightSlices;
+    one[j] = h < a.n_q_heads ? page_of(h) : make_float2(0.f, 0.f);
+    if constexpr (!kMerge) all[j] = h < a.n_q_heads ? a.totals[row0 + h] : make_float2(0.f, 1.f);
+  }
   const int L = max(0, min(a.seq_lens[seq], a.max_seq_len)), n_pages = L / kGroup + (L % kGroup != 0);
   if (first >= n_pages) return;
+  const float before = slice == 0 && page < n_pages && a.before && a.decay != 0.f ? a.before[i] : 0.f;
   const int chunks = kMerge ? chunks_of_pages(n_pages, a.plan.pages_per_chunk, a.plan.n_big, a.plan.pages_small) : 0;
-  float w = 0.f;
-#pragma unroll kMerge ? 1 : 4
-  for (int h = slice; h < a.n_q_heads; h += kWeightSlices) {
-    const int64_t row = static_cast<int64_t>(seq) * a.n_q_heads + h;
-    const float2 one = page < n_pages ? a.page_ml[row * a.page_stride + page] : make_float2(0.f, 0.f);
-    float2 all;
-    if constexpr (kMerge) {
-      const float2* const ml = reinterpret_cast<const float2*>(a.ws_ml) + row * a.plan.n_chunks;
-      all = make_float2(kNegInf, 0.f);
-      for (int c = at; c < chunks; c += kWeightPages) {
-        const float2 of = ml[c];
-        const float top = fmaxf(all.x, of.x);
-        if (top > kNegInf) all.y = all.y * __builtin_amdgcn_exp2f(all.x - top) + of.y * __builtin_amdgcn_exp2f(of.x - top);
-        all.x = top;
-      }
-      float top = all.x;
-      top = fmaxf(top, dpp_of<0x128>(top));
-      top = fmaxf(top, dpp_of<0x124>(top));
-      top = fmaxf(top, dpp_of<0x122>(top));
-      top = fmaxf(top, dpp_of<0x121>(top));
-      float sum = top > kNegInf ? all.y * __builtin_amdgcn_exp2f(all.x - top) : 0.f;
-      sum += dpp_of<0x128>(sum);
-      sum += dpp_of<0x124>(sum);
-      sum += dpp_of<0x122>(sum);
-      sum += dpp_of<0x121>(sum);
-      all = make_float2(top, sum);
-    } else {
-      all = a.totals[row];
+  auto total_of = [&](int h) {
+    if constexpr (!kMerge) return a.totals[row0 + h];
+    const float2* const ml = reinterpret_cast<const float2*>(a.ws_ml) + (row0 + h) * a.plan.n_chunks;
+    float2 t = make_float2(kNegInf, 0.f);
+    for (int c = at; c < chunks; c += kWeightPages) {
+      const float2 of = ml[c];
+      const float top = fmaxf(t.x, of.x);
+      if (top > kNegInf) t.y = t.y * __builtin_amdgcn_exp2f(t.x - top) + of.y * __builtin_amdgcn_exp2f(of.x - top);
+      t.x = top;
     }
-    if (one.y > 0.f) w += one.y * __builtin_amdgcn_exp2f(one.x - all.x) / all.y;
+    float top = t.x;
+    top = fmaxf(top, dpp_of<0x128>(top));
+    top = fmaxf(top, dpp_of<0x124>(top));
+    top = fmaxf(top, dpp_of<0x122>(top));
+    top = fmaxf(top, dpp_of<0x121>(top));
+    float sum = top > kNegInf ? t.y * __builtin_amdgcn_exp2f(t.x - top) : 0.f;
+    sum += dpp_of<0x128>(sum);
+    sum += dpp_of<0x124>(sum);
+    sum += dpp_of<0x122>(sum);
+    sum += dpp_of<0x121>(sum);
+    return make_float2(top, sum);
+  };
+  float w = 0.f;
+  auto add = [&](float2 of_page, float2 of_all) {
+    if (page < n_pages && of_page.y > 0.f) w += of_page.y * __builtin_amdgcn_exp2f(of_page.x - of_all.x) / of_all.y;
+  };
+#pragma unroll
+  for (int j = 0; j < kAhead; ++j) {
+    const int h = slice + j * kWeightSlices;
+    if (h < a.n_q_heads) {
+      if constexpr (kMerge) all[j] = total_of(h);
+      add(one[j], all[j]);
+    }
   }
+  for (int h = slice + kAhead * kWeightSlices; h < a.n_q_heads; h += kWeightSlices) add(page_of(h), total_of(h));
   part[slice][at] = w;
   __syncthreads();
   if (slice != 0 || page >= n_pages) return;
   w = 0.f;
 #pragma unroll
-  for (int i = 0; i < kWeightSlices; ++i) w += part[i][at];
-  const int64_t i = seq * a.weights_stride + page;
-  if (a.before && a.decay != 0.f) w += a.decay * a.before[i];
-  a.weights[i] = w;
+  for (int s = 0; s < kWeightSlices; ++s) w += part[s][at];
+  a.weights[i] = a.before && a.decay != 0.f ? w + a.decay * before : w;
 }
 
 struct WeightsWorkspace {
