@@ -200,7 +200,7 @@ __global__ __launch_bounds__(kBoundThreads, kGroupedAngles ? 5 : 8) void pq_boun
   const int64_t ph0 = page * a.n_kv_heads + head0;
   load(ph0);
   for (int i = tid; i < kWords * kPairs; i += kBoundThreads) (&seen[0][0])[i] = 0;
-  lds_barrier();
+  __syncthreads();
   for (int h = 0; h < heads; ++h) {
     const float rs = half_of(radius_par, 0), rz = half_of(radius_par, 1), ts = half_of(angle_par, 0), tz = half_of(angle_par, 1);
     uint32_t d[2][4];
@@ -222,7 +222,7 @@ __global__ __launch_bounds__(kBoundThreads, kGroupedAngles ? 5 : 8) void pq_boun
         set(__builtin_amdgcn_perm(words, lane4, 0x0c0c0700u), bit_of_byte<3>(four, one));
       }
     }
-    lds_barrier();
+    __syncthreads();
 
     float low_x = INFINITY, high_x = -INFINITY, low_y = INFINITY, high_y = -INFINITY;
 #pragma unroll kGroupedAngles ? 1 : (1 << TB) / 4
@@ -246,7 +246,7 @@ __global__ __launch_bounds__(kBoundThreads, kGroupedAngles ? 5 : 8) void pq_boun
       high_y = max3(high_y, near * sn, far * sn);
     }
     *reinterpret_cast<float4*>(part[wave][lane]) = make_float4(low_x, high_x, low_y, high_y);
-    lds_barrier();
+    __syncthreads();
     if (h + 1 < heads) {                                     // the bits have been read
       for (int i = tid; i < kWords * kPairs; i += kBoundThreads) (&seen[0][0])[i] = 0;
     }
@@ -273,7 +273,7 @@ __global__ __launch_bounds__(kBoundThreads, kGroupedAngles ? 5 : 8) void pq_boun
       dst[48] = code(high_y - low_y);
       if (k == 0) a.scales[ph * kBlocks + block] = largest / 127.0f;
     }
-    if (h + 1 < heads) lds_barrier();
+    if (h + 1 < heads) __syncthreads();
   }
 }
 

@@ -57,13 +57,6 @@ __device__ __forceinline__ uint32_t sum_from(uint32_t x, int lane) {
   return x + (lane < 16 ? r1 : 0) + (lane < 32 ? r2 : 0) + (lane < 48 ? r3 : 0);
 }
 
-// A wait of the work-group for what it has written to LDS.  (__syncthreads() also waits for every load from memory that is under way.)
-__device__ __forceinline__ void lds_barrier() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-  __builtin_amdgcn_s_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-}
-
 struct RankShared {
   __attribute__((aligned(16))) uint32_t hist[kBins];
   __attribute__((aligned(16))) uint32_t low[kRankWaves], high[kRankWaves];
@@ -95,7 +88,7 @@ __device__ __forceinline__ Threshold find_threshold(RankShared& sh, int count, u
   }
   reinterpret_cast<uint4*>(sh.hist)[tid] = make_uint4(0, 0, 0, 0);
   if (tid == 0) sh.listed = 0;
-  lds_barrier();
+  __syncthreads();
   if (k == 0) return {0xffffffffu, 0};
   if (k >= static_cast<uint32_t>(count)) return {0, 0xffffffffu};
   const uint4 lows = *reinterpret_cast<const uint4*>(sh.low), highs = *reinterpret_cast<const uint4*>(sh.high);
@@ -107,7 +100,7 @@ __device__ __forceinline__ Threshold find_threshold(RankShared& sh, int count, u
       const uint32_t off = v - base;
       if (v >= base && off <= limit) atomicAdd(&sh.hist[off >> shift], 1u);
     });
-    lds_barrier();
+    __syncthreads();
     // every wavefront for itself: the bin where the count from above crosses k
     constexpr int kOwn = kBins / 64;
     uint32_t h[kOwn], sum = 0;
@@ -144,7 +137,7 @@ __device__ __forceinline__ Threshold find_threshold(RankShared& sh, int count, u
       each([&](uint32_t v) {
         if (v >= base && v - base <= limit) sh.list[atomicAdd(&sh.listed, 1u)] = v;
       });
-      lds_barrier();
+      __syncthreads();
       const uint32_t mine = static_cast<uint32_t>(lane) < inside ? sh.list[lane] : 0;
       uint32_t larger = 0, equal = 0;
       for (uint32_t j = 0; j < inside; ++j) {
@@ -155,9 +148,9 @@ __device__ __forceinline__ Threshold find_threshold(RankShared& sh, int count, u
       const int here = __builtin_ctzll(__builtin_amdgcn_ballot_w64(static_cast<uint32_t>(lane) < inside && larger < k && larger + equal >= k));
       return {static_cast<uint32_t>(__builtin_amdgcn_readlane(mine, here)), k - __builtin_amdgcn_readlane(larger, here)};
     }
-    lds_barrier();                                           // everybody has read the bins
+    __syncthreads();                                           // everybody has read the bins
     reinterpret_cast<uint4*>(sh.hist)[tid] = make_uint4(0, 0, 0, 0);
-    lds_barrier();
+    __syncthreads();
   }
   return {base, k};
 }
@@ -187,7 +180,7 @@ __device__ __forceinline__ void place_keys(RankShared& sh, Places& p, const Thre
     all_ties += __builtin_popcountll(b);
   }
   if (lane == 0) sh.counts[p.turn][wave] = make_uint2(all_sure, all_ties);
-  lds_barrier();
+  __syncthreads();
   sure += p.sure;
   ties += p.ties;
 #pragma unroll

@@ -228,9 +228,9 @@ __global__ __launch_bounds__(kRankThreads) void pq_select_kernel(const SelectArg
   }
   if (shared) {
     stores_done();
-    lds_barrier();
+    __syncthreads();
     if (tid == 0) stage = arrive(a.arrivals + unit, parts) ? 1 : 0;
-    lds_barrier();
+    __syncthreads();
     if (stage == 0) return;
     if (tid == 0) reset_arrivals(a.arrivals + unit);
     if (!in_memory) {
@@ -247,7 +247,7 @@ __global__ __launch_bounds__(kRankThreads) void pq_select_kernel(const SelectArg
   int32_t id[kKeys];
 #pragma unroll
   for (int j = 0; j < kKeys; ++j) id[j] = tid * kKeys + j < pages ? row[tid * kKeys + j] : -1;
-  if constexpr (kKeys != 1) lds_barrier();
+  if constexpr (kKeys != 1) __syncthreads();
   auto four = [&](int p0) { return in_memory ? stored(p0) : *reinterpret_cast<const u32x4*>(&in_lds[p0]); };
   auto each = [&](auto f) __attribute__((always_inline)) {
     if constexpr (kKeys == 1) {
