@@ -10,7 +10,8 @@
 // (8 x 20K .. 32K tokens x 8 heads).  So a wavefront loads a token's unit of 16 symbols a lane and transposes bytes between the 16 lanes of a
 // block of pairs in registers: 20 instructions for 16 symbols.  What bounds it then is vector issue.
 //
-// One work-group one or four KV heads of a page, the next head's codes on their way while one is worked on; wavefront = 32 tokens.
+// One work-group a page and KV head; wavefront = 32 tokens.  16384 pages and heads of 8-bit symbols: 35.9 us, 4096: 11.3, 512: 3.7.  With four
+// heads one after the other, the next one's codes on their way meanwhile: 39.1, 13.9, 7.2.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -27,8 +28,6 @@ namespace {
 constexpr int kBoundThreads = 256;
 constexpr int kBoundBytes = 4 * kPairs;                      // of a page and head: centres and half-widths of 128 channels
 constexpr float kTiny = 0x1p-100f;                           // below it a block's bounds are zeros
-// Pages times KV heads from which on a work-group takes four heads: fewer are all under way at once.
-constexpr int64_t kManyHeads = 8 * 1024;
 
 struct BoundArgs {
   const uint8_t* codes;
@@ -41,7 +40,6 @@ struct BoundArgs {
   int64_t n_pool_pages;
   int32_t n_kv_heads;
   int32_t max_pages_per_seq;
-  int32_t heads_of_group;                                    // KV heads of a work-group
 };
 
 // cos and sin of the centres of the uniform grid's bins, rounded once from float64.
@@ -172,14 +170,13 @@ __global__ __launch_bounds__(kBoundThreads, kGroupedAngles ? 5 : 8) void pq_boun
   auto& seen = sh.seen;
   auto& part = sh.part;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int per_page = (a.n_kv_heads + a.heads_of_group - 1) / a.heads_of_group;
-  const int nth = blockIdx.x / per_page, head0 = blockIdx.x % per_page * a.heads_of_group, seq = blockIdx.y;
+  const int kvh = blockIdx.x % a.n_kv_heads, nth = blockIdx.x / a.n_kv_heads, seq = blockIdx.y;
   const int first = a.lens_before ? max(0, a.lens_before[seq]) / kGroup : 0, last = max(0, a.lens_after[seq]) / kGroup;
   const int64_t page_of = static_cast<int64_t>(first) + nth;
   if (page_of >= last || page_of >= a.max_pages_per_seq) return;
   const int64_t page = a.block_table[static_cast<int64_t>(seq) * a.max_pages_per_seq + page_of];
   if (page < 0 || page >= a.n_pool_pages) return;
-  const int heads = min(a.heads_of_group, a.n_kv_heads - head0);
+  const int64_t ph = page * a.n_kv_heads + kvh;
   const int block = lane_block(lane), k = lane_place(lane), pair = block * 16 + k;
   // bytes {0, 1} of the own word and of the other lane's in the lane below, {2, 3} in the one above; then the even ones and the odd ones
   const uint32_t select2 = lane & 2 ? 0x03020706u : 0x05040100u, select1 = lane & 1 ? 0x03070105u : 0x06020400u;
@@ -188,93 +185,77 @@ __global__ __launch_bounds__(kBoundThreads, kGroupedAngles ? 5 : 8) void pq_boun
   uint32_t one = 1;
   asm("" : "+v"(one));
   TokenUnit<W> raw[2];
-  uint32_t radius_par = 0, angle_par = 0;
-  auto load = [&](int64_t ph) {
-    const uint8_t* const from = a.codes + ph * (kBlocks * kGroup * UB) + (block * kGroup + wave * 32 + k) * UB;
-    raw[0].load(from);
-    raw[1].load(from + 16 * UB);
-    const uint32_t* const par = a.params + ph * (kPairs * (kGroupedAngles ? 2 : 1));
-    radius_par = par[pair];
-    if constexpr (kGroupedAngles) angle_par = par[kPairs + pair];
-  };
-  const int64_t ph0 = page * a.n_kv_heads + head0;
-  load(ph0);
+  const uint8_t* const from = a.codes + ph * (kBlocks * kGroup * UB) + (block * kGroup + wave * 32 + k) * UB;
+  raw[0].load(from);
+  raw[1].load(from + 16 * UB);
+  const uint32_t* const par = a.params + ph * (kPairs * (kGroupedAngles ? 2 : 1));
+  const uint32_t radius_par = par[pair], angle_par = kGroupedAngles ? par[kPairs + pair] : 0;
   for (int i = tid; i < kWords * kPairs; i += kBoundThreads) (&seen[0][0])[i] = 0;
   __syncthreads();
-  for (int h = 0; h < heads; ++h) {
-    const float rs = half_of(radius_par, 0), rz = half_of(radius_par, 1), ts = half_of(angle_par, 0), tz = half_of(angle_par, 1);
-    uint32_t d[2][4];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) raw[u].symbols(d[u]);
-    if (h + 1 < heads) load(ph0 + h + 1);
+  for (int u = 0; u < 2; ++u) {
+    uint32_t d[4];
+    raw[u].symbols(d);
+    transpose_bytes(d, select2, select1);
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      transpose_bytes(d[u], select2, select1);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t four = d[u][i], words = (four >> 5) & (0x01010101u * (kWords - 1));       // (bits above a symbol's are another's)
-        auto set = [&](uint32_t at, uint32_t bit) {
-          __hip_atomic_fetch_or((PQ_LDS uint32_t*)static_cast<uintptr_t>(seen_at + at), bit, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-        };
-        set(__builtin_amdgcn_perm(words, lane4, 0x0c0c0400u), bit_of_byte<0>(four, one));
-        set(__builtin_amdgcn_perm(words, lane4, 0x0c0c0500u), bit_of_byte<1>(four, one));
-        set(__builtin_amdgcn_perm(words, lane4, 0x0c0c0600u), bit_of_byte<2>(four, one));
-        set(__builtin_amdgcn_perm(words, lane4, 0x0c0c0700u), bit_of_byte<3>(four, one));
-      }
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t four = d[i], words = (four >> 5) & (0x01010101u * (kWords - 1));            // (bits above a symbol's are another's)
+      auto set = [&](uint32_t at, uint32_t bit) {
+        __hip_atomic_fetch_or((PQ_LDS uint32_t*)static_cast<uintptr_t>(seen_at + at), bit, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+      };
+      set(__builtin_amdgcn_perm(words, lane4, 0x0c0c0400u), bit_of_byte<0>(four, one));
+      set(__builtin_amdgcn_perm(words, lane4, 0x0c0c0500u), bit_of_byte<1>(four, one));
+      set(__builtin_amdgcn_perm(words, lane4, 0x0c0c0600u), bit_of_byte<2>(four, one));
+      set(__builtin_amdgcn_perm(words, lane4, 0x0c0c0700u), bit_of_byte<3>(four, one));
     }
-    __syncthreads();
-
-    float low_x = INFINITY, high_x = -INFINITY, low_y = INFINITY, high_y = -INFINITY;
-#pragma unroll kGroupedAngles ? 1 : (1 << TB) / 4
-    for (int i = 0; i < (1 << TB) / 4; ++i) {
-      const int state = 4 * i + wave;                        // angle code
-      const uint32_t radii = (seen[state / kOfWord][lane] >> ((state % kOfWord) << RB)) & static_cast<uint32_t>((uint64_t{1} << (1 << RB)) - 1);
-      float cs, sn;
-      if constexpr (kGroupedAngles) {
-        cos_sin((state + 0.5) * static_cast<double>(ts) + static_cast<double>(tz), cs, sn);
-      } else {
-        cs = bins.cs[state];
-        sn = bins.sn[state];
-      }
-      // (c + 1/2) s is exact, so that one rounding is what its sum with z has.  A state that nobody has is no number, which minima and maxima pass over
-      float near = fmaf(__builtin_ctz(radii) + 0.5f, rs, rz), far = fmaf(31.5f - __builtin_clz(radii), rs, rz);
-      near = radii == 0 ? NAN : near;
-      far = radii == 0 ? NAN : far;
-      low_x = min3(low_x, near * cs, far * cs);
-      high_x = max3(high_x, near * cs, far * cs);
-      low_y = min3(low_y, near * sn, far * sn);
-      high_y = max3(high_y, near * sn, far * sn);
-    }
-    *reinterpret_cast<float4*>(part[wave][lane]) = make_float4(low_x, high_x, low_y, high_y);
-    __syncthreads();
-    if (h + 1 < heads) {                                     // the bits have been read
-      for (int i = tid; i < kWords * kPairs; i += kBoundThreads) (&seen[0][0])[i] = 0;
-    }
-    if (wave == (h & 3)) {                                   // the wavefronts in turn
-#pragma unroll
-      for (int w = 1; w < kBoundThreads / 64; ++w) {
-        const float4 p = *reinterpret_cast<const float4*>(part[(wave + w) & 3][lane]);
-        low_x = fminf(low_x, p.x);
-        high_x = fmaxf(high_x, p.y);
-        low_y = fminf(low_y, p.z);
-        high_y = fmaxf(high_y, p.w);
-      }
-      float largest = fmaxf(fmaxf(fabsf(low_x), fabsf(high_x)), fmaxf(fabsf(low_y), fabsf(high_y)));
-      largest = fmaxf(largest, __builtin_bit_cast(float, moved<0x4e>(__builtin_bit_cast(uint32_t, largest))));   // of the block's 16 pairs
-      largest = fmaxf(largest, __builtin_bit_cast(float, moved<0xb1>(__builtin_bit_cast(uint32_t, largest))));
-      largest = max_rows(largest);
-      const float up = largest >= kTiny ? 127.0f / largest : 0.f;
-      auto code = [&](float v) { return static_cast<int8_t>(static_cast<int>(rintf(v * 0.5f * up))); };
-      const int64_t ph = ph0 + h;
-      int8_t* const dst = a.bounds + ph * kBoundBytes + block * (kBoundBytes / kBlocks) + k;
-      dst[0] = code(low_x + high_x);
-      dst[16] = code(low_y + high_y);
-      dst[32] = code(high_x - low_x);
-      dst[48] = code(high_y - low_y);
-      if (k == 0) a.scales[ph * kBlocks + block] = largest / 127.0f;
-    }
-    if (h + 1 < heads) __syncthreads();
   }
+  __syncthreads();
+
+  const float rs = half_of(radius_par, 0), rz = half_of(radius_par, 1), ts = half_of(angle_par, 0), tz = half_of(angle_par, 1);
+  float low_x = INFINITY, high_x = -INFINITY, low_y = INFINITY, high_y = -INFINITY;
+#pragma unroll kGroupedAngles ? 1 : (1 << TB) / 4
+  for (int i = 0; i < (1 << TB) / 4; ++i) {
+    const int state = 4 * i + wave;                        // angle code
+    const uint32_t radii = (seen[state / kOfWord][lane] >> ((state % kOfWord) << RB)) & static_cast<uint32_t>((uint64_t{1} << (1 << RB)) - 1);
+    float cs, sn;
+    if constexpr (kGroupedAngles) {
+      cos_sin((state + 0.5) * static_cast<double>(ts) + static_cast<double>(tz), cs, sn);
+    } else {
+      cs = bins.cs[state];
+      sn = bins.sn[state];
+    }
+    // (c + 1/2) s is exact, so that one rounding is what its sum with z has.  A state that nobody has is no number, which minima and maxima pass over
+    float near = fmaf(__builtin_ctz(radii) + 0.5f, rs, rz), far = fmaf(31.5f - __builtin_clz(radii), rs, rz);
+    near = radii == 0 ? NAN : near;
+    far = radii == 0 ? NAN : far;
+    low_x = min3(low_x, near * cs, far * cs);
+    high_x = max3(high_x, near * cs, far * cs);
+    low_y = min3(low_y, near * sn, far * sn);
+    high_y = max3(high_y, near * sn, far * sn);
+  }
+  *reinterpret_cast<float4*>(part[wave][lane]) = make_float4(low_x, high_x, low_y, high_y);
+  __syncthreads();
+  if (wave != 0) return;
+#pragma unroll
+  for (int w = 1; w < kBoundThreads / 64; ++w) {
+    const float4 p = *reinterpret_cast<const float4*>(part[w][lane]);
+    low_x = fminf(low_x, p.x);
+    high_x = fmaxf(high_x, p.y);
+    low_y = fminf(low_y, p.z);
+    high_y = fmaxf(high_y, p.w);
+  }
+  float largest = fmaxf(fmaxf(fabsf(low_x), fabsf(high_x)), fmaxf(fabsf(low_y), fabsf(high_y)));
+  largest = fmaxf(largest, __builtin_bit_cast(float, moved<0x4e>(__builtin_bit_cast(uint32_t, largest))));   // of the block's 16 pairs
+  largest = fmaxf(largest, __builtin_bit_cast(float, moved<0xb1>(__builtin_bit_cast(uint32_t, largest))));
+  largest = max_rows(largest);
+  const float up = largest >= kTiny ? 127.0f / largest : 0.f;
+  auto code = [&](float v) { return static_cast<int8_t>(static_cast<int>(rintf(v * 0.5f * up))); };
+  int8_t* const dst = a.bounds + ph * kBoundBytes + block * (kBoundBytes / kBlocks) + k;
+  dst[0] = code(low_x + high_x);
+  dst[16] = code(low_y + high_y);
+  dst[32] = code(high_x - low_x);
+  dst[48] = code(high_y - low_y);
+  if (k == 0) a.scales[ph * kBlocks + block] = largest / 127.0f;
 }
 
 template <int RB, int TB>
@@ -331,8 +312,7 @@ extern "C" int pq_bound_pages(const pq_layout* layout, const void* codes_pool, c
   a.n_pool_pages = n_pool_pages;
   a.n_kv_heads = layout->n_kv_heads;
   a.max_pages_per_seq = max_pages_per_seq;
-  a.heads_of_group = groups * n_seqs * layout->n_kv_heads >= kManyHeads ? 4 : 1;
-  const dim3 grid(static_cast<uint32_t>(groups * ((layout->n_kv_heads + a.heads_of_group - 1) / a.heads_of_group)), static_cast<uint32_t>(n_seqs));
+  const dim3 grid(static_cast<uint32_t>(groups * layout->n_kv_heads), static_cast<uint32_t>(n_seqs));
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   switch (layout->r_bits * 10 + layout->t_bits) {
     case 44: launch_bound<4, 4>(layout, a, grid, st); break;
