@@ -736,6 +736,67 @@ def test_captured_steps():
             assert torch.equal(a.nan_to_num(nan=-3.0) if a.is_floating_point() else a, b.nan_to_num(nan=-3.0) if b.is_floating_point() else b)
 
 
+@pytest.mark.parametrize("grouped,v_bits", [(False, 16), (True, 16), (False, 4)])
+def test_pages_far_into_the_pools(grouped, v_bits):
+    """Bytes of codes and values past 2^32: the same as near the pools' beginning.  (By a multiple of 8 pages: values are read in an order
+    that depends on the page's id modulo 8.)"""
+    c = Cache([1500, 515, 60, 1408], 2, (4, 4), grouped, v_bits)
+    q = _queries(4, 8, 3)
+
+    def results():
+        pools = _bound(c)
+        return pools, _sparse(c, q, pools, 4), _weigh(c, q)
+
+    near = results()
+    n = c.codes.shape[0]
+    far = ((1 << 32) // (2 * 4 * G * 16) + 15) // 8 * 8
+    for name in ("codes", "params", "v_pool", "v_params"):
+        small = getattr(c, name)
+        if small is not None:
+            big = torch.empty((far + n, *small.shape[1:]), dtype=small.dtype, device=DEV)
+            big[far:] = small
+            setattr(c, name, big)
+    assert c.codes.nbytes > 1 << 32 and c.v_pool.nbytes > 1 << 32
+    c.block_table = torch.where(c.block_table >= 0, c.block_table + far, c.block_table)
+    c.table = np.where(c.table >= 0, c.table + far, c.table)
+    pools, sparse, weigh = results()
+    for a, b in zip(near[0], pools):
+        assert torch.equal(a.view(torch.uint8), b[far:].view(torch.uint8))
+    out, selected, lens = near[1]
+    assert torch.equal(sparse[0], out) and torch.equal(sparse[1], torch.where(selected >= 0, selected + far * c.heads, selected)) and torch.equal(sparse[2], lens)
+    assert torch.equal(weigh[0], near[2][0]) and torch.equal(weigh[1], near[2][1])
+
+
+def test_bounds_far_into_their_pool():
+    c = _Plain([700 * G], 8, 700)
+    bounds, scales = _random_pools(700, 8, 4)
+    q = _queries(1, 32, 5)
+    want = _select(c, q, bounds, scales, 20)
+    far = (1 << 32) // (8 * 256) + 5
+    pools = [torch.empty((far + 700, *x.shape[1:]), dtype=x.dtype, device=DEV) for x in (bounds, scales)]
+    for big, small in zip(pools, (bounds, scales)):
+        big[far:] = small
+    c.block_table += far
+    got = _select(c, q, *pools, 20)
+    assert torch.equal(got[0], want[0] + far * 8) and torch.equal(got[1], want[1])
+
+
+def test_one_workspace_for_calls_of_many_shapes():
+    """What one call leaves there is nothing to the next: arrival words lie where another shape's keys were."""
+    import paper_2502_00527_amd as pq
+    cases = []
+    for seqs, heads, pages in [(1, 1, 300), (3, 1, 5000), (2, 8, 1030), (1, 2, 9000), (1, 4, 1500), (40, 2, 700)]:
+        c = _Plain([pages * G] * seqs, heads, 500, seed=pages)
+        cases.append((c, _queries(seqs, 4 * heads, pages), *_random_pools(500, heads, pages)))
+    wants = [_select(*case, 17) for case in cases]
+    work = torch.from_numpy(np.random.default_rng(3).integers(0, 256, max(pq.pq_select_workspace_bytes(c.layout, len(c.lens), c.max_seq_len) for c, *_ in cases)).astype(np.uint8)).to(DEV)
+    for at in list(range(6)) + [4, 0, 3, 3, 1, 5, 2, 0]:
+        c, q, bounds, scales = cases[at]
+        selected, lens = torch.zeros_like(wants[at][0]), torch.zeros_like(wants[at][1])
+        pq.pq_select_pages(c.layout, q, bounds, scales, c.block_table, c.seq_lens, c.max_seq_len, 1, 1, selected, lens, work)
+        assert torch.equal(selected, wants[at][0]) and torch.equal(lens, wants[at][1]), at
+
+
 def test_calls_on_another_stream():
     """Two streams at once, a workspace each."""
     c = Cache([3000, 515, 60, 1408], 2)
