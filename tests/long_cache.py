@@ -108,7 +108,7 @@ def page_weights(cache, s, q):
         kh, qh = k[:, h // group], q[h].double()
         w = torch.softmax((kh * qh).sum(-1) * cache.sm_scale, 0)
         total[:len(w)] += w
-        most = max(most, float(((kh * qh).abs().sum(-1)).max()) * float(cache.sm_scale))
+        most = max(most, float(((kh * qh).abs().sum(-1)).max()) * abs(float(cache.sm_scale)))
     return total.view(pages, G).sum(-1), most
 
 

@@ -375,6 +375,36 @@ def test_a_choice_that_is_given():
     assert torch.equal(own, _sparse(c, other, None, 4, given=(selected, lens))[0])
 
 
+@pytest.mark.parametrize("grouped", [False, True])
+@pytest.mark.parametrize("sm_scale", [-0.088, 0.0])
+def test_negative_and_zero_softmax_scales(sm_scale, grouped):
+    """The choice goes by the scores without it."""
+    c = Cache([1500, 515, 60], 2, (4, 4), grouped)
+    c.sm_scale = sm_scale
+    q = _queries(3, 8, 3)
+    _check_sparse(c, q, 4)
+    _check_weights(c, q)
+
+
+@pytest.mark.parametrize("grouped", [False, True])
+def test_sparse_of_missing_pages(grouped):
+    """Pages outside the pool count as no tokens; where all are, the output is zero."""
+    c = Cache([1500, 700, 1280], 2, (4, 4), grouped)
+    pools = _bound(c)
+    q = _queries(3, 8, 3)
+    c.block_table[0, 3:] = c.codes.shape[0]
+    c.block_table[1, :] = -1
+    out, selected, lens = _sparse(c, q, pools, 6, 1, 2)
+    assert not out[1].any() and bool((selected[1] == -1).all()) and lens[1].tolist() == [700] * 2
+    assert bool((selected[0, :, :3] >= 0).all()) and bool((selected[0, :, 3:] == -1).all())
+    tokens = 3 * G
+    for h in range(8):
+        k, v = c.k64[0][:tokens, h // 4], c.v64[0][:tokens, h // 4]
+        w = torch.softmax((k * q[0, h].double()).sum(-1) * c.sm_scale, 0)
+        want = (w[:, None] * v).sum(0)
+        assert float((out[0, h].double() - want).norm() / want.norm()) <= 1e-6
+
+
 # ---- attention that sums the pages' weights --------------------------------------------------------------
 
 
