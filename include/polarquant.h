@@ -508,7 +508,8 @@ size_t pq_sparse_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_
 
 /*
  * pq_sparse_attention -- pq_select_pages, and decode attention over the chosen pages.  Arguments as in pq_select_pages and
- * pq_decode_attention (raw scores apart); results are pq_decode_attention's over the tokens of the chosen pages, in precision too.  A sequence of
+ * pq_decode_attention (raw scores apart); results are pq_decode_attention's over the tokens of the chosen pages, in precision too -- quantized values
+ * are summed about the middle of their codes here and in pq_decode_attention_weights, which is 2 to 4 times as precise.  A sequence of
  * no more than n_selected pages gets attention over all of it.
  *   bounds, bound_scales   both NULL: `selected` and `selected_lens` are given, as pq_select_pages wrote them for the same lengths (the choice
  *                   of another layer, say); block_table, seq_lens, n_first and n_last are then not looked at (the first two may be NULL)
@@ -532,7 +533,8 @@ size_t pq_weights_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32
  *   weights_before  device fp32 [n_seqs][weights_stride], or NULL: 0 (decay == 0 does not read it either); may be `weights`
  *   weights         device fp32 [n_seqs][weights_stride], written for the pages that a sequence has, others are left as they were;
  *                   weights_stride >= ceil(max_seq_len / g)
- *   the others      as in pq_decode_attention (raw scores apart), `out` in its precision; weights are sums of fp32 exponentials
+ *   the others      as in pq_decode_attention (raw scores apart), `out` in its precision (with fp16 values bit for bit where the same kernels
+ *                   serve it: not the grouped quantizer with 1 or 2 query heads per KV head); weights are sums of fp32 exponentials
  *   workspace       >= pq_weights_workspace_bytes(...).  Calls that overlap need one each, captured ones too
  */
 int pq_decode_attention_weights(const pq_layout* layout, const void* q, pq_dtype q_dtype, int32_t n_seqs, int32_t n_q_heads,

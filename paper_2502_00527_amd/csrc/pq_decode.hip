@@ -599,7 +599,7 @@ int pq::attend_alike(const pq_layout* layout, const void* q, pq_dtype q_dtype, i
                      const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* seq_lens, int32_t max_seq_len, float sm_scale, float* out,
                      const void* residual_keys, void* workspace, hipStream_t stream) {
   const bool grouped = layout->angle_quantizer == PQ_ANGLE_GROUPED;
-  if (grouped && !grouped_on_matrix(layout, n_q_heads / layout->n_kv_heads))  // (whose chunks are whole rounds)
+  if (v_bits == 16 && grouped && !grouped_on_matrix(layout, n_q_heads / layout->n_kv_heads))   // (whose chunks are whole rounds)
     return pq_decode_attention(layout, q, q_dtype, n_seqs, n_q_heads, codes_pool, params_pool, v_pool, v_bits, v_params_pool, n_pool_pages, block_table,
                                max_pages_per_seq, seq_lens, max_seq_len, sm_scale, out, nullptr, 0, residual_keys, workspace,
                                pq_decode_workspace_bytes(layout, n_seqs, n_q_heads, max_seq_len), stream);
@@ -615,7 +615,9 @@ int pq::attend_alike(const pq_layout* layout, const void* q, pq_dtype q_dtype, i
   hipError_t e = hipSuccess;
   for (a.head0 = 0; a.head0 < a.group_total && e == hipSuccess; a.head0 += a.n_heads) {
     a.n_heads = std::min(a.group_total - a.head0, kMaxHeads);
-    if (grouped) launch_grouped(layout->r_bits * 10 + layout->t_bits, v_bits, a, grid, stream);
+    if (v_bits == 4) launch_weights_v4(layout, a, grid, stream);               // (centred: closer to float64, as fast)
+    else if (v_bits == 2) launch_weights_v2(layout, a, grid, stream);
+    else if (grouped) launch_grouped(layout->r_bits * 10 + layout->t_bits, v_bits, a, grid, stream);
     else launch_attention(layout->r_bits + layout->t_bits, v_bits, false, a, grid, stream);
     e = hipGetLastError();
   }

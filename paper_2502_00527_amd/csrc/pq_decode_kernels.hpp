@@ -93,7 +93,7 @@ struct DecodeArgs {
   float sin_tab[kMaxAngleBins];
   int32_t window;           // pq_window_attention: tokens of the window, and the sinks
   int32_t n_sinks;
-  float2* page_ml;          // pq_decode_attention_weights: [seq][q_head][page_stride] (m, l) of each page ...
+  float2* page_ml;          // pq_decode_attention_weights: [seq][q_head][page_stride] (m, l) of each page, or null ...
   float2* totals;           // ... and of all, [seq][q_head]
   int32_t page_stride;
 };

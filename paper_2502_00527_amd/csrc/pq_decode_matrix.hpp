@@ -949,13 +949,23 @@ __device__ __forceinline__ void priority_of_rest(int left, int all) {
 // code was masked in place as an fp16 denormal, code * 2^(position - 24).  Fields are moved up to
 // bits 4 .. 9 first: the matrix unit aligns products by their operands' exponent fields, and the
 // low bits of products with denormals further down are lost (measured: 2e-4 of the output with
-// fields at bit 0, 1e-6 at bits 4 and up).
-template <int VB>
+// fields at bit 0, 1e-6 at bits 4 and up).  kCentred: up to the highest bits that all of them reach.
+template <int VB, bool kCentred>
 __device__ __forceinline__ constexpr float code_unscale(int k) {
   constexpr int kAt2[8] = {4, 6, 8, 6, 8, 4, 6, 8};
-  const int at = VB == 4 ? ((k & 3) == 1 ? 4 : 6) : kAt2[k];
+  const int at = kCentred ? (VB == 4 ? 6 : 8) : (VB == 4 ? ((k & 3) == 1 ? 4 : 6) : kAt2[k]);
   return static_cast<float>(1 << (24 - at));
 }
+
+// Codes about their middle.  code * s is up to the values' range and z minus as much of it, so that their sums over many tokens, far larger than
+// the output, take its last bits with them.  kCentred: (code - middle) * s and z + middle * s, the middle's part being one more
+// product for each of the codes', with an operand of this constant.  Errors against float64 (2-norm, 20000 tokens of 4-bit values) 3.2e-6 -> 0.9e-6, of
+// 2-bit ones too, 5 - 6 % of each kernel's instructions: 8 x 20000 tokens 51.0 -> 53.0 us, 8 x 16 chosen pages 17.5 -> 17.7.  (The correction a page at once, by 4
+// products and 32 additions: 52.5 us, 1.05e-6; fields left at bits 4 and 6: 52.5, 1.03e-6.)
+template <int VB>
+constexpr float kCodeMiddle = VB == 4 ? 7.5f : 1.5f;
+template <int VB>
+constexpr uint32_t kLessMiddle = 0x80008000u | (static_cast<uint32_t>(kCodeMiddle<VB> * (VB == 4 ? 64 : 256)) * 0x00010001u);   // at code_unscale's bits
 
 // Stores a page's raw scores, left by a walk in plain token order and folded, for the heads from row `first_head` of a.scores
 // on: the lane's tokens 4 row .. + 3 of its batches, of one head.  Tokens from nv on are not stored.
@@ -1046,12 +1056,13 @@ __device__ __forceinline__ void grouped_scores_body(const DecodeArgs& a) {
 // kCut: the chunks are cut on the device (a.cut_places > 0).  kMatWaves: wavefronts of the work-group, 4 or 8.
 // kGroupedRadius: 0 on the uniform grid; with the grouped angle quantizer the radius bits (queries of either type are
 // taken as fp32 there, so that Q32 is true).  kWindow: through a sliding window with sinks (WindowView; the launch is cut on the host).
-// kWeights: each page's sum of exponentials and the maximum it was taken against go to a.page_ml, those of all pages to a.totals.
+// kWeights: each page's sum of exponentials and the maximum it was taken against go to a.page_ml, those of all pages to a.totals (unless they
+// are null); quantized values are centred.
 template <int W, int VB, int NH, bool Q32, bool kCut, int kMatWaves, int kGroupedRadius = 0, bool kWindow = false, bool kWeights = false>
 __device__ __forceinline__ void attention_body(const DecodeArgs& a) {
   constexpr int UB = 2 * W;
   constexpr int kMatThreads = kMatWaves * 64;
-  constexpr bool kQuantV = VB != 16;
+  constexpr bool kQuantV = VB != 16, kCentred = kQuantV && kWeights;
   constexpr bool kGrouped = kGroupedRadius != 0;
   static_assert(!kGrouped || (Q32 && kMatWaves == 4), "what the grouped quantizer's kernels are");
   static_assert(!kWindow || !kCut, "the cut on the device goes by the whole lengths");
@@ -1364,6 +1375,7 @@ __device__ __forceinline__ void attention_body(const DecodeArgs& a) {
     const f32x2 part = split_part<kUp>(lane_now() & 8);
     uint32_t p_op[8][2];                                               // batch t: fp16 pairs of tokens 4 row + (0, 1), (2, 3)
     [[maybe_unused]] float l_page = 0.f;
+    [[maybe_unused]] const float middle = kCentred && (lane_now() & 8) ? __builtin_ldexpf(kCodeMiddle<VB>, -s_exp) : 0.f;
 #pragma unroll
     for (int t = 0; t < kOwn; ++t) {
       float p[4];
@@ -1378,6 +1390,7 @@ __device__ __forceinline__ void attention_body(const DecodeArgs& a) {
           const f16x2 sz = u2h(vp[i]);
           lz_run = fmaf(p[i], static_cast<float>(sz.y), lz_run);
           p[i] = fmaf(p[i], static_cast<float>(sz.x), 0.f);
+          if constexpr (kCentred) lz_run = fmaf(p[i], middle, lz_run);
         }
       }
       if constexpr (!kQuantV) {
@@ -1401,10 +1414,15 @@ __device__ __forceinline__ void attention_body(const DecodeArgs& a) {
       l_page = sum_rows(l_page);
       if constexpr (NH == 4) l_page += dpp_of<0x12c>(l_page);          // the other half's batches
       const int h = lane_now();
-      if (h < a.n_heads) a.page_ml[(first_head + h) * a.page_stride + pi] = make_float2(m_run, l_page);
+      if (a.page_ml != nullptr && h < a.n_heads) a.page_ml[(first_head + h) * a.page_stride + pi] = make_float2(m_run, l_page);
     }
 
     // ---- values: acc += P^T V, 32 tokens (batches 2g, 2g + 1) per instruction ----
+    auto less_middle = [&](f16x8 weights, f32x4 sum) -> f32x4 {
+      if constexpr (!kCentred) return sum;
+      constexpr uint32_t m = kLessMiddle<VB>;
+      return __builtin_amdgcn_mfma_f32_16x16x32_f16(weights, as_operand(m, m, m, m), sum, 0, 0, 0);
+    };
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       if (g == 1) prepare_page(lane_now());
@@ -1442,8 +1460,9 @@ __device__ __forceinline__ void attention_body(const DecodeArgs& a) {
             uint32_t f[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-              f[j] = (k == 0 ? x[j] << 6 : (k == 1 ? x[j] : x[j] >> (4 * k - 6))) & (k == 1 ? 0x00f000f0u : 0x03c003c0u);
-            acc[4 * dh + k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pa, as_operand(f[0], f[1], f[2], f[3]), acc[4 * dh + k], 0, 0, 0);
+              if constexpr (kCentred) f[j] = (k < 2 ? x[j] << (6 - 4 * k) : x[j] >> (4 * k - 6)) & 0x03c003c0u;
+              else f[j] = (k == 0 ? x[j] << 6 : (k == 1 ? x[j] : x[j] >> (4 * k - 6))) & (k == 1 ? 0x00f000f0u : 0x03c003c0u);
+            acc[4 * dh + k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pa, as_operand(f[0], f[1], f[2], f[3]), less_middle(pa, acc[4 * dh + k]), 0, 0, 0);
           }
         }
         vq[2 * g] = buf_load16<kAuxStream>(rv_nxt, voff_values, (2 * g) * 1024);
@@ -1459,8 +1478,10 @@ __device__ __forceinline__ void attention_body(const DecodeArgs& a) {
                                          0x03000300u, 0x00300030u, 0x00c000c0u, 0x03000300u};
           uint32_t f[4];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) f[j] = (k < 3 ? x[j] << 4 : (k < 5 ? x[j] : x[j] >> 6)) & kMask[k];
-          acc[k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pa, as_operand(f[0], f[1], f[2], f[3]), acc[k], 0, 0, 0);
+          for (int j = 0; j < 4; ++j)
+            if constexpr (kCentred) f[j] = (k < 5 ? x[j] << (8 - 2 * k) : x[j] >> (2 * k - 8)) & 0x03000300u;
+            else f[j] = (k < 3 ? x[j] << 4 : (k < 5 ? x[j] : x[j] >> 6)) & kMask[k];
+          acc[k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pa, as_operand(f[0], f[1], f[2], f[3]), less_middle(pa, acc[k]), 0, 0, 0);
         }
         vq[g] = buf_load16<kAuxStream>(rv_nxt, voff_values, g * 1024);
         __builtin_amdgcn_sched_barrier(0);
@@ -1513,7 +1534,7 @@ __device__ __forceinline__ void attention_body(const DecodeArgs& a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         acc[e][i] = sum_parts(acc[e][i] * back, acc[4 + e][i] * back) * wgt[i];
-        if constexpr (kQuantV) acc[e][i] *= row < 2 ? code_unscale<VB>(e) : code_unscale<VB>(4 + e);
+        if constexpr (kQuantV) acc[e][i] *= row < 2 ? code_unscale<VB, kCentred>(e) : code_unscale<VB, kCentred>(4 + e);
       }
     if ((row & 1) < NH / 4) {
 #pragma unroll

@@ -85,7 +85,7 @@ constexpr int kFinishLdsFloats = kFinishThreads * 5;
 // arrival is registered -- not by fences, which write back and invalidate whole caches (measured:
 // with fences in every work-group the launch takes twice as long).
 // The unit's partials: head h (from a.head0 on), chunk c in row row0 + h * stride + c.
-// kWeights: a unit that is finished here leaves its heads' maxima and sums in a.totals.
+// kWeights: a unit that is finished here leaves its heads' maxima and sums in a.totals, if there is such an array.
 template <int NH, bool kWeights = false, typename Partial>
 __device__ __forceinline__ void finish_chunk(const DecodeArgs& a, int seq, int kvh, int chunk, int n_chunks_seq, int64_t row0,
                                              int stride, int tid, Partial partial, float* lent, int* stage) {
@@ -101,7 +101,7 @@ __device__ __forceinline__ void finish_chunk(const DecodeArgs& a, int seq, int k
       const float inv = l > 0.f ? 1.f / l : 0.f;
       reinterpret_cast<float4*>(out_rows)[tid] = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
       if constexpr (kWeights) {
-        if (quad == 0) a.totals[head_row + h] = make_float2(M, l);
+        if (quad == 0 && a.totals != nullptr) a.totals[head_row + h] = make_float2(M, l);
       }
     }
     return;
@@ -183,7 +183,7 @@ __device__ __forceinline__ void finish_chunk(const DecodeArgs& a, int seq, int k
     const float inv = lt > 0.f ? 1.f / lt : 0.f;
     reinterpret_cast<float4*>(out_rows)[ch * 32 + quad] = make_float4(r.x * inv, r.y * inv, r.z * inv, r.w * inv);
     if constexpr (kWeights) {
-      if (quad == 0) a.totals[head_row + ch] = make_float2(m, lt);
+      if (quad == 0 && a.totals != nullptr) a.totals[head_row + ch] = make_float2(m, lt);
     }
   }
   if (tid == 0) reset_arrivals(word);

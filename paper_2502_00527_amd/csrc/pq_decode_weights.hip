@@ -1,5 +1,6 @@
 // Decode attention that leaves each page's sum of exponentials beside its output (pq_decode_attention_weights): the kernels of
-// pq_decode_matrix.hpp with kWeights, and their launch ladder.  The grouped quantizer's walk serves one and two query heads per KV head, too.
+// pq_decode_matrix.hpp with kWeights, and their launch ladder.  The grouped quantizer's walk serves one and two query heads per KV head, too.  Attention over chosen pages
+// with quantized values goes through them without the sums.
 //
 // This file is the fp16-value kernels; pq_decode_weights_v4.hip and pq_decode_weights_v2.hip compile it again for 4-bit and
 // 2-bit values.

@@ -337,6 +337,36 @@ def test_sparse_every_number(n_selected, n_first, n_last, grouped):
     _check_sparse(Cache([6000, 3000, 900], 2, (4, 4), grouped), _queries(3, 8, 4), n_selected, n_first, n_last, max_seq_len=47 * G)
 
 
+@pytest.mark.parametrize("group", [1, 2, 3, 7, 12])
+@pytest.mark.parametrize("grouped", [False, True])
+@pytest.mark.parametrize("v_bits", [4, 2])
+def test_sparse_every_group_with_quantized_values(group, grouped, v_bits):
+    _check_sparse(Cache([1500, 1, 0, 1281, 128], 2, (4, 4), grouped, v_bits), _queries(5, 2 * group, 4), 5, 1, 2)
+
+
+@pytest.mark.parametrize("bits,grouped", [((4, 4), False), ((3, 3), False), ((4, 4), True)])
+@pytest.mark.parametrize("v_bits", [4, 2])
+@pytest.mark.parametrize("lens", [[53] * 4, [5000, 3000], [20000]])
+def test_quantized_values_are_summed_as_precisely_as_in_fp32(bits, grouped, v_bits, lens):
+    """No further from float64 than attention over the values and keys in fp32, by torch: both round as often as there are tokens; twice for another order."""
+    c = Cache(lens, 2, bits, grouped, v_bits)
+    q = _queries(len(lens), 8, 3)
+    pools = _bound(c)
+    outs = [_weigh(c, q)[0], _sparse(c, q, pools, 200)[0]]
+    off, plain = np.zeros(2), 0.0
+    for s in range(len(lens)):
+        for h in range(8):
+            def attend(k, v, x):
+                w = torch.softmax((k * x).sum(-1) * c.sm_scale, 0)
+                return (w[:, None] * v).sum(0)
+            k, v = c.k64[s][:, h // 4], c.v64[s][:, h // 4]
+            want = attend(k, v, q[s, h].double())
+            size = float(want.norm()) ** 2
+            plain += float((attend(k.float(), v.float(), q[s, h].float()).double() - want).norm()) ** 2 / size
+            off += [float((o[s, h].double() - want).norm()) ** 2 / size for o in outs]
+    assert (np.sqrt(off) <= 2 * np.sqrt(plain)).all(), (np.sqrt(off), np.sqrt(plain))
+
+
 def test_sparse_of_many_sequences():
     rng = np.random.default_rng(2)
     _check_sparse(Cache([int(n) for n in rng.integers(1, 1200, 70)], 4, (3, 3), v_bits=4), _queries(70, 16, 4), 3)
@@ -418,8 +448,8 @@ def _decode(c, q):
 
 def _check_weights(c, q, **more):
     out, weights = _weigh(c, q, **more)
-    # (the grouped quantizer has another kernel for one and two heads)
-    same = c.layout.angle_quantizer == 0 or q.shape[1] // c.heads > 2
+    # (the grouped quantizer has another kernel for one and two heads; quantized values are summed about the middle of their codes here)
+    same = c.v_bits == 16 and (c.layout.angle_quantizer == 0 or q.shape[1] // c.heads > 2)
     assert not same or torch.equal(out, _decode(c, q)), "not the output of decode attention"
     for s, L in enumerate(c.lens):
         pages = (L + G - 1) // G
