@@ -588,10 +588,10 @@ extern "C" int pq_window_attention(const pq_layout* layout, const void* q, pq_dt
 // Chunks as for a window: sequences are alike, as many chunks as start at once (the general plan makes chunks of 8 or 16 pages: 128 units of 48 pages are
 // then 384 work-groups, 46.8 us; in fours of 12 pages 512, 44.3).
 size_t pq::alike_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_t n_q_heads, int32_t max_seq_len) {
-  const size_t general = pq_decode_workspace_bytes(layout, n_seqs, n_q_heads, max_seq_len);
+  if (check_decode_shape(layout, n_seqs, n_q_heads, max_seq_len) != PQ_OK) return 0;
   const ChunkPlan plan = plan_window(layout, n_seqs, max_seq_len);
-  if (general == 0 || plan.n_chunks > 65535) return 0;                         // grid.z
-  return std::max(general, carve_window_workspace(nullptr, layout, n_seqs, n_q_heads, plan).bytes);
+  if (plan.n_chunks > 65535) return 0;                       // grid.z
+  return carve_window_workspace(nullptr, layout, n_seqs, n_q_heads, plan).bytes;
 }
 
 int pq::attend_alike(const pq_layout* layout, const void* q, pq_dtype q_dtype, int32_t n_seqs, int32_t n_q_heads, const void* codes_pool,
@@ -599,10 +599,6 @@ int pq::attend_alike(const pq_layout* layout, const void* q, pq_dtype q_dtype, i
                      const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* seq_lens, int32_t max_seq_len, float sm_scale, float* out,
                      const void* residual_keys, void* workspace, hipStream_t stream) {
   const bool grouped = layout->angle_quantizer == PQ_ANGLE_GROUPED;
-  if (v_bits == 16 && grouped && !grouped_on_matrix(layout, n_q_heads / layout->n_kv_heads))   // (whose chunks are whole rounds)
-    return pq_decode_attention(layout, q, q_dtype, n_seqs, n_q_heads, codes_pool, params_pool, v_pool, v_bits, v_params_pool, n_pool_pages, block_table,
-                               max_pages_per_seq, seq_lens, max_seq_len, sm_scale, out, nullptr, 0, residual_keys, workspace,
-                               pq_decode_workspace_bytes(layout, n_seqs, n_q_heads, max_seq_len), stream);
   const ChunkPlan plan = plan_window(layout, n_seqs, max_seq_len);
   const Workspace ws = carve_window_workspace(workspace, layout, n_seqs, n_q_heads, plan);
   DecodeArgs a = attention_args(layout, q, q_dtype, n_seqs, n_q_heads, codes_pool, params_pool, v_pool, v_params_pool, n_pool_pages, block_table,
@@ -615,8 +611,11 @@ int pq::attend_alike(const pq_layout* layout, const void* q, pq_dtype q_dtype, i
   hipError_t e = hipSuccess;
   for (a.head0 = 0; a.head0 < a.group_total && e == hipSuccess; a.head0 += a.n_heads) {
     a.n_heads = std::min(a.group_total - a.head0, kMaxHeads);
-    if (v_bits == 4) launch_weights_v4(layout, a, grid, stream);               // (centred: closer to float64, as fast)
+    // quantized values centred (closer to float64, as fast); the grouped quantizer with one or two heads on the matrix units (16 x 48 pages 57 us, on
+    // the vector unit 67 and 71; 8 pages of one sequence 20.1, there 18.7)
+    if (v_bits == 4) launch_weights_v4(layout, a, grid, stream);
     else if (v_bits == 2) launch_weights_v2(layout, a, grid, stream);
+    else if (grouped && !grouped_on_matrix(layout, a.group_total)) launch_weights_v16(layout, a, grid, stream);
     else if (grouped) launch_grouped(layout->r_bits * 10 + layout->t_bits, v_bits, a, grid, stream);
     else launch_attention(layout->r_bits + layout->t_bits, v_bits, false, a, grid, stream);
     e = hipGetLastError();

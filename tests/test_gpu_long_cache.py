@@ -367,6 +367,23 @@ def test_quantized_values_are_summed_as_precisely_as_in_fp32(bits, grouped, v_bi
     assert (np.sqrt(off) <= 2 * np.sqrt(plain)).all(), (np.sqrt(off), np.sqrt(plain))
 
 
+@pytest.mark.parametrize("grouped,group,v_bits", [(False, 4, 16), (True, 1, 16), (True, 4, 16), (False, 4, 4)])
+def test_sparse_of_many_long_choices(grouped, group, v_bits):
+    """More units than work-groups run at once: hundreds of chosen pages in one chunk.  256 sequences that are the same."""
+    c = Cache([640 * G - 5], 2, (4, 4), grouped, v_bits)
+    q = _queries(1, 2 * group, 3)
+    pools = _bound(c)
+    want, spread, slope = (x[0] for x in c.rows(0, q, [c.lens[0] - 1]))
+    bar = ref.output_bar(spread, slope, want, ref.page_weights(c, 0, q[0])[1]) if v_bits == 16 else 2.4e-5
+    one, selected, lens = _sparse(c, q, pools, 640)
+    c.residual = c.residual.expand(256, -1, -1, -1).contiguous()
+    c.block_table, c.seq_lens = c.block_table.expand(256, -1).contiguous(), c.seq_lens.expand(256).contiguous()
+    out, all_selected, all_lens = _sparse(c, q.expand(256, -1, -1).contiguous(), pools, 640)
+    assert bool((out == out[:1]).all()) and bool((all_selected == selected).all()) and bool((all_lens == lens).all())
+    for got in (one[0], out[0]):
+        assert float((got.double() - want).norm() / want.norm()) <= bar
+
+
 def test_sparse_of_many_sequences():
     rng = np.random.default_rng(2)
     _check_sparse(Cache([int(n) for n in rng.integers(1, 1200, 70)], 4, (3, 3), v_bits=4), _queries(70, 16, 4), 3)
