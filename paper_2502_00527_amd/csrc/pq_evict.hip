@@ -4,7 +4,8 @@
 // pages by summing over the sequences before it: one launch, nobody waits for anybody.  Which ones is a choice of the k largest keys
 // (pq_rank.hpp), the keys being the weights' upside down.
 //
-// One work-group a sequence.  Bound: a launch's own time; 16 bytes a page are read and written.
+// One work-group a sequence.  Bound: a launch's own time, 3.6 us, and four waits of the work-group; 16 bytes a page are read and written.  64 sequences of 100
+// pages 5.6 us, 48 of up to 1024 5.8; one of 8192 pages, which read their weights again each time, 30.
 #include <hip/hip_runtime.h>
 
 #include "pq_decode_sched.hpp"
