@@ -5,7 +5,7 @@
 // (pq_rank.hpp), the keys being the weights' upside down.
 //
 // One work-group a sequence.  Bound: a launch's own time, 3.6 us, and four waits of the work-group; 16 bytes a page are read and written.  64 sequences of 100
-// pages 5.6 us, 48 of up to 1024 5.8; one of 8192 pages, which read their weights again each time, 30.
+// pages 5.6 us, 48 of up to 1024 5.8; one of 8192 pages, which read their weights again each time, 25 (one by one 30).
 #include <hip/hip_runtime.h>
 
 #include "pq_decode_sched.hpp"
@@ -79,7 +79,15 @@ __global__ __launch_bounds__(kRankThreads) void pq_evict_kernel(const EvictArgs 
       const int p = tid * kKeysPerThread + j;
       if (p >= begin && p < end) f(first_key[j]);
     }
-    for (int p = max(begin, kRankRound) + tid; p < end; p += kRankThreads) f(key_of_weight(a.weights[weight_row + p]));
+    constexpr int kAtOnce = 8;                               // loads that are under way together
+    for (int p0 = max(begin, kRankRound) + tid; p0 < end; p0 += kAtOnce * kRankThreads) {
+      float w[kAtOnce];
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) w[j] = p0 + j * kRankThreads < end ? a.weights[weight_row + p0 + j * kRankThreads] : 0.f;
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j)
+        if (p0 + j * kRankThreads < end) f(key_of_weight(w[j]));
+    }
   };
   const Threshold t = find_threshold(rank, end - begin, static_cast<uint32_t>(k.gone), each, tid);
   before = (sums[0] + sums[1]) + (sums[2] + sums[3]);
