@@ -960,7 +960,7 @@ __device__ __forceinline__ constexpr float code_unscale(int k) {
 // Codes about their middle.  code * s is up to the values' range and z minus as much of it, so that their sums over many tokens, far larger than
 // the output, take its last bits with them.  kCentred: (code - middle) * s and z + middle * s, the middle's part being one more
 // product for each of the codes', with an operand of this constant.  Errors against float64 (2-norm, 20000 tokens of 4-bit values) 3.2e-6 -> 0.9e-6, of
-// 2-bit ones too, 5 - 6 % of each kernel's instructions: 8 x 20000 tokens 51.0 -> 53.0 us, 8 x 16 chosen pages 17.5 -> 17.7.  (The correction a page at once, by 4
+// 2-bit ones too, 7 % more vector instructions: 8 x 20000 tokens 51.0 -> 53.0 us, 8 x 16 chosen pages 17.5 -> 17.7.  (The correction a page at once, by 4
 // products and 32 additions: 52.5 us, 1.05e-6; fields left at bits 4 and 6: 52.5, 1.03e-6.)
 template <int VB>
 constexpr float kCodeMiddle = VB == 4 ? 7.5f : 1.5f;
