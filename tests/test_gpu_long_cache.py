@@ -772,14 +772,17 @@ def test_a_serving_loop_under_a_budget(grouped):
     assert len(held) + len(loop.free) == 26
 
 
-def test_captured_steps():
-    """All five calls in one graph, replayed with other queries and lengths between, each replay against the eager calls."""
-    c = Cache([1500, 515, 60, 1408], 2)
-    pq, q = c.pq, _queries(4, 8, 3)
+@pytest.mark.parametrize("lens,heads,v_bits", [([1500, 515, 60, 1408], 2, 16), ([40000, 9000, 300, 12000], 8, 16), ([40000, 9000, 300, 12000], 8, 4)])
+def test_captured_steps(lens, heads, v_bits):
+    """All five calls in one graph, replayed with other queries and lengths between, each replay against the eager calls: one work-group a unit, and units shared
+    among work-groups, chunks cut on the device and merged in the kernel."""
+    c = Cache(lens, heads, v_bits=v_bits)
+    pq, n_q = c.pq, 4 * heads
+    q = _queries(4, n_q, 3)
     bounds, scales = _bound_pools(c)
-    work = torch.empty(pq.pq_sparse_workspace_bytes(c.layout, 4, 8, c.max_seq_len, 4), dtype=torch.uint8, device=DEV)
-    work2 = torch.empty(pq.pq_weights_workspace_bytes(c.layout, 4, 8, c.max_seq_len), dtype=torch.uint8, device=DEV)
-    selected, sel_lens = torch.zeros((4, 2, 4), dtype=torch.int32, device=DEV), torch.zeros((4, 2), dtype=torch.int32, device=DEV)
+    work = torch.empty(pq.pq_sparse_workspace_bytes(c.layout, 4, n_q, c.max_seq_len, 4), dtype=torch.uint8, device=DEV)
+    work2 = torch.empty(pq.pq_weights_workspace_bytes(c.layout, 4, n_q, c.max_seq_len), dtype=torch.uint8, device=DEV)
+    selected, sel_lens = torch.zeros((4, heads, 4), dtype=torch.int32, device=DEV), torch.zeros((4, heads), dtype=torch.int32, device=DEV)
     out, out2 = torch.zeros(q.shape, device=DEV), torch.zeros(q.shape, device=DEV)
     width = c.block_table.shape[1]
     weights, after_w = torch.zeros((4, width), device=DEV), torch.zeros((4, width), device=DEV)
@@ -789,9 +792,9 @@ def test_captured_steps():
     def step():
         pq.pq_bound_pages(c.layout, c.codes, c.params, c.block_table, None, c.seq_lens, c.max_seq_len, bounds, scales)
         pq.pq_sparse_attention(c.layout, q, c.codes, c.params, c.v_pool, bounds, scales, c.block_table, c.seq_lens, c.max_seq_len, 1, 1, float(c.sm_scale),
-                               selected, sel_lens, out, work, c.residual)
+                               selected, sel_lens, out, work, c.residual, c.v_bits, c.v_params)
         pq.pq_decode_attention_weights(c.layout, q, c.codes, c.params, c.v_pool, c.block_table, c.seq_lens, c.max_seq_len, float(c.sm_scale), out2, weights, work2,
-                                       None, 1.0, c.residual)
+                                       None, 1.0, c.residual, c.v_bits, c.v_params)
         pq.pq_evict_pages(c.layout, c.block_table, c.seq_lens, weights, 5, 1, 1, after_t, after_l, after_w, freed, counts)
         return [x.clone() for x in (bounds, scales, selected, sel_lens, out, out2, weights, after_t, after_l, after_w, freed, counts)]
 
@@ -800,9 +803,8 @@ def test_captured_steps():
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         captured = step()
-    lens = [c.lens, [1000, 515, 0, 1281], [129, 500, 60, 640], c.lens]
-    for i, now in enumerate(lens):
-        q.copy_(_queries(4, 8, 50 + i))
+    for i, now in enumerate([c.lens, [1000, 515, 0, 1281], [lens[0] - 371, 500, 60, 640], c.lens]):
+        q.copy_(_queries(4, n_q, 50 + i))
         c.seq_lens.copy_(_ints(now))
         graph.replay()
         torch.cuda.synchronize()
