@@ -13,7 +13,10 @@
 // arrival word makes the choice (pq_decode_sched.hpp): one launch, nobody waits for anybody.
 //
 // Bound: waits for memory and for one another, one after the other -- table, bounds, keys of the other work-groups, counts.  One sequence of 1024 pages (8 KV
-// heads) 8.0 us, 32 ragged ones of up to 256 7.1, a launch's own time being 3.6; 32 of 1024 pages, 72 MB, 21.6.
+// heads) 8.0 us, 32 ragged ones of up to 256 6.7, a launch's own time being 3.6; 32 of 1024 pages, 72 MB, 22.
+//
+// The grid runs over sequences first: work-groups of one sequence then tend to start on the same of the 8 dies, whose caches keep lines that its heads share, the
+// block table's and the scales' (16 bytes a head).  64 sequences of 256 pages 12.0 -> 10.3 us, 16 of 1024 14.5 -> 12.5, 32 ragged ones of up to 256 7.3 -> 6.7.
 //
 // A choice is a row of a block table: page and KV head are one index into the pools taken head by head, so that attention over the
 // chosen pages is decode attention of n_seqs * n_kv_heads sequences with one KV head each.
@@ -183,7 +186,7 @@ __global__ __launch_bounds__(kRankThreads) void pq_select_kernel(const SelectArg
   __shared__ RankShared rank;
   __shared__ __attribute__((aligned(16))) uint32_t in_lds[kKeys == 1 ? 4 : kMostKeys];
   __shared__ int stage;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kvh = blockIdx.x, seq = blockIdx.y, part = blockIdx.z;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kvh = blockIdx.y, seq = blockIdx.x, part = blockIdx.z;
   const int64_t unit = static_cast<int64_t>(seq) * a.n_kv_heads + kvh;
   const int32_t* const row = a.block_table + static_cast<int64_t>(seq) * a.max_pages_per_seq;
   int32_t* const out = a.selected + unit * a.n_selected;
@@ -301,7 +304,8 @@ void launch_select(const SelectArgs& a, dim3 grid, hipStream_t st) {
 int64_t most_pages(int32_t max_seq_len) { return (static_cast<int64_t>(max_seq_len) + kGroup - 1) / kGroup; }
 
 // Pages of a work-group: all of a unit's, if that is one batch of loads a wavefront or the units fill the compute units; otherwise as few as make
-// no more than a work-group a compute unit, or a batch.  (8 units of 1024 pages 8.2 us, a work-group each 15.6; 128 of 512 10.5 and 11.5; 256 of 512 14.3 and 13.6.
+// no more than a work-group a compute unit, or a batch.  (8 units of 1024 pages 8.2 us, a work-group each 15.6; 128 of 512 10.5 and 11.5; 256 of 512 12.3 and 12.4, of 1024 21.7 and 22.0; 512 of 512 22.1
+// and 20.7, 1024 of 312 29.0 and 25.8.
 // With twice as many work-groups 32 units of 1024 pages 10.7 instead of 9.3.)
 int32_t pages_of_part(const pq_layout* l, int32_t n_seqs, int32_t max_seq_len) {
   const int64_t pages = most_pages(max_seq_len), units = static_cast<int64_t>(n_seqs) * l->n_kv_heads;
@@ -373,7 +377,7 @@ int launch_selection(const pq_layout* l, const void* q, pq_dtype q_dtype, int32_
   a.q_is_f32 = q_dtype == PQ_F32 ? 1 : 0;
   a.key_stride = static_cast<int32_t>(key_stride(max_seq_len));
   a.part_pages = pages_of_part(l, n_seqs, max_seq_len);
-  const dim3 grid(l->n_kv_heads, n_seqs, (a.max_pages + a.part_pages - 1) / a.part_pages);
+  const dim3 grid(n_seqs, l->n_kv_heads, (a.max_pages + a.part_pages - 1) / a.part_pages);
   if (a.max_pages <= kBatchPages) launch_select<kTilesAtOnce, 1>(a, grid, st);
   else if (a.part_pages == kBatchPages / 4) launch_select<1, 4>(a, grid, st);
   else if (a.part_pages == kBatchPages / 2) launch_select<2, 4>(a, grid, st);
