@@ -434,9 +434,10 @@ extern "C" int pq_sparse_attention(const pq_layout* layout, const void* q, pq_dt
                                    int32_t* selected, int32_t* selected_lens, float* out, const void* residual_keys, void* workspace,
                                    size_t workspace_bytes, void* hip_stream) {
   if (!out || (reinterpret_cast<uintptr_t>(out) & 15u)) return PQ_ERR_INVALID_ARG;
-  int st = check_selection(layout, n_seqs, n_q_heads, max_seq_len, n_selected, n_first, n_last);
+  // a choice that is given needs neither bounds nor the table, lengths are its own, and which pages were sure to be in it is of no account
   const bool given = !bounds && !bound_scales;
-  if (st == PQ_OK)                                           // (a choice that is given needs neither bounds nor the table, lengths are its own)
+  int st = check_selection(layout, n_seqs, n_q_heads, max_seq_len, n_selected, given ? 0 : n_first, given ? 1 : n_last);
+  if (st == PQ_OK)
     st = check_selection_pointers(layout, q, q_dtype, given ? q : bounds, given ? q : bound_scales, n_pool_pages, given ? selected : block_table,
                                   given ? INT32_MAX : max_pages_per_seq, given ? selected_lens : seq_lens, max_seq_len, selected, selected_lens);
   if (st != PQ_OK) return st;

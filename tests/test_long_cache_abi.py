@@ -124,3 +124,12 @@ def test_sizes(lib):
     assert pq.pq_sparse_workspace_bytes(LAY, 2, 32, 1024, 0) == 0 and pq.pq_sparse_workspace_bytes(LAY, 2, 12, 1024, 4) == 0
     assert pq.pq_weights_workspace_bytes(LAY, 2, 12, 1024) == 0
     assert pq.pq_weights_workspace_bytes(LAY, 2, 32, 1024) >= pq.pq_decode_workspace_bytes(LAY, 2, 32, 1024) + 2 * 32 * 8 * 8
+
+
+@pytest.mark.parametrize("first,last", [(0, 0), (1, 1), (4, 1), (0, 5), (-1, 1), (3, -7), (2 ** 31 - 1, 2 ** 31 - 1)])
+def test_a_given_choice_has_no_first_and_last_pages(lib, first, last):
+    """bounds and bound_scales NULL: n_first, n_last, the table and the lengths are not looked at -- the call gets as far as its workspace --, the rest is."""
+    given = dict(bounds=NULL, scales=NULL, table=NULL, lens=NULL, width=0, first=first, last=last)
+    assert _call(lib, "pq_sparse_attention", SPARSE, **given) == WORKSPACE
+    for change in (dict(chosen=0), dict(selected=NULL), dict(selected_lens=NULL), dict(selected=ODD), dict(q=NULL), dict(heads=12), dict(max_seq_len=0), dict(out=NULL)):
+        assert _call(lib, "pq_sparse_attention", SPARSE, **{**given, **change}) == INVALID
