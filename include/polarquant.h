@@ -124,7 +124,8 @@ size_t pq_vq_bytes_per_page(const pq_layout* layout, int32_t v_bits);
 size_t pq_vq_params_bytes_per_page(const pq_layout* layout);
 
 /* Bytes of scratch pq_decode_attention needs for n_seqs sequences of at most
- * max_seq_len tokens (256-byte aligned device memory); 0 on invalid arguments. */
+ * max_seq_len tokens (256-byte aligned device memory); 0 on invalid arguments.  Of this shape: a smaller batch, cut
+ * into more chunks, may need more. */
 size_t pq_decode_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_t n_q_heads,
                                  int32_t max_seq_len);
 
@@ -424,7 +425,7 @@ int pq_chunk_attention(const pq_layout* layout, const void* q, pq_dtype q_dtype,
                        int32_t max_seq_len, int32_t window, int32_t n_sinks, float sm_scale, void* out,
                        const void* residual_keys, void* workspace, size_t workspace_bytes, void* hip_stream);
 
-/* Bytes of scratch pq_window_attention needs (256-byte aligned device memory); 0 on invalid arguments. */
+/* Bytes of scratch pq_window_attention needs (256-byte aligned device memory); 0 on invalid arguments.  Of this shape, as pq_decode_workspace_bytes. */
 size_t pq_window_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_t n_q_heads, int32_t max_seq_len,
                                  int32_t window, int32_t n_sinks);
 
@@ -476,7 +477,7 @@ int pq_bound_pages(const pq_layout* layout, const void* codes_pool, const void* 
                    const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* lens_before, const int32_t* lens_after,
                    int32_t n_seqs, int32_t max_new_tokens, void* bounds, void* bound_scales, void* hip_stream);
 
-/* Bytes of scratch pq_select_pages needs (256-byte aligned device memory); 0 on invalid arguments. */
+/* Bytes of scratch pq_select_pages needs (256-byte aligned device memory), for any smaller n_seqs and max_seq_len, too; 0 on invalid arguments. */
 size_t pq_select_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_t max_seq_len);
 
 /*
@@ -503,7 +504,7 @@ int pq_select_pages(const pq_layout* layout, const void* q, pq_dtype q_dtype, in
                     const int32_t* seq_lens, int32_t max_seq_len, int32_t n_selected, int32_t n_first, int32_t n_last,
                     int32_t* selected, int32_t* selected_lens, void* workspace, size_t workspace_bytes, void* hip_stream);
 
-/* Bytes of scratch pq_sparse_attention needs (256-byte aligned device memory); 0 on invalid arguments. */
+/* Bytes of scratch pq_sparse_attention needs (256-byte aligned device memory), for any smaller n_seqs, max_seq_len and n_selected, too; 0 on invalid arguments. */
 size_t pq_sparse_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_t n_q_heads, int32_t max_seq_len, int32_t n_selected);
 
 /*
@@ -522,7 +523,7 @@ int pq_sparse_attention(const pq_layout* layout, const void* q, pq_dtype q_dtype
                         int32_t* selected, int32_t* selected_lens, float* out, const void* residual_keys, void* workspace,
                         size_t workspace_bytes, void* hip_stream);
 
-/* Bytes of scratch pq_decode_attention_weights needs (256-byte aligned device memory); 0 on invalid arguments. */
+/* Bytes of scratch pq_decode_attention_weights needs (256-byte aligned device memory), for any smaller n_seqs and max_seq_len, too; 0 on invalid arguments. */
 size_t pq_weights_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_t n_q_heads, int32_t max_seq_len);
 
 /*

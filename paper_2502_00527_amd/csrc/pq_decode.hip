@@ -164,8 +164,7 @@ struct Workspace {
 
 size_t round256(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
 
-Workspace carve_workspace(void* base, const pq_layout* l, int32_t n_seqs, int32_t n_q_heads, int32_t max_seq_len) {
-  const size_t slots = workspace_slots(l, n_seqs, n_q_heads, max_seq_len);
+Workspace carve_workspace(void* base, const pq_layout* l, int32_t n_seqs, int32_t max_seq_len, size_t slots) {
   const size_t acc_bytes = round256(slots * kHeadDim * sizeof(float));
   const size_t ml_bytes = round256(slots * 2 * sizeof(float));
   Workspace w;
@@ -176,6 +175,9 @@ Workspace carve_workspace(void* base, const pq_layout* l, int32_t n_seqs, int32_
   const size_t words = units + static_cast<size_t>(four_page_groups(l, n_seqs, max_seq_len)) + units;
   w.bytes = acc_bytes + ml_bytes + round256(words * sizeof(uint64_t));
   return w;
+}
+Workspace carve_workspace(void* base, const pq_layout* l, int32_t n_seqs, int32_t n_q_heads, int32_t max_seq_len) {
+  return carve_workspace(base, l, n_seqs, max_seq_len, workspace_slots(l, n_seqs, n_q_heads, max_seq_len));
 }
 
 // cos / sin of the centre of every angle bin of the uniform grid over [-pi, pi) (Section 3.2
@@ -517,15 +519,17 @@ namespace pq {
 namespace {
 
 // The window's workspace: one partial a chunk and query head, and the units' arrival words.
-Workspace carve_window_workspace(void* base, const pq_layout* l, int32_t n_seqs, int32_t n_q_heads, const ChunkPlan& plan) {
-  const size_t slots = static_cast<size_t>(n_seqs) * n_q_heads * plan.n_chunks;
+Workspace carve_window_workspace(void* base, size_t units, size_t slots) {
   const size_t acc_bytes = round256(slots * kHeadDim * sizeof(float)), ml_bytes = round256(slots * 2 * sizeof(float));
   Workspace w;
   w.acc = static_cast<float*>(base);
   w.ml = reinterpret_cast<float*>(static_cast<uint8_t*>(base) + acc_bytes);
   w.arrivals = reinterpret_cast<uint64_t*>(static_cast<uint8_t*>(base) + acc_bytes + ml_bytes);
-  w.bytes = acc_bytes + ml_bytes + round256(static_cast<size_t>(n_seqs) * l->n_kv_heads * sizeof(uint64_t));
+  w.bytes = acc_bytes + ml_bytes + round256(units * sizeof(uint64_t));
   return w;
+}
+Workspace carve_window_workspace(void* base, const pq_layout* l, int32_t n_seqs, int32_t n_q_heads, const ChunkPlan& plan) {
+  return carve_window_workspace(base, static_cast<size_t>(n_seqs) * l->n_kv_heads, static_cast<size_t>(n_seqs) * n_q_heads * plan.n_chunks);
 }
 
 int check_window(const pq_layout* l, int32_t n_seqs, int32_t n_q_heads, int32_t max_seq_len, int32_t window, int32_t n_sinks) {
@@ -586,12 +590,13 @@ extern "C" int pq_window_attention(const pq_layout* layout, const void* q, pq_dt
 }
 
 // Chunks as for a window: sequences are alike, as many chunks as start at once (the general plan makes chunks of 8 or 16 pages: 128 units of 48 pages are
-// then 384 work-groups, 46.8 us; in fours of 12 pages 512, 44.3).
+// then 384 work-groups, 46.8 us; in fours of 12 pages 512, 44.3).  The size is an upper bound over all smaller batches and lengths: a serving loop makes one workspace.
 size_t pq::alike_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_t n_q_heads, int32_t max_seq_len) {
   if (check_decode_shape(layout, n_seqs, n_q_heads, max_seq_len) != PQ_OK) return 0;
   const ChunkPlan plan = plan_window(layout, n_seqs, max_seq_len);
   if (plan.n_chunks > 65535) return 0;                       // grid.z
-  return carve_window_workspace(nullptr, layout, n_seqs, n_q_heads, plan).bytes;
+  const size_t units = static_cast<size_t>(n_seqs) * layout->n_kv_heads, pages = (static_cast<size_t>(max_seq_len) + kGroup - 1) / kGroup;
+  return carve_window_workspace(nullptr, units, window_partials_up_to(units, pages) * (n_q_heads / layout->n_kv_heads)).bytes;
 }
 
 int pq::attend_alike(const pq_layout* layout, const void* q, pq_dtype q_dtype, int32_t n_seqs, int32_t n_q_heads, const void* codes_pool,
@@ -721,6 +726,7 @@ __global__ __launch_bounds__(kMergeThreads) void pq_page_weights_kernel(const We
   a.weights[i] = a.before && a.decay != 0.f ? w + a.decay * before : w;
 }
 
+// (With partials for any smaller batch, so that its size grows with the batch's.)
 struct WeightsWorkspace {
   Workspace decode;
   float2 *page_ml, *totals;
@@ -728,7 +734,7 @@ struct WeightsWorkspace {
 };
 WeightsWorkspace carve_weights_workspace(void* base, const pq_layout* l, int32_t n_seqs, int32_t n_q_heads, int32_t max_seq_len) {
   WeightsWorkspace w;
-  w.decode = carve_workspace(base, l, n_seqs, n_q_heads, max_seq_len);
+  w.decode = carve_workspace(base, l, n_seqs, max_seq_len, workspace_slots_up_to(l, n_seqs, n_q_heads, max_seq_len));
   const size_t rows = static_cast<size_t>(n_seqs) * n_q_heads, pages = (static_cast<size_t>(max_seq_len) + kGroup - 1) / kGroup;
   const size_t total_bytes = round256(rows * sizeof(float2));
   uint8_t* const at = static_cast<uint8_t*>(base) + w.decode.bytes;

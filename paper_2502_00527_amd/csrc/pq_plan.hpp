@@ -127,6 +127,14 @@ inline size_t workspace_slots(const pq_layout* l, int32_t n_seqs, int32_t n_q_he
   return std::max(chunk_slots, (static_cast<size_t>(four_page_groups(l, n_seqs, max_seq_len)) + units) * (n_q_heads / l->n_kv_heads));
 }
 
+// workspace_slots() of no batch of fewer sequences or a lower max_seq_len is above this, and it grows with both.  plan_chunks() takes chunks of 32 pages, or the longest ones that make
+// 512 work-groups -- with chunks twice as long there would be fewer, so that there are fewer than 1024 -- or chunks of 4 pages with fewer than that.
+inline size_t workspace_slots_up_to(const pq_layout* l, int32_t n_seqs, int32_t n_q_heads, int32_t max_seq_len) {
+  const int64_t pages = (static_cast<int64_t>(max_seq_len) + kGroup - 1) / kGroup, units = static_cast<int64_t>(n_seqs) * l->n_kv_heads;
+  const int64_t chunks = std::max<int64_t>(units * ((pages + 31) / 32), std::min<int64_t>(1023, units * ((pages + 3) / 4)));
+  return static_cast<size_t>(std::max<int64_t>(chunks, four_page_groups(l, n_seqs, max_seq_len) + units)) * (n_q_heads / l->n_kv_heads);
+}
+
 // Chunk plan of the uniform angle grid's attention kernel for launches that are cut on the host, as if
 // every sequence had max_seq_len tokens (chunk_lengths() says why chunks are as long as they are).
 // The two-stage entry points, whose second one does not know the values' width, use the fp16 plan.
@@ -231,6 +239,11 @@ inline ChunkPlan plan_window(const pq_layout* l, int32_t n_seqs, int32_t bound) 
   p.pages_per_chunk = p.pages_small = static_cast<int32_t>(length);
   p.n_chunks = p.n_big = static_cast<int32_t>((pages + length - 1) / length);
   return p;
+}
+// Partials of a query head of plan_window()'s chunks, for no more units and pages than these: kResidentGroups chunks in all, unless there are more units, and none below kWaveRound pages
+// where a unit has several.
+inline size_t window_partials_up_to(int64_t units, int64_t pages) {
+  return static_cast<size_t>(std::min<int64_t>(std::max<int64_t>(units, kResidentGroups), units * ((pages + kWaveRound - 1) / kWaveRound)));
 }
 inline bool window_merges_in_kernel(const pq_layout* l, const ChunkPlan& plan, int32_t n_seqs) {
   return plan.n_chunks == 1 || (plan.n_chunks <= kMergeFan && static_cast<int64_t>(n_seqs) * l->n_kv_heads * plan.n_chunks >= kComputeUnits);

@@ -331,10 +331,12 @@ int check_selection(const pq_layout* l, int32_t n_seqs, int32_t n_q_heads, int32
 int64_t key_stride(int32_t max_seq_len) { return (most_pages(max_seq_len) + 3) & ~int64_t{3}; }
 size_t round256(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
 size_t arrival_bytes(const pq_layout* l, int32_t n_seqs) { return round256(static_cast<size_t>(n_seqs) * l->n_kv_heads * sizeof(uint64_t)); }
-// The arrival words, then the keys.
+// The arrival words, then the keys: as many bytes as a batch of no more sequences and pages may need.  Units of up to kMostKeys pages are shared in batches of fewer
+// than kComputeUnits units only, so that a smaller batch may need more than this one.
 size_t select_bytes(const pq_layout* l, int32_t n_seqs, int32_t max_seq_len) {
-  if (!shares_units(l, n_seqs, max_seq_len)) return 256;
-  return arrival_bytes(l, n_seqs) + round256(static_cast<size_t>(n_seqs) * l->n_kv_heads * key_stride(max_seq_len) * sizeof(uint32_t));
+  const int64_t most_seqs = most_pages(max_seq_len) > kMostKeys ? n_seqs : std::min<int64_t>(n_seqs, (kComputeUnits - 1) / l->n_kv_heads);
+  if (most_seqs == 0 || !shares_units(l, static_cast<int32_t>(most_seqs), max_seq_len)) return 256;
+  return arrival_bytes(l, static_cast<int32_t>(most_seqs)) + round256(static_cast<size_t>(most_seqs) * l->n_kv_heads * key_stride(max_seq_len) * sizeof(uint32_t));
 }
 
 // The arguments that the selection reads or writes, beyond check_selection().

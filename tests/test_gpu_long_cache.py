@@ -920,3 +920,34 @@ def test_both_ways_of_marshalling(monkeypatch):
     monkeypatch.setattr(pq, "_calls", pq._ByCtypes())
     for a, b in zip(native, all_calls()):
         assert torch.equal(a.nan_to_num(nan=-3.0) if a.is_floating_point() else a, b.nan_to_num(nan=-3.0) if b.is_floating_point() else b)
+
+
+@pytest.mark.parametrize("v_bits", [16, 4])
+def test_one_workspace_for_a_batch_that_shrinks(v_bits):
+    """A workspace of the largest batch, with anything in it, serves smaller batches and shorter bounds of the lengths: the same results as with one of their own.  Above
+    and below the number of units that are shared among work-groups."""
+    import paper_2502_00527_amd as pq
+    rng = np.random.default_rng(4)
+    lens = [270 * G, 50 * G - 5] + [int(n) for n in rng.integers(1, 3000, 34)]
+    c = Cache(lens, 8, v_bits=v_bits)
+    q, pools, whole = _queries(len(lens), 16, 3), _bound(c), (c.block_table, c.seq_lens, c.residual)
+    sizes = [pq.pq_select_workspace_bytes(c.layout, len(lens), c.max_seq_len), pq.pq_sparse_workspace_bytes(c.layout, len(lens), 16, c.max_seq_len, 12),
+             pq.pq_weights_workspace_bytes(c.layout, len(lens), 16, c.max_seq_len)]
+    works = [torch.from_numpy(rng.integers(0, 256, n + 256).astype(np.uint8)).to(DEV) for n in sizes]
+    for work, n in zip(works, sizes):
+        work[n:] = 0x5A
+    for n, most in [(36, 270 * G), (31, 270 * G), (5, 270 * G), (1, 270 * G), (32, 270 * G), (2, 260 * G), (36, 257 * G), (3, 8 * G)]:
+        c.block_table, c.seq_lens, c.residual = (x[:n].contiguous() for x in whole)
+        mine = q[:n].contiguous()
+        want = [*_select(c, mine, *pools, 12, max_seq_len=most), *_sparse(c, mine, pools, 12, max_seq_len=most), *_weigh(c, mine, max_seq_len=most, stride=c.block_table.shape[1])]
+        got = [torch.full_like(x, -5) for x in want]
+        pq.pq_select_pages(c.layout, mine, *pools, c.block_table, c.seq_lens, most, 1, 1, got[0], got[1], works[0][:sizes[0]])
+        pq.pq_sparse_attention(c.layout, mine, c.codes, c.params, c.v_pool, *pools, c.block_table, c.seq_lens, most, 1, 1, float(c.sm_scale), got[3], got[4], got[2],
+                               works[1][:sizes[1]], c.residual, c.v_bits, c.v_params)
+        pq.pq_decode_attention_weights(c.layout, mine, c.codes, c.params, c.v_pool, c.block_table, c.seq_lens, most, float(c.sm_scale), got[5], got[6],
+                                       works[2][:sizes[2]], None, 1.0, c.residual, c.v_bits, c.v_params)
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b), (n, most)
+        for work, size in zip(works, sizes):
+            assert bool((work[size:] == 0x5A).all()), "written past the workspace"

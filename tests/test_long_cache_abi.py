@@ -133,3 +133,34 @@ def test_a_given_choice_has_no_first_and_last_pages(lib, first, last):
     assert _call(lib, "pq_sparse_attention", SPARSE, **given) == WORKSPACE
     for change in (dict(chosen=0), dict(selected=NULL), dict(selected_lens=NULL), dict(selected=ODD), dict(q=NULL), dict(heads=12), dict(max_seq_len=0), dict(out=NULL)):
         assert _call(lib, "pq_sparse_attention", SPARSE, **{**given, **change}) == INVALID
+
+
+def _never_falls(sizes):
+    """sizes[i][j]...: along no axis does a size get smaller."""
+    import numpy as np
+    a = np.array(sizes, np.int64)
+    assert (a > 0).all()
+    for axis in range(a.ndim):
+        fall = np.argwhere(np.diff(a, axis=axis) < 0)
+        assert len(fall) == 0, (axis, fall[:5].tolist())
+
+
+N_SEQS = [1, 2, 3, 5, 7, 8, 12, 13, 16, 31, 32, 33, 63, 64, 65, 100, 127, 128, 200, 255, 256, 257, 511, 512, 513, 600, 1000, 2000]
+LENGTHS = [1, 128, 129, 500, 896, 897, 1024, 4000, 20000, 32768, 32769, 40000, 65536, 100000, 127999, 131072, 500000, 8192 * 128, 8192 * 128 + 1, 1 << 21]
+
+
+@pytest.mark.parametrize("heads", [1, 2, 3, 8, 32])
+def test_a_workspace_serves_smaller_batches(lib, heads):
+    """A serving loop makes one workspace for its largest batch, and batches shrink: no size falls as sequences, lengths or chosen pages become more."""
+    layout = pq.Layout(128, 4, 4, 128, heads)
+    seqs = [n for n in N_SEQS if n * heads <= 65535]
+    _never_falls([[pq.pq_select_workspace_bytes(layout, n, most) for most in LENGTHS] for n in seqs])
+
+
+@pytest.mark.parametrize("heads,group", [(1, 1), (2, 16), (3, 5), (8, 4), (32, 2)])
+@pytest.mark.parametrize("angles", [0, 1])
+def test_a_workspace_of_attention_serves_smaller_batches(lib, heads, group, angles):
+    layout = pq.Layout(128, 4, 4, 128, heads, angles)
+    _never_falls([[pq.pq_weights_workspace_bytes(layout, n, heads * group, most) for most in LENGTHS] for n in N_SEQS])
+    chosen = [1, 4, 7, 8, 9, 13, 16, 17, 32, 48, 100, 500, 3000, 100000]
+    _never_falls([[[pq.pq_sparse_workspace_bytes(layout, n, heads * group, most, c) for c in chosen] for most in LENGTHS] for n in N_SEQS])
