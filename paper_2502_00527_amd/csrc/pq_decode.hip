@@ -590,11 +590,13 @@ extern "C" int pq_window_attention(const pq_layout* layout, const void* q, pq_dt
 }
 
 // Chunks as for a window: sequences are alike, as many chunks as start at once (the general plan makes chunks of 8 or 16 pages: 128 units of 48 pages are
-// then 384 work-groups, 46.8 us; in fours of 12 pages 512, 44.3).  The size is an upper bound over all smaller batches and lengths: a serving loop makes one workspace.
+// then 384 work-groups, 46.8 us; in fours of 12 pages 512, 44.3).
+static ChunkPlan plan_alike(const pq_layout* layout, int32_t n_seqs, int32_t max_seq_len) { return plan_window(layout, n_seqs, max_seq_len); }
+
+// An upper bound over all smaller batches and lengths: a serving loop makes one workspace.
 size_t pq::alike_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_t n_q_heads, int32_t max_seq_len) {
   if (check_decode_shape(layout, n_seqs, n_q_heads, max_seq_len) != PQ_OK) return 0;
-  const ChunkPlan plan = plan_window(layout, n_seqs, max_seq_len);
-  if (plan.n_chunks > 65535) return 0;                       // grid.z
+  if (plan_alike(layout, n_seqs, max_seq_len).n_chunks > 65535) return 0;          // grid.z
   const size_t units = static_cast<size_t>(n_seqs) * layout->n_kv_heads, pages = (static_cast<size_t>(max_seq_len) + kGroup - 1) / kGroup;
   return carve_window_workspace(nullptr, units, window_partials_up_to(units, pages) * (n_q_heads / layout->n_kv_heads)).bytes;
 }
@@ -602,10 +604,11 @@ size_t pq::alike_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_
 int pq::attend_alike(const pq_layout* layout, const void* q, pq_dtype q_dtype, int32_t n_seqs, int32_t n_q_heads, const void* codes_pool,
                      const void* params_pool, const void* v_pool, int32_t v_bits, const void* v_params_pool, int64_t n_pool_pages,
                      const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* seq_lens, int32_t max_seq_len, float sm_scale, float* out,
-                     const void* residual_keys, void* workspace, hipStream_t stream) {
+                     const void* residual_keys, void* workspace, size_t workspace_bytes, hipStream_t stream) {
   const bool grouped = layout->angle_quantizer == PQ_ANGLE_GROUPED;
-  const ChunkPlan plan = plan_window(layout, n_seqs, max_seq_len);
+  const ChunkPlan plan = plan_alike(layout, n_seqs, max_seq_len);
   const Workspace ws = carve_window_workspace(workspace, layout, n_seqs, n_q_heads, plan);
+  if (ws.bytes > workspace_bytes) return PQ_ERR_WORKSPACE;   // (what the plan takes, whatever the size function says)
   DecodeArgs a = attention_args(layout, q, q_dtype, n_seqs, n_q_heads, codes_pool, params_pool, v_pool, v_params_pool, n_pool_pages, block_table,
                                 max_pages_per_seq, seq_lens, max_seq_len, sm_scale, out, residual_keys, ws, plan);
   // (few units, too: 8 of 32 pages 0.5 us less than with a merge launch)

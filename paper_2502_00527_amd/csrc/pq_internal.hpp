@@ -22,12 +22,12 @@ int check_attention(const pq_layout* layout, const void* q, pq_dtype q_dtype, in
                     const void* residual_keys);
 
 // Attention of sequences that are nearly all as long as max_seq_len lets them be (pq_decode.hip), of arguments that check_attention() has
-// passed; the workspace is of as many bytes (0: there is no such launch), 256-byte aligned.
+// passed; the workspace is of as many bytes or more (0: there is no such launch), 256-byte aligned.  A workspace that the launch's plan does not fit into is refused.
 size_t alike_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_t n_q_heads, int32_t max_seq_len);
 int attend_alike(const pq_layout* layout, const void* q, pq_dtype q_dtype, int32_t n_seqs, int32_t n_q_heads, const void* codes_pool,
                  const void* params_pool, const void* v_pool, int32_t v_bits, const void* v_params_pool, int64_t n_pool_pages,
                  const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* seq_lens, int32_t max_seq_len, float sm_scale, float* out,
-                 const void* residual_keys, void* workspace, hipStream_t stream);
+                 const void* residual_keys, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 // An encoder's work-groups (256 threads) are one a (token group, KV head) in a one-dimensional grid, which HIP limits to
 // 2^32 - 1 threads: launch(first group, groups) is called for as many ranges of token groups as that takes.

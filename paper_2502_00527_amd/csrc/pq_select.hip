@@ -458,5 +458,5 @@ extern "C" int pq_sparse_attention(const pq_layout* layout, const void* q, pq_dt
     if (st != PQ_OK) return st;
   }
   return attend_alike(&one, q, q_dtype, rows, heads, codes_pool, params_pool, v_pool, v_bits, v_params_pool, row_pages, selected, n_selected, selected_lens,
-                      tokens, sm_scale, out, residual_keys, static_cast<uint8_t*>(workspace) + before, static_cast<hipStream_t>(hip_stream));
+                      tokens, sm_scale, out, residual_keys, static_cast<uint8_t*>(workspace) + before, workspace_bytes - before, static_cast<hipStream_t>(hip_stream));
 }
