@@ -333,7 +333,8 @@ int pq_append_keys(const pq_layout* layout, const void* new_keys, pq_dtype key_d
  *
  *   seq_lens, new_lens   device int32 [n_seqs]; negative counts as 0; a sequence's sum, and that of all
  *                        new_lens, is below 2^31.  Not changed in place: no output may be one of the inputs
- *   free_pages           device int32 [n_free]: page ids to take from the front of (NULL if n_free is 0)
+ *   free_pages           device int32 [n_free]: page ids to take from the front of (NULL if n_free is 0).  Negative entries, as
+ *                        pq_evict_pages lists missing pages, are passed over
  *   block_table          device int32 [n_seqs][max_pages_per_seq]; entries of the pages that new tokens begin are written,
  *                        -1 where free_pages has run out; others are left as they are.  A page
  *                        past the row's width has no entry (its place in free_pages is skipped)
@@ -342,8 +343,9 @@ int pq_append_keys(const pq_layout* layout, const void* new_keys, pq_dtype key_d
  *                        page is missing and for places past the last new token.  Tokens past max_new_tokens get neither
  *                        slots nor pages
  *   lens_after           device int32 [n_seqs], written: seq_lens + new_lens
- *   counts               device int32 [2], written: pages that the new tokens begin (the call has used the first
- *                        min(counts[0], n_free) of free_pages; more than n_free means that some are missing), new tokens
+ *   counts               device int32 [2], written: pages that the new tokens begin and the entries that were passed over before the last of
+ *                        them (the call has used the first min(counts[0], n_free) of free_pages; more than n_free means that some pages are
+ *                        missing, and how many), new tokens
  *
  * n_seqs <= 2^20, max_new_tokens < 2^31.  No workspace; calls that overlap share nothing but their outputs.
  */
@@ -558,7 +560,10 @@ int pq_decode_attention_weights(const pq_layout* layout, const void* q, pq_dtype
  *                   had: those that are left, then -1 and weights of 0
  *   lens_after      device int32 [n_seqs], written: tokens that are left; not seq_lens
  *   freed           device int32 [n_freed], written: block-table entries of the pages given up, sequence by sequence and in each from its
- *                   beginning, as they were (-1 where a page was missing; a page that two rows hold as often as they give it up); as far as n_freed.  free_pages of a later pq_plan_pages
+ *                   beginning, as they were; as far as n_freed.  They are free_pages of a later pq_plan_pages, which passes over those of missing pages,
+ *                   where these are negative (an entry past the pool's end would be taken for a page).  Not so where rows share pages: a page that
+ *                   another row keeps is in the list all the same, and one that two rows give up is in it twice.  Such a list is to be
+ *                   gone through by the caller, who counts a page's holders, before anything is planned from it
  *   counts          device int32 [1], written: pages given up
  * n_seqs <= 65535.  No workspace; calls that overlap share nothing but their outputs.
  */

@@ -5,12 +5,17 @@
 // page(position / g) * g + position % g.  A page is begun by the one new token with position % g == 0,
 // which writes the block-table entry: nobody reads an entry that somebody writes.
 //
+// Free pages are the entries of free_pages that are not negative.  Each work-group looks for negative ones among as many entries as the sequences of its tiles
+// need, while the entries that it takes are on their way, and only where there are some goes through the list in order (find_pages()).  The look takes 0.1 us of a step
+// and 0.7 of the prompts below, 13 KB of the list in each work-group; 1.0 of twice as many tokens, and 1.9 with a search for the end of what a work-group's own tokens need.
+//
 // One launch: each work-group owns a range of tokens and finds the sequences they belong to by itself, a tile of
 // kTile sequences at a time (prefix sums of tokens and pages, then a binary search a token in LDS), up to the
 // tile that holds its last token.  Few tokens a thread, searched side by side: 200 sequences with
-// 400K tokens take 5.8 us, with eight a thread one after the other they took 9.3 (a launch by itself: 3.7 - 4.2).  The last work-group goes through all of them and writes what belongs to sequences.
+// 400K tokens take 6.4 us (5.8 before free_pages was looked through), with eight a thread one after the other they took 9.3 (a launch by itself: 3.7 - 4.2).  The last work-group goes through all of them and writes what belongs to sequences.
 #include <hip/hip_runtime.h>
 
+#include "pq_decode_kernels.hpp"
 #include "pq_internal.hpp"
 
 namespace pq {
@@ -37,17 +42,64 @@ struct PlanArgs {
   int32_t max_pages_per_seq;
 };
 
+constexpr int kScan = 2;                                     // loads of four entries of free_pages that a thread has under way together
+constexpr uint32_t kHeld = 0xffffffffu;                      // the token's page is there already
+
 __device__ __forceinline__ uint32_t pages_up(uint32_t tokens) { return (tokens + kGroup - 1) / kGroup; }
+
+// The ids of places among the entries of free_pages that are not negative, -1 from the last of them on, and the entries of the list that `pages` of them
+// take, those that are passed over with them (the list's length and as many as there are too few, if it runs out).  All threads of the work-group call it; `ids` and `counts` are LDS
+// that nobody reads any more.
+__device__ __forceinline__ uint32_t find_pages(const PlanArgs& a, uint32_t pages, const uint32_t (&place)[kTokensPerThread], int32_t (&id)[kTokensPerThread], int32_t* ids,
+                                               uint32_t* counts, int tid) {
+  const int lane = tid & 63, wave = tid >> 6;
+#pragma unroll
+  for (int k = 0; k < kTokensPerThread; ++k)
+    if (place[k] != kHeld) id[k] = -1;
+  uint32_t found = 0, used = 0;                              // ids in the entries so far, entries up to the last one that is needed
+  for (int64_t first = 0; first < a.n_free && found < pages; first += kPlanThreads) {
+    const int32_t v = first + tid < a.n_free ? a.free_pages[first + tid] : -1;
+    const uint64_t mask = __builtin_amdgcn_ballot_w64(v >= 0);
+    __syncthreads();                                         // everybody has read what the round before wrote
+    if (lane == 0) counts[wave] = __builtin_popcountll(mask);
+    __syncthreads();
+    uint32_t at = __builtin_popcountll(mask & ((uint64_t{1} << lane) - 1)), all = 0;
+#pragma unroll
+    for (int w = 0; w < kPlanThreads / 64; ++w) {
+      at += w < wave ? counts[w] : 0;
+      all += counts[w];
+    }
+    if (v >= 0) ids[at] = v;
+    if (v >= 0 && found + at == pages - 1) ids[kPlanThreads] = static_cast<int32_t>(first) + tid + 1;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kTokensPerThread; ++k)
+      if (place[k] != kHeld && place[k] >= found && place[k] - found < all) id[k] = ids[place[k] - found];
+    found += all;
+    if (found >= pages) used = static_cast<uint32_t>(ids[kPlanThreads]);
+  }
+  return found >= pages ? used : static_cast<uint32_t>(a.n_free) + (pages - found);
+}
 
 __global__ __launch_bounds__(kPlanThreads) void pq_plan_pages_kernel(const PlanArgs a) {
   __shared__ uint32_t first_token[kTile + 1];                // of the tile's sequences, and of what follows
   __shared__ uint32_t first_page[kTile];                     // place in free_pages
-  __shared__ uint32_t wave_tokens[kPlanThreads / 64], wave_pages[kPlanThreads / 64];
+  __shared__ uint32_t wave_tokens[kPlanThreads / 64], wave_pages[kPlanThreads / 64], gaps[kPlanThreads / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const bool last = blockIdx.x == gridDim.x - 1;
   const uint32_t begin = blockIdx.x * kTokensPerGroup;
   const uint32_t end = static_cast<uint32_t>(min(a.max_new_tokens, static_cast<int64_t>(begin) + kTokensPerGroup));
   uint32_t tokens = 0, pages = 0;                            // of the sequences before the tile
+  // of this thread's tokens: place among the free pages, entry of the block table (-1: past the row), place in the page (-1: no such token)
+  uint32_t place[kTokensPerThread];
+  int64_t entry[kTokensPerThread];
+  int within[kTokensPerThread];
+  int32_t id[kTokensPerThread];
+#pragma unroll
+  for (int k = 0; k < kTokensPerThread; ++k) {
+    place[k] = kHeld;
+    entry[k] = within[k] = id[k] = -1;
+  }
   int search_from = kTile / 2;                               // half of a power of two that no tile has more sequences than
   while (search_from >= a.n_seqs && search_from > 0) search_from >>= 1;
   for (int s0 = 0; s0 < a.n_seqs && (last || tokens < end); s0 += kTile) {
@@ -113,19 +165,47 @@ __global__ __launch_bounds__(kPlanThreads) void pq_plan_pages_kernel(const PlanA
       const int low = low_of[k], s = min(s0 + low, a.n_seqs - 1);     // (sums past 2^32 are not in order)
       const uint32_t len = max(0, a.seq_lens[s]);
       const uint32_t position = len + (token - first_token[low]), page = position / kGroup, have = pages_up(len);
-      int32_t* const row = a.block_table + static_cast<int64_t>(s) * a.max_pages_per_seq;
-      const bool in_row = page < static_cast<uint32_t>(a.max_pages_per_seq);
-      int32_t id = -1;
-      if (page >= have) {
-        const uint32_t place = first_page[low] + (page - have);
-        if (in_row && place < static_cast<uint32_t>(a.n_free)) id = a.free_pages[place];
-        if (in_row && position % kGroup == 0) row[page] = id;
-      } else if (in_row) {
-        id = row[page];
-      }
-      a.slots[token] = id >= 0 ? static_cast<int64_t>(id) * kGroup + position % kGroup : -1;
+      entry[k] = page < static_cast<uint32_t>(a.max_pages_per_seq) ? static_cast<int64_t>(s) * a.max_pages_per_seq + page : -1;
+      place[k] = page >= have ? first_page[low] + (page - have) : kHeld;
+      within[k] = position % kGroup;
+      if (entry[k] >= 0 && place[k] == kHeld) id[k] = a.block_table[entry[k]];
+      else if (entry[k] >= 0 && place[k] < static_cast<uint32_t>(a.n_free)) id[k] = a.free_pages[place[k]];
     }
-    __syncthreads();                                         // the next tile writes what was searched
+    // (the next tile writes what was searched)
+    if (s0 + kTile < a.n_seqs && (last || tokens < end)) __syncthreads();
+  }
+  uint32_t used = pages;
+  const uint32_t needed = min(pages, static_cast<uint32_t>(a.n_free));
+  if (needed > 0) {                                          // a negative one among them?  (Zeros behind them)
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(a.free_pages, needed * 4u);
+    auto four = [&](uint32_t first) {
+      const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(r, first * 4u, 0, 0);
+      return (v.x | v.y) | (v.z | v.w);
+    };
+    bool gap;
+    if (needed <= 4 * 64) {                                  // every wavefront for itself
+      gap = __builtin_amdgcn_ballot_w64(static_cast<int32_t>(four(4 * lane)) < 0) != 0;
+    } else {
+      uint32_t all = 0;
+      for (uint32_t first = 4 * tid; first < needed; first += kScan * 4 * kPlanThreads) {
+        uint32_t some[kScan];
+#pragma unroll
+        for (int i = 0; i < kScan; ++i) some[i] = four(first + i * 4 * kPlanThreads);
+#pragma unroll
+        for (int i = 0; i < kScan; ++i) all |= some[i];
+      }
+      const bool mine = __builtin_amdgcn_ballot_w64(static_cast<int32_t>(all) < 0) != 0;
+      if (lane == 0) gaps[wave] = mine;
+      __syncthreads();
+      gap = (gaps[0] | gaps[1] | gaps[2] | gaps[3]) != 0;
+    }
+    if (gap) used = find_pages(a, pages, place, id, reinterpret_cast<int32_t*>(first_page), wave_pages, tid);
+  }
+#pragma unroll
+  for (int k = 0; k < kTokensPerThread; ++k) {
+    if (within[k] < 0) continue;
+    if (place[k] != kHeld && entry[k] >= 0 && within[k] == 0) a.block_table[entry[k]] = id[k];
+    a.slots[begin + k * kPlanThreads + tid] = entry[k] >= 0 && id[k] >= 0 ? static_cast<int64_t>(id[k]) * kGroup + within[k] : -1;
   }
   for (int k = 0; k < kTokensPerThread; ++k) {               // behind the last token
     const uint32_t token = begin + k * kPlanThreads + tid;
@@ -133,7 +213,7 @@ __global__ __launch_bounds__(kPlanThreads) void pq_plan_pages_kernel(const PlanA
   }
   if (last && tid == 0) {
     a.starts[a.n_seqs] = static_cast<int32_t>(tokens);
-    a.counts[0] = static_cast<int32_t>(pages);
+    a.counts[0] = static_cast<int32_t>(used);
     a.counts[1] = static_cast<int32_t>(tokens);
   }
 }

@@ -951,3 +951,35 @@ def test_one_workspace_for_a_batch_that_shrinks(v_bits):
             assert torch.equal(a, b), (n, most)
         for work, size in zip(works, sizes):
             assert bool((work[size:] == 0x5A).all()), "written past the workspace"
+
+
+def test_pages_are_planned_from_an_eviction_with_missing_ones():
+    """Sequences that got no pages while none were free give up entries without a page: what is planned from the list of freed ones passes over these, and every new token has a
+    slot of its own."""
+    import paper_2502_00527_amd as pq
+    lay, width = pq.Layout(D, 4, 4, G, 2), 12
+    table = torch.full((3, width), -1, dtype=torch.int32, device=DEV)
+
+    def plan(lens, new, free):
+        starts, counts, after = torch.zeros(4, dtype=torch.int32, device=DEV), _ints([0, 0]), torch.zeros_like(lens)
+        slots = torch.full((sum(new),), -9, dtype=torch.int64, device=DEV)
+        pq.pq_plan_pages(lay, lens, _ints(new), free, table, starts, slots, after, counts)
+        return after, slots, counts.tolist()
+
+    lens, slots, counts = plan(_ints([0, 0, 0]), [3 * G, 9 * G, 5 * G], torch.arange(17, dtype=torch.int32, device=DEV))
+    assert counts == [17, 17 * G] and bool((slots >= 0).all())
+    lens, slots, counts = plan(lens, [5 * G, 0, 0], _ints([]))
+    assert counts == [5, 5 * G] and bool((slots == -1).all())              # the first sequence has three pages, five are missing
+    weights = torch.rand((3, width), device=DEV) + 0.1
+    weights[0, 3:8] = 0
+    freed, count, after = torch.full((40,), -1, dtype=torch.int32, device=DEV), _ints([0]), torch.zeros_like(lens)
+    pq.pq_evict_pages(lay, table, lens, weights, 4, 0, 0, table, after, weights, freed, count)
+    # four entries of the first sequence, those without a page, which weigh nothing; five of the second one, one of the third
+    assert int(count) == 4 + 5 + 1 and bool((freed[:4] == -1).all()) and bool((freed[4:10] >= 0).all())
+    held = set(table[table >= 0].tolist())
+    lens, slots, counts = plan(after, [G, G, G], freed[:10])
+    assert counts == [7, 3 * G] and bool((slots >= 0).all()) and len(set(slots.tolist())) == 3 * G
+    assert (slots[::G] // G).tolist() == freed[4:7].tolist() and not set(freed[4:7].tolist()) & held
+    # more pages than there are free ones: one is short
+    lens, slots, counts = plan(lens, [2 * G, 2 * G, 0], freed[7:10])
+    assert counts == [4, 4 * G] and int((slots < 0).sum()) == G and bool((slots[:3 * G] >= 0).all())

@@ -89,3 +89,55 @@ def test_room_for_fewer_or_more_tokens_than_there_are(n_slots):
 def test_no_sequences():
     table, starts, slots, after, counts = _run([], [], [3], np.zeros((0, 4), np.int32), 9)
     assert starts.tolist() == [0] and counts.tolist() == [0, 0] and (slots == -1).all()
+
+
+def _with_gaps(free, gaps, rng):
+    """`free` with negative entries at `gaps` random places, and what the plan takes of it: the list in order, without them."""
+    out = list(free)
+    for at in sorted(rng.integers(0, len(free) + 1, gaps), reverse=True):
+        out.insert(int(at), int(rng.choice([-1, -1, -7, -2 ** 31])))
+    return np.array(out, np.int32)
+
+
+def _check_gaps(lens, new, gaps, n_free=None, n_slots=None, width=None, seed=0):
+    """The header's walk over the entries that are not negative; the first count is where it has got to in the whole list, or how many pages it lacks behind it."""
+    lens, new = np.asarray(lens, np.int32), np.asarray(new, np.int32)
+    rng = np.random.default_rng(seed)
+    held = (np.maximum(lens, 0) + G - 1) // G
+    most = (np.maximum(lens, 0) + np.maximum(new, 0) + G - 1) // G
+    need = int((most - held).sum())
+    table = rng.integers(0, 1 << 24, (len(lens), width or max(1, int(most.max())))).astype(np.int32)
+    ids = rng.permutation(need + 5).astype(np.int32)[:need + 5 if n_free is None else n_free]
+    free = _with_gaps(ids, gaps, rng)
+    n_slots = int(np.maximum(new, 0).sum()) if n_slots is None else n_slots
+    got, want = _run(lens, new, free, table, n_slots), list(_plan(lens, new, ids, table, n_slots))
+    there = np.flatnonzero(free >= 0)
+    want[4][0] = 0 if need == 0 else (there[need - 1] + 1 if need <= len(there) else len(free) + need - len(there))
+    for a, b in zip(got, want):
+        np.testing.assert_array_equal(a, b)
+
+
+@pytest.mark.parametrize("gaps", [1, 3, 300])
+@pytest.mark.parametrize("lens,new", [([0], [1]), ([127], [1]), ([128], [1]), ([5], [500]), ([127, 0, 256], [2, 0, 1]), ([300, 7], [0, 0]), ([-4, 9], [3, -2]), ([100, 250, 0, 128], [300, 6, 700, 128])])
+def test_missing_pages_among_the_free_ones(lens, new, gaps):
+    for seed in range(3):
+        _check_gaps(lens, new, gaps, seed=seed)
+
+
+@pytest.mark.parametrize("n_free", [0, 1, 7])
+def test_missing_pages_and_free_ones_that_run_out(n_free):
+    _check_gaps([100, 250, 0, 128], [300, 6, 700, 128], 5, n_free=n_free)
+    _check_gaps([100, 250, 0, 128], [300, 6, 700, 128], 400, n_free=n_free)
+
+
+@pytest.mark.parametrize("seqs,most_len,most_new,gaps", [(64, 16384, 1, 2), (1025, 300, 40, 1), (1025, 300, 40, 900), (2500, 1000, 1, 7), (3, 9, 9000, 3), (40, 300, 9000, 1), (40, 300, 9000, 2500),
+                                                         (3000, 100, 400, 5000)])
+def test_missing_pages_in_long_lists(seqs, most_len, most_new, gaps):
+    rng = np.random.default_rng(gaps)
+    lens, new = rng.integers(0, most_len + 1, seqs), rng.integers(0, most_new + 1, seqs)
+    _check_gaps(lens, new, gaps, seed=gaps)
+    _check_gaps(lens, new, gaps, seed=gaps, n_free=1100, n_slots=int(new.sum()) - int(new.sum()) // 3, width=20)
+
+
+def test_missing_pages_alone():
+    _check_gaps([100, 10], [300, 300], 600, n_free=0)
