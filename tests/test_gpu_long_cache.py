@@ -983,3 +983,27 @@ def test_pages_are_planned_from_an_eviction_with_missing_ones():
     # more pages than there are free ones: one is short
     lens, slots, counts = plan(lens, [2 * G, 2 * G, 0], freed[7:10])
     assert counts == [4, 4 * G] and int((slots < 0).sum()) == G and bool((slots[:3 * G] >= 0).all())
+
+
+@pytest.mark.parametrize("bits,grouped", [((4, 4), False), ((3, 3), True)])
+@pytest.mark.parametrize("v_bits", [4, 2])
+def test_codes_are_summed_about_their_middle(bits, grouped, v_bits):
+    """Where it shows: queries of zeros, so that every weight is exactly 1 and nothing but the sums is rounded, over 640 pages whose mean is small against the values' range, by so many
+    units that chunks are long.  In units of 2^-24 / sqrt(3) = 3.4e-8 of a value's size: a token's zero point and its codes' middle are 2.7.  About the middle, 32 tokens' codes and middles
+    are two products of at most 8 roundings each at up to 32 * 2.7 + the sum so far, 64 roundings a page at 86 + 0.7 of the chunk's sum.  A wavefront has at most 160 pages (chosen ones: one chunk), a sum of 143 and
+    so an error of sqrt(160 * 64) * (86 + 100) = 18800, 132 of the sum: 4.6e-6; 16 pages with the weights, 91: 3.1e-6; 8 with grouped angles.  What joins them adds a few roundings of the sum.
+    As they are, codes and zero points are sums of 2.7 a token before they meet.  At one rounding a product a wavefront of 8 pages has sqrt(32) * 1380 = 7800 of a sum of 32: 245, 8.4e-6, of 16 pages 1.7e-5: 2.7 times
+    the bounds above and more."""
+    c = Cache([640 * G - 5], 2, bits, grouped, v_bits)
+    pools = _bound(c)
+    c.residual = c.residual.expand(256, -1, -1, -1).contiguous()
+    c.block_table, c.seq_lens = c.block_table.expand(256, -1).contiguous(), c.seq_lens.expand(256).contiguous()
+    q = torch.zeros((256, 8, D), dtype=torch.float16, device=DEV)
+    want = c.v64[0].mean(0)                                              # [KV head, d]
+    off = []
+    for out in (_weigh(c, q)[0], _sparse(c, q, pools, 640)[0], _decode(c, q)):           # pq_decode_attention sums codes as they are
+        assert bool((out == out[:1]).all())
+        off.append(float((out[0].view(2, 4, D).double() - want[:, None]).norm() / want.norm() / 2))
+    # (2 bits of a code, 11 of its scale and 10 of a wavefront's 1024 tokens with grouped angles are 23 bits: nothing is rounded before the quotient, centred or not.  That is two
+    # roundings, sqrt(2) * 2^-24 / sqrt(3) = 5e-8)
+    assert max(off[:2]) <= 4.6e-6 and off[0] <= max(off[2] / 2, 2.0 ** -23), off
