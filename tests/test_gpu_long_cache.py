@@ -1007,3 +1007,41 @@ def test_codes_are_summed_about_their_middle(bits, grouped, v_bits):
     # (2 bits of a code, 11 of its scale and 10 of a wavefront's 1024 tokens with grouped angles are 23 bits: nothing is rounded before the quotient, centred or not.  That is two
     # roundings, sqrt(2) * 2^-24 / sqrt(3) = 5e-8)
     assert max(off[:2]) <= 4.6e-6 and off[0] <= max(off[2] / 2, 2.0 ** -23), off
+
+
+@pytest.mark.parametrize("heads,group", [(4, 10), (5, 7), (8, 8), (3, 16), (6, 12)])
+@pytest.mark.parametrize("lens", [[3000, 1], [700, 90, 0], [2000] * 20])
+def test_weights_of_many_query_heads(heads, group, lens):
+    """More than 32 of them, also such as are no multiple of 16: a launch that leaves its chunks to the merge, sequences of one chunk, and chunks merged in the kernel."""
+    _check_weights(Cache(lens, heads), _queries(len(lens), heads * group, 3))
+
+
+@pytest.mark.parametrize("lens,heads,group", [([3000, 1300], 4, 10), ([700, 900], 8, 8), ([3000, 1300], 2, 2)])
+@pytest.mark.parametrize("grouped", [False, True])
+def test_weights_of_missing_pages_and_many_heads(lens, heads, group, grouped):
+    """The others' weights are those over the tokens that are there, with chunks merged by the second launch, a whole one missing among them, and with one chunk a sequence."""
+    c = Cache(lens, heads, (4, 4), grouped)
+    n_q = heads * group
+    q = _queries(len(lens), n_q, 3)
+    gone = [[4, 5, 6, 7, 1], [0, 6]]
+    for s, pages in enumerate(gone):
+        c.block_table[s, pages] = torch.tensor([-1, c.codes.shape[0]], dtype=torch.int32, device=DEV).repeat(3)[:len(pages)]
+    out, weights = _weigh(c, q)
+    for s, L in enumerate(lens):
+        there = torch.cat([torch.arange(p * G, min(L, (p + 1) * G), device=DEV) for p in range((L + G - 1) // G) if p not in gone[s]])
+        mass, most = torch.zeros((L + G - 1) // G, dtype=torch.float64, device=DEV), 0.0
+        for h in range(n_q):
+            k, v = c.k64[s][there, h // group], c.v64[s][there, h // group]
+            terms = k * q[s, h].double()
+            w = torch.softmax(terms.sum(-1) * c.sm_scale, 0)
+            mass.index_add_(0, there // G, w)
+            size = float(terms.abs().sum(-1).max()) * float(c.sm_scale)
+            most = max(most, size)
+            want, spread = (w[:, None] * v).sum(0), ((w * w)[:, None] * (v * v)).sum(0).sqrt()
+            pair_q, pair_k = (x[..., :64] ** 2 + x[..., 64:] ** 2 for x in (q[s, h].double(), k))
+            slope = (pair_q * pair_k).sum(-1).max().sqrt() * float(c.sm_scale)
+            assert float((out[s, h].double() - want).norm() / want.norm()) <= ref.output_bar(spread, slope, want, size)
+        held = [p for p in gone[s] if p < len(mass)]
+        assert not weights[s, held].any()
+        wrong = (weights[s, :len(mass)].double() - mass).abs() - ref.weight_tolerance(mass, most, n_q)
+        assert bool((wrong <= 0).all()), (s, float(wrong.max()))
