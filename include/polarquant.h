@@ -489,6 +489,8 @@ size_t pq_select_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_
  * m_b = largest |q_i| of a block over the KV head's query heads, q8_i = round(q_i * (127 / m_b)) (0 where m_b < 2^-100) and
  * u_b = m_b scale_b:  (n_0 u_0 + n_1 u_1) + (n_2 u_2 + n_3 u_3),  n_b = sum over the block of q8_i c_i + |q8_i| w_i,  the largest of the query
  * heads; every operation rounded to fp32, so that the choice does not depend on how a launch is shared out.  Among equals the first pages.
+ * With c, w and q8 off by half a step each, no key of the page has a q . k above (score + sum over the blocks of u_b (sum over the block of |q8_i| + 64 . 32)) / 127: a
+ * block's scale goes by its largest channel, and channels far smaller than that one count with its step.
  *
  *   q               device [n_seqs][n_q_heads][d], q_dtype PQ_F16 or PQ_F32 (16-byte aligned); n_q_heads / n_kv_heads 1 .. 16
  *   bounds, bound_scales   of every page but the last n_last and the first n_first

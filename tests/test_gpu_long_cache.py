@@ -1045,3 +1045,28 @@ def test_weights_of_missing_pages_and_many_heads(lens, heads, group, grouped):
         assert not weights[s, held].any()
         wrong = (weights[s, :len(mass)].double() - mass).abs() - ref.weight_tolerance(mass, most, n_q)
         assert bool((wrong <= 0).all()), (s, float(wrong.max()))
+
+
+@pytest.mark.parametrize("bits,grouped", FORMATS)
+@pytest.mark.parametrize("key_scale", [1.0, 30.0])
+def test_a_score_is_a_bound(bits, grouped, key_scale):
+    """No key of a page has a product with a query above (score + sum over the blocks of u_b (sum of |q8_i| + 64 * 32)) / 127: centres, half-widths and queries are each off by half a step, a channel by
+    |q8| / 2 + |q8| / 2 + (|centre| + half-width) / 2 <= |q8| + 63.5 steps; the rest of the 64 is what fp32 rounds.  One channel of 128 is eight times the others' size, and its block's scale with it."""
+    c = Cache([1536, 700], 2, bits, grouped, key_scale=key_scale)
+    q = _queries(2, 8, 7, torch.float32)
+    q[0, 1, 5], q[1, :, 64:] = 20.0, q[1, :, 64:] * 0.01
+    bounds, scales = (x.cpu().numpy() for x in _bound(c))
+    for s, L in enumerate(c.lens):
+        for h in range(2):
+            whole = L // G
+            mine, ids = q[s, 4 * h:4 * h + 4].cpu().numpy(), c.table[s, :whole]
+            score = ref.scores_of(mine, bounds[ids, h], scales[ids, h]).astype(np.float64)
+            slack = np.zeros((4, whole))
+            for b in range(4):
+                part = np.concatenate([mine[:, 16 * b:16 * b + 16], mine[:, 64 + 16 * b:80 + 16 * b]], -1).astype(np.float64)
+                m = abs(part).max()
+                q8 = abs(np.rint(part * (127 / m))).sum(-1)
+                slack += (q8[:, None] + 64 * 32) * (m * scales[ids, h, b].astype(np.float64))[None]
+            k = c.k64[s][:whole * G, h].view(whole, G, D).cpu().numpy()
+            top = np.einsum("ptd,gd->gpt", k, mine.astype(np.float64)).max(-1)               # [query, page]
+            assert (127 * top <= score[None] + slack).all()
