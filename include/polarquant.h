@@ -473,7 +473,8 @@ size_t pq_bound_scales_bytes_per_page(const pq_layout* layout);
  *   max_new_tokens  host-known upper bound of lens_after - lens_before; groups past what so many tokens can complete get no bounds
  *   bounds, bound_scales   device (16-byte aligned), written for the named pages only; page ids outside [0, n_pool_pages) are skipped, and so are
  *                   pages past max_pages_per_seq
- * n_seqs == 0 or max_new_tokens == 0 is a no-op.
+ * n_seqs == 0 or max_new_tokens == 0 is a no-op.  A step in which no page is completed takes a launch all the same (4 us), as the lengths are the device's: a
+ * program that knows them may leave the call out.
  */
 int pq_bound_pages(const pq_layout* layout, const void* codes_pool, const void* params_pool, int64_t n_pool_pages,
                    const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* lens_before, const int32_t* lens_after,
@@ -502,6 +503,8 @@ size_t pq_select_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_
  *   selected_lens   device int32 [n_seqs][n_kv_heads], written: tokens in the chosen pages (the last of them is the sequence's last)
  *   workspace       >= pq_select_workspace_bytes(...); contents are scratch.  Calls that overlap need one each, captured ones too
  * n_seqs * n_kv_heads <= 65535, n_pool_pages * n_kv_heads < 2^31 (PQ_ERR_UNSUPPORTED beyond).
+ * How a launch is shared out goes by n_seqs * n_kv_heads and max_seq_len, as if sequences were alike.  From 256 (sequence, KV head)s on each is one work-group's, so that a sequence
+ * far longer than the others is better chosen for in a call of its own (8 KV heads: one of 4096 pages among 31 of 64 52 us; in two calls 16 + 5).
  */
 int pq_select_pages(const pq_layout* layout, const void* q, pq_dtype q_dtype, int32_t n_seqs, int32_t n_q_heads, const void* bounds,
                     const void* bound_scales, int64_t n_pool_pages, const int32_t* block_table, int32_t max_pages_per_seq,
@@ -519,6 +522,8 @@ size_t pq_sparse_workspace_bytes(const pq_layout* layout, int32_t n_seqs, int32_
  *   bounds, bound_scales   both NULL: `selected` and `selected_lens` are given, as pq_select_pages wrote them for the same lengths (the choice
  *                   of another layer, say); block_table, seq_lens, n_first and n_last are then not looked at (the first two may be NULL)
  *   workspace       >= pq_sparse_workspace_bytes(...)
+ * Chunks are cut as if every sequence had n_selected pages, or max_seq_len tokens if that is less; from 257 (sequence, KV head)s on each is one chunk.  A few sequences with many
+ * chosen pages beside many that have few are better two calls (8 KV heads: one of 256 chosen pages beside 63 of 8 255 us; in two calls 29 + 31).
  */
 int pq_sparse_attention(const pq_layout* layout, const void* q, pq_dtype q_dtype, int32_t n_seqs, int32_t n_q_heads, const void* codes_pool,
                         const void* params_pool, const void* v_pool, int32_t v_bits, const void* v_params_pool, const void* bounds,

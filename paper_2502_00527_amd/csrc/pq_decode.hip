@@ -590,7 +590,7 @@ extern "C" int pq_window_attention(const pq_layout* layout, const void* q, pq_dt
 }
 
 // Chunks as for a window: sequences are alike, as many chunks as start at once (the general plan makes chunks of 8 or 16 pages: 128 units of 48 pages are
-// then 384 work-groups, 46.8 us; in fours of 12 pages 512, 44.3).
+// then 384 work-groups, 46.8 us; in fours of 12 pages 512, 44.3).  That is assumed, not known: 512 units of which 8 have 256 pages and the others 8 take 255 us, in two launches 29 + 31.
 static ChunkPlan plan_alike(const pq_layout* layout, int32_t n_seqs, int32_t max_seq_len) { return plan_window(layout, n_seqs, max_seq_len); }
 
 // An upper bound over all smaller batches and lengths: a serving loop makes one workspace.

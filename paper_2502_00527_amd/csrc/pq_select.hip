@@ -15,8 +15,9 @@
 // Bound: waits for memory and for one another, one after the other -- table, bounds, keys of the other work-groups, counts.  One sequence of 1024 pages (8 KV
 // heads) 8.0 us, 32 ragged ones of up to 256 6.7, a launch's own time being 3.6; 32 of 1024 pages, 72 MB, 22.
 //
-// The grid runs over sequences first: work-groups of one sequence then tend to start on the same of the 8 dies, whose caches keep lines that its heads share, the
-// block table's and the scales' (16 bytes a head).  64 sequences of 256 pages 12.0 -> 10.3 us, 16 of 1024 14.5 -> 12.5, 32 ragged ones of up to 256 7.3 -> 6.7.
+// The grid runs over sequences first: work-groups go round the 8 dies, so that those of one sequence tend to start on one die where n_seqs is a multiple of 8, on two or four of them where it
+// has a factor of 4 or 2, and its cache keeps lines that heads share, the block table's and the scales' (16 bytes a head).  64 sequences of 256 pages 12.0 -> 10.3 us, 16 of 1024
+// 14.5 -> 12.5, 32 ragged ones of up to 256 7.3 -> 6.7.  Other numbers of 256 pages: 60 10.0 us where 64 take 10.0, 20 6.7, 13 6.6 where 16 take 6.6.
 //
 // A choice is a row of a block table: page and KV head are one index into the pools taken head by head, so that attention over the
 // chosen pages is decode attention of n_seqs * n_kv_heads sequences with one KV head each.
@@ -307,6 +308,7 @@ int64_t most_pages(int32_t max_seq_len) { return (static_cast<int64_t>(max_seq_l
 // no more than a work-group a compute unit, or a batch.  (8 units of 1024 pages 8.2 us, a work-group each 15.6; 128 of 512 10.5 and 11.5; 256 of 512 12.3 and 12.4, of 1024 21.7 and 22.0; 512 of 512 22.1
 // and 20.7, 1024 of 312 29.0 and 25.8.
 // With twice as many work-groups 32 units of 1024 pages 10.7 instead of 9.3.)
+// All of these are of equal lengths, and the rule knows no others: it goes by max_seq_len.  256 units of which 8 have 4096 pages and the others 64 take 52 us, the 8 alone 16.
 int32_t pages_of_part(const pq_layout* l, int32_t n_seqs, int32_t max_seq_len) {
   const int64_t pages = most_pages(max_seq_len), units = static_cast<int64_t>(n_seqs) * l->n_kv_heads;
   if (pages <= kBatchPages || (units >= kComputeUnits && pages <= kMostKeys)) return static_cast<int32_t>(std::min<int64_t>(pages, kMostKeys));
